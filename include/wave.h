@@ -301,6 +301,146 @@ wave_status wave_full_attention_decode(const void *q, const void *K, const void 
                                        int Hq, int Hkv, int N, int d, float *out, float *lse,
                                        void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * The plain cache: rotary positions, and one cache of raw rows per sequence
+ * that grows token by token, is attended exactly (alone or behind a prefix that
+ * the whole batch shares) and is kept at a budget by what its rows are worth.
+ * It holds what no index holds: the tokens of ragged conversations, read by
+ * the same decode conventions (q, out, lse) as above, so that its lse merges
+ * with that of any other zone.
+ * ------------------------------------------------------------------------- */
+
+/* Rotary positions with 1 .. WAVE_ROTARY_MAX_AXES axes.  The first rot_dim
+ * channels of a row form rot_dim / 2 pairs, the others stay as they are.  Pair
+ * i of a token turns by the angle coordinate[axis[i]] * inv_freq[i]:
+ *   (x, y) -> (x cos - y sin, x sin + y cos).
+ * Plain data: wave_rotary_plan fills it, and a caller with frequencies of its
+ * own (a scaled or a learned ladder) writes them into inv_freq afterwards. */
+enum { WAVE_ROTARY_MAX_AXES = 4, WAVE_ROTARY_MAX_PAIRS = 64 };
+typedef enum {
+  WAVE_ROTARY_RUNS = 0,    /* axis 0 has the first sections[0] pairs, axis 1 the next, ... */
+  WAVE_ROTARY_TURNS = 1,   /* pairs dealt out in turn: axis 0, 1, .., 0, 1, .. while an axis has some left */
+  WAVE_ROTARY_LADDERS = 2  /* as runs, and the frequencies of every axis start anew */
+} wave_rotary_order;
+typedef enum {
+  WAVE_ROTARY_HALVES = 0,   /* pair i: channels i and i + rot_dim / 2 */
+  WAVE_ROTARY_NEIGHBOURS = 1 /* pair i: channels 2 i and 2 i + 1      */
+} wave_rotary_pairing;
+typedef struct {
+  int32_t rot_dim;          /* rotated channels: a multiple of 16, at most d           */
+  int32_t n_axes;
+  int32_t pairing;          /* wave_rotary_pairing                                     */
+  int32_t axis[WAVE_ROTARY_MAX_PAIRS];     /* axis of each pair, < n_axes              */
+  double inv_freq[WAVE_ROTARY_MAX_PAIRS];  /* radians per position of each pair        */
+} wave_rotary;
+
+/* Host only.  sections: HOST [n_axes], pairs of each axis, adding up to
+ * rot_dim / 2 (an axis may have none).  inv_freq[i] = base^(-i / (rot_dim / 2)),
+ * with WAVE_ROTARY_LADDERS base^(-i' / sections[a]) for the i'-th pair of axis a.
+ * WAVE_ERR_SHAPE: rot_dim not a multiple of 16 in 16 .. 128, or sections that do
+ * not add up; WAVE_ERR_ARG: anything else (base must be finite and > 0). */
+wave_status wave_rotary_plan(wave_rotary *rotary, int rot_dim, double base, const int32_t *sections,
+                             int n_axes, int order, int pairing);
+
+/* Rotates x into y.
+ *   x, y       DEVICE [B,H,N,d] dtype, 16-byte aligned; y may be x, and must not
+ *              overlap it otherwise
+ *   coords     DEVICE [n_axes,B,N] int32, any values
+ * Angles are formed in fp64 (their error is about 2^-53 of the angle, so positions of a million
+ * are as exact as small ones), sine and cosine and the products in fp32, and
+ * each result is rounded once to dtype.  H and N may be anything >= 1. */
+wave_status wave_rotary_apply(const void *x, const int32_t *coords, const wave_rotary *rotary, int dtype,
+                              int B, int H, int N, int d, void *y, void *hip_stream);
+
+/* One cache of raw key and value rows per (sequence, KV head).  Plain data, all
+ * arrays caller-owned; a field that a call does not need may be NULL.  Rows of
+ * sequence b are the first lengths[b] of each of its units, in no order that
+ * matters; what lies behind them is never read and may hold anything.  The
+ * library reads lengths on the device: a value outside 0 .. capacity counts as
+ * the nearer of the two. */
+typedef struct {
+  int32_t dtype;            /* wave_dtype                                              */
+  int32_t B, Hkv, d;
+  int32_t capacity;         /* rows allocated per unit                                 */
+  void *k, *v;              /* DEVICE [B,Hkv,capacity,d] dtype, 16-byte aligned        */
+  int32_t *positions;       /* DEVICE [B,Hkv,capacity] number of each row's token in   */
+                            /*        its sequence                                     */
+  float *weights;           /* DEVICE [B,Hkv,capacity] attention weight received so far */
+  int32_t *lengths;         /* DEVICE [B] rows in use                                  */
+  int32_t *tokens;          /* DEVICE [B] tokens appended so far, evicted ones too     */
+} wave_cache;
+
+/* Appends n_new tokens (1 for a decode step, any number for a prompt) to every sequence:
+ * keys and queries are rotated as by wave_rotary_apply, and token t of sequence
+ * b becomes row lengths[b] + t of its units, with position tokens[b] + t and
+ * weight 0.  q is only rotated; it may be used by wave_cache_attention_decode
+ * as it is where n_new = 1.
+ *   k_new, v_new  DEVICE [B,Hkv,n_new,d] dtype
+ *   q             DEVICE [B,Hq,n_new,d] dtype or NULL (then Hq and q_out are not
+ *                 looked at); q_out the same shape, may be q
+ *   counts        DEVICE [B] int32 or NULL: only the first counts[b] of the n_new
+ *                 tokens exist (a padded batch; a value outside 0 .. n_new counts as
+ *                 the nearer); nothing of the others is written, their rows of
+ *                 q_out included
+ *   rotary        HOST, or NULL: keys go in as they are; q must then be NULL
+ *   coords        DEVICE [n_axes,B,n_new] int32, or NULL: tokens[b] + t on every axis
+ *   lengths_out, tokens_out  DEVICE [B]: the numbers after the call.  Each may be
+ *                 the cache's own array (updated in place) and must not overlap it
+ *                 otherwise; tokens_out may be NULL where cache->tokens is.
+ * cache->positions, weights and tokens may be NULL (positions and NULL coords
+ * need tokens).  The caller keeps lengths[b] + counts[b] <= capacity: rows that
+ * do not fit are left out, and lengths and tokens advance by those that did. */
+wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const void *v_new, const void *q,
+                              int Hq, int n_new, const int32_t *counts, const wave_rotary *rotary,
+                              const int32_t *coords, void *q_out, int32_t *lengths_out,
+                              int32_t *tokens_out, void *hip_stream);
+
+/* Exact attention of one token per sequence over a prefix that all sequences
+ * share and the sequence's own rows, under one softmax:
+ *   o = softmax([q Kp^T, q K_b^T] / sqrt(d)) [Vp; V_b].
+ * The prefix is read once for the batch (all B * G queries of a KV head
+ * multiply the same rows), the own rows once per KV head.
+ *   q             DEVICE [B,Hq,d] dtype, 16-byte aligned
+ *   prefix_k, prefix_v  DEVICE [Hkv,P,d] dtype, 16-byte aligned; may be NULL where P = 0
+ *   weights_out   DEVICE [B,Hkv,capacity] fp32 or NULL.  Each own row j of a unit
+ *                 gets decay * weights[j] + the sum over the unit's G heads of the
+ *                 softmax weight that row j received (the prefix's share counts in
+ *                 the normaliser).  May be cache->weights, and must not overlap it
+ *                 otherwise; rows behind the length are left as they are.  decay in
+ *                 0 .. 1; with 0 the old weights are not read
+ *   out           DEVICE [B,Hq,d] fp32;  lse DEVICE [B,Hq] fp32 (natural log)
+ *   workspace     DEVICE, 256-byte aligned, >= wave_cache_attention_workspace(...)
+ * A sequence with neither prefix nor own rows has out = 0 and lse = -infinity.
+ * Scores are exact products of the stored values, summed in fp32; the softmax and
+ * all sums are fp32.  For bf16 caches a softmax weight meets the values as two
+ * bf16 numbers that together hold 16 of its bits. */
+size_t wave_cache_attention_workspace(const wave_cache *cache, int Hq, int P, int accumulate);
+wave_status wave_cache_attention_decode(const void *q, int Hq, const wave_cache *cache,
+                                        const void *prefix_k, const void *prefix_v, int P, float decay,
+                                        float *weights_out, float *out, float *lse, void *workspace,
+                                        size_t workspace_bytes, void *hip_stream);
+
+/* Eviction by accumulated attention weight: every unit of a sequence with more
+ * than n_keep rows keeps n_keep of them.  Rows whose position is below n_sink or
+ * among the last n_local of the sequence's tokens come first, then the rows of
+ * the largest weight; equal ones: the lower row first; a weight that is not a number
+ * counts as less than any other.  A kept row below n_keep stays where it is; the
+ * i-th kept row from n_keep on moves to the i-th row below it that left.  So in
+ * place only the moved rows are read and written, and the order of the rows
+ * changes: positions says which is which.
+ *   from          the cache (weights, positions, tokens and lengths are needed)
+ *   to            what it becomes: to->k and to->v are from's own (in place) or
+ *                 other arrays (all kept rows are written there, e.g. into a
+ *                 smaller cache); the same choice, each on its own, for positions,
+ *                 weights, lengths and tokens.  An array that both name needs the same
+ *                 capacity, others must not overlap.  to->capacity >= min(n_keep,
+ *                 from->capacity).  Rows behind the new length are left as they are
+ *   n_sink + n_local <= n_keep (WAVE_ERR_ARG otherwise)
+ *   workspace     DEVICE, 256-byte aligned, >= wave_cache_evict_workspace(...) */
+size_t wave_cache_evict_workspace(const wave_cache *from, int n_keep);
+wave_status wave_cache_evict(const wave_cache *from, const wave_cache *to, int n_keep, int n_sink,
+                             int n_local, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Test hook, host only: the k_s distinct seed-token indices (relative to the
  * segment start) with which segment s of unit (b, h) starts k-means: the first
  * k_s entries of a Fisher-Yates shuffle of 0..L_s-1 driven by splitmix64 keyed

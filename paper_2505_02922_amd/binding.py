@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, List, Optional, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -27,6 +27,9 @@ EXPORTS = ("wave_index_plan", "wave_index_build", "wave_index_append_plan", "wav
            "wave_attention_decode_static",
            "wave_attention_decode_budget_workspace", "wave_attention_decode_budget",
            "wave_full_attention_workspace", "wave_full_attention_decode", "wave_init_indices",
+           "wave_rotary_plan", "wave_rotary_apply", "wave_cache_append",
+           "wave_cache_attention_workspace", "wave_cache_attention_decode",
+           "wave_cache_evict_workspace", "wave_cache_evict",
            "wave_kmeans_assign_step", "wave_calibration_copy", "wave_calibration_read",
            "wave_profile_enable", "wave_profile_read", "wave_status_string")
 
@@ -46,6 +49,24 @@ class wave_index(ctypes.Structure):
                 ("appended_segments", ctypes.c_int32), ("update_segment_len", ctypes.c_int32),
                 ("update_clusters", ctypes.c_int32), ("row_capacity", ctypes.c_int32),
                 ("cluster_capacity", ctypes.c_int32)]
+
+
+WAVE_ROTARY_MAX_AXES, WAVE_ROTARY_MAX_PAIRS = 4, 64
+WAVE_ROTARY_RUNS, WAVE_ROTARY_TURNS, WAVE_ROTARY_LADDERS = 0, 1, 2
+WAVE_ROTARY_HALVES, WAVE_ROTARY_NEIGHBOURS = 0, 1
+
+
+class wave_rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("axis", ctypes.c_int32 * WAVE_ROTARY_MAX_PAIRS),
+                ("inv_freq", ctypes.c_double * WAVE_ROTARY_MAX_PAIRS)]
+
+
+class wave_cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("weights", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("tokens", ctypes.c_void_p)]
 
 
 class WaveError(RuntimeError):
@@ -86,6 +107,17 @@ def lib() -> ctypes.CDLL:
         L.wave_full_attention_workspace.argtypes = [i32, i32, i32, i32]
         L.wave_full_attention_decode.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp,
                                                  sz, vp]
+        L.wave_rotary_plan.argtypes = [ctypes.POINTER(wave_rotary), i32, ctypes.c_double,
+                                       ctypes.POINTER(ctypes.c_int32), i32, i32, i32]
+        L.wave_rotary_apply.argtypes = [vp, vp, ctypes.POINTER(wave_rotary), i32, i32, i32, i32, i32, vp, vp]
+        L.wave_cache_append.argtypes = [ctypes.POINTER(wave_cache), vp, vp, vp, i32, i32, vp,
+                                        ctypes.POINTER(wave_rotary), vp, vp, vp, vp, vp]
+        L.wave_cache_attention_workspace.argtypes = [ctypes.POINTER(wave_cache), i32, i32, i32]
+        L.wave_cache_attention_decode.argtypes = [vp, i32, ctypes.POINTER(wave_cache), vp, vp, i32,
+                                                  ctypes.c_float, vp, vp, vp, vp, sz, vp]
+        L.wave_cache_evict_workspace.argtypes = [ctypes.POINTER(wave_cache), i32]
+        L.wave_cache_evict.argtypes = [ctypes.POINTER(wave_cache), ctypes.POINTER(wave_cache), i32, i32, i32,
+                                       vp, sz, vp]
         L.wave_init_indices.argtypes = [u64, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int32)]
         L.wave_kmeans_assign_step.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp]
         L.wave_calibration_copy.argtypes = [vp, vp, sz, i32, vp]
@@ -101,6 +133,8 @@ def lib() -> ctypes.CDLL:
         L.wave_full_attention_workspace.restype = sz
         L.wave_attention_decode_static_capacity.restype = sz
         L.wave_attention_decode_budget_workspace.restype = sz
+        L.wave_cache_attention_workspace.restype = sz
+        L.wave_cache_evict_workspace.restype = sz
         _lib = L
     return _lib
 
@@ -387,6 +421,224 @@ def wave_full_attention_decode(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor
     if st != 0:
         raise WaveError(st, "wave_full_attention_decode")
     return out, lse
+
+
+def _require(ok: bool, status: int, where: str) -> None:
+    if not ok:
+        raise WaveError(status, where)
+
+
+def _require_on_gpu(device: torch.device, where: str, *tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor on the one GPU `device` (a kernel would fault on another's memory)."""
+    _require(device.type == "cuda" and all(t is None or t.device == device for t in tensors), 1, where)
+
+
+def _require_dense(where: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...]) -> None:
+    """What a call writes, or keeps from call to call, is taken as it is: never a copy of it."""
+    _require(t.dtype == dtype, 3, where)
+    _require(tuple(t.shape) == tuple(shape), 2, where)
+    _require(t.is_contiguous(), 1, where)
+
+
+def _enqueue(where: str, device: torch.device, *args) -> None:
+    """Calls a C entry point with `device`'s current stream as its last argument, on that device."""
+    if device.index == torch.cuda.current_device():
+        st = getattr(lib(), where)(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = getattr(lib(), where)(*args, torch.cuda.current_stream().cuda_stream)
+    if st != 0:
+        raise WaveError(st, where)
+
+
+def wave_rotary_plan(rot_dim: int, base: float, sections: Optional[Sequence[int]] = None,
+                     order: int = WAVE_ROTARY_RUNS, pairing: int = WAVE_ROTARY_HALVES) -> wave_rotary:
+    """Rotary positions of rot_dim channels.  sections: pairs of each axis (default: one axis).  Other
+    frequencies (a scaled ladder) may be written into the result's inv_freq."""
+    sections = [rot_dim // 2] if sections is None else list(sections)
+    r = wave_rotary()
+    st = lib().wave_rotary_plan(ctypes.byref(r), rot_dim, base, (ctypes.c_int32 * max(len(sections), 1))(*sections),
+                                len(sections), order, pairing)
+    if st != 0:
+        raise WaveError(st, "wave_rotary_plan")
+    return r
+
+
+def wave_rotary_apply(x: torch.Tensor, coords: torch.Tensor, rotary: wave_rotary,
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [B, H, N, d] f32 or bf16, coords [n_axes, B, N] int32 -> x rotated (into `out`, which may be x
+    itself: rotated in place)."""
+    where = "wave_rotary_apply"
+    _require(x.dim() == 4 and coords.dim() == 3, 2, where)
+    B, H, N, d = x.shape
+    _require(coords.dtype == torch.int32, 3, where)
+    _require(tuple(coords.shape) == (rotary.n_axes, B, N), 2, where)
+    _require_on_gpu(x.device, where, coords, out)
+    if out is None:
+        x = x.contiguous()
+        out = torch.empty_like(x)
+    else:
+        _require_dense(where, out, x.dtype, x.shape)
+        x = x.contiguous()
+    coords = coords.contiguous()
+    if x.numel():
+        _enqueue(where, x.device, x.data_ptr(), coords.data_ptr(), ctypes.byref(rotary), _dtype_code(x.dtype),
+                 B, H, N, d, out.data_ptr())
+    return out
+
+
+class Cache:
+    """A wave_cache struct plus the torch tensors that own its arrays: k and v [B, Hkv, capacity, d],
+    positions and weights [B, Hkv, capacity], lengths and tokens [B]."""
+
+    def __init__(self, c: wave_cache, tensors: Dict[str, Optional[torch.Tensor]], dtype: torch.dtype,
+                 device: torch.device):
+        self.c = c
+        self.t = tensors
+        self.dtype = dtype
+        self.device = device
+        self.B, self.Hkv, self.d, self.capacity = c.B, c.Hkv, c.d, c.capacity
+
+    def __getattr__(self, name):
+        t = self.__dict__.get("t", {})
+        if name in t:
+            return t[name]
+        raise AttributeError(name)
+
+
+def cache_from_tensors(k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
+                       weights: Optional[torch.Tensor], lengths: torch.Tensor,
+                       tokens: Optional[torch.Tensor]) -> Cache:
+    """A cache over tensors that the caller holds; they are taken as they are (contiguous, one GPU)."""
+    where = "cache_from_tensors"
+    _require(k.dim() == 4, 2, where)
+    B, Hkv, capacity, d = k.shape
+    _require_dense(where, k, k.dtype, (B, Hkv, capacity, d))
+    _require_dense(where, v, k.dtype, (B, Hkv, capacity, d))
+    for t, dt in ((positions, torch.int32), (weights, torch.float32)):
+        if t is not None:
+            _require_dense(where, t, dt, (B, Hkv, capacity))
+    for t in (lengths, tokens):
+        if t is not None:
+            _require_dense(where, t, torch.int32, (B,))
+    _require(all(t is None or t.device == k.device for t in (v, positions, weights, lengths, tokens)), 1, where)
+    tensors = {"k": k, "v": v, "positions": positions, "weights": weights, "lengths": lengths, "tokens": tokens}
+    c = wave_cache()
+    c.dtype, c.B, c.Hkv, c.d, c.capacity = _dtype_code(k.dtype), B, Hkv, d, capacity
+    for name, t in tensors.items():
+        setattr(c, name, _ptr(t))
+    return Cache(c, tensors, k.dtype, k.device)
+
+
+def alloc_cache(dtype: torch.dtype, B: int, Hkv: int, d: int, capacity: int, device="cuda") -> Cache:
+    """An empty cache."""
+    rows, new = (B, Hkv, capacity), dict(device=torch.empty(0, device=device).device)
+    return cache_from_tensors(torch.empty(rows + (d,), dtype=dtype, **new), torch.empty(rows + (d,), dtype=dtype, **new),
+                              torch.full(rows, -1, dtype=torch.int32, **new), torch.zeros(rows, **new),
+                              torch.zeros(B, dtype=torch.int32, **new), torch.zeros(B, dtype=torch.int32, **new))
+
+
+def wave_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                      coords: Optional[torch.Tensor] = None, rotary: Optional[wave_rotary] = None,
+                      counts: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                      lengths_out: Optional[torch.Tensor] = None,
+                      tokens_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """k, v [B, Hkv, n, d] and q [B, Hq, n, d] of n new tokens per sequence (counts [B] int32: of its first
+    counts[b]).  Rotates q and k by coords [n_axes, B, n] int32 (None: the tokens' numbers), writes k and v
+    behind each sequence's rows and advances lengths and tokens, in place unless other tensors are given.
+    Returns q rotated (q_out, which may be q)."""
+    where = "wave_cache_append"
+    _require(k.dim() == 4 and k.shape == v.shape and k.shape[:2] == (cache.B, cache.Hkv) and k.shape[3] == cache.d, 2, where)
+    _require(k.dtype == v.dtype == cache.dtype, 3, where)
+    B, _, n, d = k.shape
+    Hq = 0
+    if q is not None:
+        _require(q.dim() == 4 and q.shape[0] == B and tuple(q.shape[2:]) == (n, d), 2, where)
+        _require(q.dtype == cache.dtype, 3, where)
+        Hq = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if counts is None else \
+                torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        _require_dense(where, q_out, q.dtype, q.shape)
+        q = q.contiguous()
+    if coords is not None:
+        _require(coords.dtype == torch.int32, 3, where)
+        _require(rotary is not None, 1, where)
+        _require(tuple(coords.shape) == (rotary.n_axes, B, n), 2, where)
+        coords = coords.contiguous()
+    if counts is not None:
+        _require(counts.dtype == torch.int32, 3, where)
+        _require(tuple(counts.shape) == (B,), 2, where)
+        counts = counts.contiguous()
+    lengths_out = cache.lengths if lengths_out is None else lengths_out
+    tokens_out = cache.tokens if tokens_out is None else tokens_out
+    for t in (lengths_out, tokens_out):
+        if t is not None:
+            _require_dense(where, t, torch.int32, (B,))
+    _require_on_gpu(cache.device, where, k, v, q, q_out, coords, counts, lengths_out, tokens_out)
+    k, v = k.contiguous(), v.contiguous()
+    _enqueue(where, cache.device, ctypes.byref(cache.c), _ptr(k), _ptr(v), _ptr(q), Hq, n, _ptr(counts),
+             ctypes.byref(rotary) if rotary is not None else None, _ptr(coords), _ptr(q_out) if q is not None else None,
+             _ptr(lengths_out), _ptr(tokens_out))
+    return q_out if q is not None else None
+
+
+def wave_cache_attention_workspace(cache: Cache, Hq: int, P: int, accumulate: bool) -> int:
+    return int(lib().wave_cache_attention_workspace(ctypes.byref(cache.c), Hq, P, 1 if accumulate else 0))
+
+
+def wave_cache_attention_decode(q: torch.Tensor, cache: Cache, prefix_k: Optional[torch.Tensor] = None,
+                                prefix_v: Optional[torch.Tensor] = None, decay: float = 1.0,
+                                weights_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                                lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """q [B, Hq, d] against the prefix [Hkv, P, d] that the batch shares (None: there is none) and each
+    sequence's rows, under one softmax.  weights_out (cache.weights: in place) receives decay * weights +
+    what each row got in this step.  Returns (out [B,Hq,d] f32, lse [B,Hq] f32)."""
+    where = "wave_cache_attention_decode"
+    _require(q.dim() == 3 and q.shape[0] == cache.B and q.shape[2] == cache.d, 2, where)
+    _require(q.dtype == cache.dtype, 3, where)
+    _require((prefix_k is None) == (prefix_v is None), 1, where)
+    B, Hq, d = q.shape
+    P = 0
+    if prefix_k is not None:
+        _require(prefix_k.dim() == 3 and prefix_k.shape == prefix_v.shape, 2, where)
+        _require(prefix_k.shape[0] == cache.Hkv and prefix_k.shape[2] == d, 2, where)
+        _require(prefix_k.dtype == prefix_v.dtype == cache.dtype, 3, where)
+        P = prefix_k.shape[1]
+        prefix_k, prefix_v = prefix_k.contiguous(), prefix_v.contiguous()
+    if weights_out is not None:
+        _require_dense(where, weights_out, torch.float32, (B, cache.Hkv, cache.capacity))
+    if out is None:
+        out = torch.empty(B, Hq, d, dtype=torch.float32, device=q.device)
+    if lse is None:
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
+    _require_dense(where, out, torch.float32, (B, Hq, d))
+    _require_dense(where, lse, torch.float32, (B, Hq))
+    if ws is None:
+        ws = workspace(wave_cache_attention_workspace(cache, Hq, P, weights_out is not None), cache.device)
+    _require_on_gpu(cache.device, where, q, prefix_k, prefix_v, weights_out, out, lse, ws)
+    q = q.contiguous()
+    _enqueue(where, cache.device, q.data_ptr(), Hq, ctypes.byref(cache.c), _ptr(prefix_k), _ptr(prefix_v), P, decay,
+             _ptr(weights_out), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+    return out, lse
+
+
+def wave_cache_evict_workspace(cache: Cache, n_keep: int) -> int:
+    return int(lib().wave_cache_evict_workspace(ctypes.byref(cache.c), n_keep))
+
+
+def wave_cache_evict(cache: Cache, n_keep: int, n_sink: int, n_local: int, to: Optional[Cache] = None,
+                     ws: Optional[torch.Tensor] = None) -> Cache:
+    """Keeps the n_keep rows of every unit that are the first n_sink and last n_local tokens of the sequence or have
+    the largest weights; in place, or into `to`.  Returns the cache that holds them."""
+    where = "wave_cache_evict"
+    to = cache if to is None else to
+    if ws is None:
+        ws = workspace(wave_cache_evict_workspace(cache, n_keep), cache.device)
+    _require_on_gpu(cache.device, where, to.k, ws)
+    _enqueue(where, cache.device, ctypes.byref(cache.c), ctypes.byref(to.c), n_keep, n_sink, n_local, ws.data_ptr(),
+             ws.numel() * ws.element_size())
+    return to
 
 
 def wave_init_indices(seed: int, b: int, h: int, s: int, L_s: int, k_s: int) -> List[int]:

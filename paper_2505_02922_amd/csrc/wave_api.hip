@@ -1,6 +1,7 @@
 // C-ABI entry points of the wave-index library: planning, argument checks,
 // dispatch to the build and decode launch code, the host-side seed-point hook
 // and the event profiler.
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -488,6 +489,219 @@ wave_status wave_full_attention_decode(const void* q, const void* K, const void*
     return WAVE_ERR_WORKSPACE;
   return launch_full_attention(q, K, V, dtype, B, Hq, Hkv, N, d, out, lse, workspace,
                                static_cast<hipStream_t>(hip_stream));
+}
+
+// ----------------------------------------------------------------------------
+// Rotary positions and the plain cache
+// ----------------------------------------------------------------------------
+static bool overlaps(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+// the same array, or arrays that have nothing in common
+static bool same_or_apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  return a == b || !overlaps(a, a_bytes, b, b_bytes);
+}
+static size_t elem_bytes(int dtype) { return dtype == WAVE_BF16 ? 2 : 4; }
+// workgroups of 256 threads in one launch dimension (a dimension has fewer than 2^32 threads)
+constexpr long long kMaxGrid = 1ll << 24;
+
+wave_status wave_rotary_plan(wave_rotary* rotary, int rot_dim, double base, const int32_t* sections, int n_axes,
+                             int order, int pairing) {
+  if (!rotary || !sections || !(base > 0.0) || !(base < HUGE_VAL)) return WAVE_ERR_ARG;
+  if (n_axes < 1 || n_axes > WAVE_ROTARY_MAX_AXES) return WAVE_ERR_ARG;
+  if (order != WAVE_ROTARY_RUNS && order != WAVE_ROTARY_TURNS && order != WAVE_ROTARY_LADDERS) return WAVE_ERR_ARG;
+  if (pairing != WAVE_ROTARY_HALVES && pairing != WAVE_ROTARY_NEIGHBOURS) return WAVE_ERR_ARG;
+  const int pairs = rot_dim / 2;
+  if (rot_dim < 16 || rot_dim > 2 * WAVE_ROTARY_MAX_PAIRS || rot_dim % 16) return WAVE_ERR_SHAPE;
+  long long sum = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (sections[a] < 0) return WAVE_ERR_ARG;
+    sum += sections[a];
+  }
+  if (sum != pairs) return WAVE_ERR_SHAPE;
+  wave_rotary r{};
+  r.rot_dim = rot_dim;
+  r.n_axes = n_axes;
+  r.pairing = pairing;
+  int given[WAVE_ROTARY_MAX_AXES] = {0, 0, 0, 0}, a = 0;
+  for (int i = 0; i < pairs; ++i) {
+    while (given[a] == sections[a]) a = (a + 1) % n_axes;  // (ends: fewer pairs are given than there are)
+    r.axis[i] = a;
+    const double step = order == WAVE_ROTARY_LADDERS ? (double)given[a] / sections[a] : (double)i / pairs;
+    r.inv_freq[i] = pow(base, -step);
+    ++given[a];
+    if (order == WAVE_ROTARY_TURNS) a = (a + 1) % n_axes;
+  }
+  *rotary = r;
+  return WAVE_OK;
+}
+
+static wave_status check_rotary(const wave_rotary* r, int d, RotaryArgs* out) {
+  if (!r || r->n_axes < 1 || r->n_axes > WAVE_ROTARY_MAX_AXES) return WAVE_ERR_ARG;
+  if (r->pairing != WAVE_ROTARY_HALVES && r->pairing != WAVE_ROTARY_NEIGHBOURS) return WAVE_ERR_ARG;
+  if (r->rot_dim < 16 || r->rot_dim > d || r->rot_dim % 16) return WAVE_ERR_SHAPE;
+  *out = RotaryArgs{};
+  out->rot = r->rot_dim;
+  out->pairing = r->pairing;
+  for (int i = 0; i < r->rot_dim / 2; ++i) {
+    if (r->axis[i] < 0 || r->axis[i] >= r->n_axes) return WAVE_ERR_ARG;
+    if (!(fabs(r->inv_freq[i]) < HUGE_VAL)) return WAVE_ERR_ARG;
+    out->axis[i] = r->axis[i];
+    out->turns[i] = r->inv_freq[i] * 0.15915494309189533577;  // 1 / (2 pi)
+  }
+  return WAVE_OK;
+}
+
+wave_status wave_rotary_apply(const void* x, const int32_t* coords, const wave_rotary* rotary, int dtype, int B, int H,
+                              int N, int d, void* y, void* hip_stream) {
+  if (dtype != WAVE_F32 && dtype != WAVE_BF16) return WAVE_ERR_DTYPE;
+  if (!x || !y || !coords || B < 1 || H < 1 || N < 1) return WAVE_ERR_ARG;
+  if (!aligned16(x) || !aligned16(y)) return WAVE_ERR_ARG;
+  if (d != 64 && d != 128) return WAVE_ERR_SHAPE;
+  RotaryArgs rot;
+  const wave_status st = check_rotary(rotary, d, &rot);
+  if (st != WAVE_OK) return st;
+  if ((long long)B * H >= (1ll << 31) || (long long)B * N >= (1ll << 31)) return WAVE_ERR_SHAPE;
+  const size_t bytes = (size_t)B * H * N * d * elem_bytes(dtype);
+  if (!same_or_apart(x, bytes, y, bytes)) return WAVE_ERR_ARG;
+  return launch_rotary(x, coords, rot, dtype, B, H, N, d, y, static_cast<hipStream_t>(hip_stream));
+}
+
+static wave_status check_cache(const wave_cache* c) {
+  if (!c) return WAVE_ERR_ARG;
+  if (c->dtype != WAVE_F32 && c->dtype != WAVE_BF16) return WAVE_ERR_DTYPE;
+  if (c->B < 1 || c->Hkv < 1 || c->capacity < 1) return WAVE_ERR_ARG;
+  if (c->d != 64 && c->d != 128) return WAVE_ERR_SHAPE;
+  if ((long long)c->B * c->Hkv * 8 >= kMaxGrid || c->capacity > (1 << 30)) return WAVE_ERR_SHAPE;
+  return WAVE_OK;
+}
+static wave_status check_cache_buffers(const wave_cache& c) {
+  if (!c.k || !c.v || !c.lengths || !aligned16(c.k) || !aligned16(c.v)) return WAVE_ERR_ARG;
+  return WAVE_OK;
+}
+static size_t cache_rows(const wave_cache& c) { return (size_t)c.B * c.Hkv * c.capacity; }
+static size_t cache_bytes(const wave_cache& c) { return cache_rows(c) * c.d * elem_bytes(c.dtype); }
+
+wave_status wave_cache_append(const wave_cache* cache, const void* k_new, const void* v_new, const void* q, int Hq,
+                              int n_new, const int32_t* counts, const wave_rotary* rotary, const int32_t* coords,
+                              void* q_out, int32_t* lengths_out, int32_t* tokens_out, void* hip_stream) {
+  wave_status st = check_cache(cache);
+  if (st != WAVE_OK) return st;
+  st = check_cache_buffers(*cache);
+  if (st != WAVE_OK) return st;
+  const wave_cache& c = *cache;
+  if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new) || n_new < 1 || !lengths_out) return WAVE_ERR_ARG;
+  if (n_new > (1 << 30)) return WAVE_ERR_SHAPE;
+  if (c.tokens ? !tokens_out : (c.positions || tokens_out || (rotary && !coords))) return WAVE_ERR_ARG;
+  if (!rotary && (q || coords)) return WAVE_ERR_ARG;
+  RotaryArgs rot;
+  if (rotary) {
+    st = check_rotary(rotary, c.d, &rot);
+    if (st != WAVE_OK) return st;
+  }
+  const size_t es = elem_bytes(c.dtype), cb = cache_bytes(c), counts_bytes = sizeof(int32_t) * (size_t)c.B;
+  const size_t kvb = (size_t)c.B * c.Hkv * n_new * c.d * es;
+  if (q) {
+    if (Hq < 1) return WAVE_ERR_ARG;
+    if ((long long)c.B * Hq >= kMaxGrid) return WAVE_ERR_SHAPE;
+    if (!q_out || !aligned16(q) || !aligned16(q_out)) return WAVE_ERR_ARG;
+    const size_t qb = (size_t)c.B * Hq * n_new * c.d * es;
+    if (!same_or_apart(q, qb, q_out, qb) || overlaps(q_out, qb, c.k, cb) || overlaps(q_out, qb, c.v, cb) ||
+        overlaps(q_out, qb, k_new, kvb) || overlaps(q_out, qb, v_new, kvb) || overlaps(q, qb, c.k, cb) ||
+        overlaps(q, qb, c.v, cb))
+      return WAVE_ERR_ARG;
+  }
+  if (overlaps(k_new, kvb, c.k, cb) || overlaps(k_new, kvb, c.v, cb) || overlaps(v_new, kvb, c.k, cb) ||
+      overlaps(v_new, kvb, c.v, cb))
+    return WAVE_ERR_ARG;
+  if (!same_or_apart(lengths_out, counts_bytes, c.lengths, counts_bytes) ||
+      !same_or_apart(tokens_out, counts_bytes, c.tokens, counts_bytes) ||
+      overlaps(lengths_out, counts_bytes, c.tokens, counts_bytes) ||
+      overlaps(tokens_out, counts_bytes, c.lengths, counts_bytes) ||
+      overlaps(lengths_out, counts_bytes, tokens_out, counts_bytes) ||
+      overlaps(counts, counts_bytes, lengths_out, counts_bytes) || overlaps(counts, counts_bytes, tokens_out, counts_bytes))
+    return WAVE_ERR_ARG;
+  if ((long long)c.B * (((long long)n_new + 31) / 32) >= kMaxGrid) return WAVE_ERR_SHAPE;
+  return launch_cache_append(c, k_new, v_new, q, q ? Hq : 0, n_new, counts, rotary ? &rot : nullptr, coords, q_out,
+                             lengths_out, tokens_out, static_cast<hipStream_t>(hip_stream));
+}
+
+static wave_status check_cache_attention(const wave_cache* cache, int Hq, int P) {
+  const wave_status st = check_cache(cache);
+  if (st != WAVE_OK) return st;
+  if (P < 0) return WAVE_ERR_ARG;
+  if (Hq < cache->Hkv || Hq % cache->Hkv != 0 || Hq / cache->Hkv > 8 || P > (1 << 30)) return WAVE_ERR_SHAPE;
+  if ((long long)cache->B * cache->Hkv * (((long long)cache->capacity + 1023) / 1024) >= kMaxGrid) return WAVE_ERR_SHAPE;
+  return WAVE_OK;
+}
+
+size_t wave_cache_attention_workspace(const wave_cache* cache, int Hq, int P, int accumulate) {
+  if (check_cache_attention(cache, Hq, P) != WAVE_OK) return 0;
+  return cache_attend_geometry(*cache, Hq, P, accumulate != 0).total;
+}
+
+wave_status wave_cache_attention_decode(const void* q, int Hq, const wave_cache* cache, const void* prefix_k,
+                                        const void* prefix_v, int P, float decay, float* weights_out, float* out,
+                                        float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  wave_status st = check_cache_attention(cache, Hq, P);
+  if (st != WAVE_OK) return st;
+  st = check_cache_buffers(*cache);
+  if (st != WAVE_OK) return st;
+  if (!q || !aligned16(q) || !out || !lse) return WAVE_ERR_ARG;
+  if (P > 0 && (!prefix_k || !prefix_v || !aligned16(prefix_k) || !aligned16(prefix_v))) return WAVE_ERR_ARG;
+  if (weights_out) {
+    if (!(decay >= 0.f && decay <= 1.f) || (decay > 0.f && !cache->weights)) return WAVE_ERR_ARG;
+    const size_t wb = cache_rows(*cache) * sizeof(float);
+    if (!same_or_apart(weights_out, wb, cache->weights, wb)) return WAVE_ERR_ARG;
+  }
+  const size_t need = cache_attend_geometry(*cache, Hq, P, weights_out != nullptr).total;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need)
+    return WAVE_ERR_WORKSPACE;
+  return launch_cache_attend(q, Hq, *cache, prefix_k, prefix_v, P, decay, weights_out, out, lse, workspace,
+                             static_cast<hipStream_t>(hip_stream));
+}
+
+size_t wave_cache_evict_workspace(const wave_cache* from, int n_keep) {
+  if (check_cache(from) != WAVE_OK || n_keep < 0) return 0;
+  return cache_evict_geometry(*from, n_keep).total;
+}
+
+wave_status wave_cache_evict(const wave_cache* from, const wave_cache* to, int n_keep, int n_sink, int n_local,
+                             void* workspace, size_t workspace_bytes, void* hip_stream) {
+  for (const wave_cache* c : {from, to}) {
+    wave_status st = check_cache(c);
+    if (st != WAVE_OK) return st;
+    st = check_cache_buffers(*c);
+    if (st != WAVE_OK) return st;
+    if (!c->weights || !c->positions || !c->tokens) return WAVE_ERR_ARG;
+  }
+  if (n_keep < 0 || n_sink < 0 || n_local < 0 || (long long)n_sink + n_local > n_keep) return WAVE_ERR_ARG;
+  if (to->dtype != from->dtype || to->B != from->B || to->Hkv != from->Hkv || to->d != from->d) return WAVE_ERR_SHAPE;
+  if (to->capacity < n_keep && to->capacity < from->capacity) return WAVE_ERR_SHAPE;
+  if ((to->k == from->k) != (to->v == from->v)) return WAVE_ERR_ARG;
+  const size_t es = elem_bytes(from->dtype) * from->d;
+  const void* a[6] = {from->k, from->v, from->positions, from->weights, from->lengths, from->tokens};
+  const void* b[6] = {to->k, to->v, to->positions, to->weights, to->lengths, to->tokens};
+  const size_t row[6] = {es, es, sizeof(int32_t), sizeof(float), 0, 0};
+  for (int i = 0; i < 6; ++i)
+    for (int j = 0; j < 6; ++j) {
+      const size_t ab = i < 4 ? cache_rows(*from) * row[i] : sizeof(int32_t) * (size_t)from->B;
+      const size_t bb = j < 4 ? cache_rows(*to) * row[j] : sizeof(int32_t) * (size_t)to->B;
+      if (i == j && a[i] == b[j]) {
+        if (i < 4 && from->capacity != to->capacity) return WAVE_ERR_ARG;
+      } else if (overlaps(a[i], ab, b[j], bb)) {
+        return WAVE_ERR_ARG;
+      }
+      if (i < j) {  // to's own arrays are written side by side
+        const size_t ib = i < 4 ? cache_rows(*to) * row[i] : sizeof(int32_t) * (size_t)to->B;
+        if (overlaps(b[i], ib, b[j], bb)) return WAVE_ERR_ARG;
+      }
+    }
+  const size_t need = cache_evict_geometry(*from, n_keep).total;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need)
+    return WAVE_ERR_WORKSPACE;
+  return launch_cache_evict(*from, *to, n_keep, n_sink, n_local, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
 wave_status wave_init_indices(uint64_t seed, int b, int h, int s, int L_s, int k_s, int32_t* out) {

@@ -349,6 +349,38 @@ wave_status launch_append(const wave_index& old_ix, const void* K_new, const voi
 wave_status launch_assign_step(const void* xhat, const void* chat, int dtype, int L_s, int k_s, int d,
                                int32_t* assign, void* ws, hipStream_t st);
 
+// The plain cache (wave_cache.hip, wave_cache_attention.hip).  Lengths are the device's, so a launch is laid out for the
+// capacity and finds its own share of the rows that are there.
+// Rotary plan as the kernels read it: turns instead of radians, so that the reduction of an angle is exact.
+struct RotaryArgs {
+  double turns[WAVE_ROTARY_MAX_PAIRS];  // of a circle per position
+  int axis[WAVE_ROTARY_MAX_PAIRS];
+  int rot, pairing;
+};
+wave_status launch_rotary(const void* x, const int32_t* coords, const RotaryArgs& rot, int dtype, int B, int H,
+                          int N, int d, void* y, hipStream_t st);
+wave_status launch_cache_append(const wave_cache& cache, const void* k_new, const void* v_new, const void* q, int Hq,
+                                int n_new, const int32_t* counts, const RotaryArgs* rot, const int32_t* coords,
+                                void* q_out, int32_t* lengths_out, int32_t* tokens_out, hipStream_t st);
+struct CacheAttendGeom {
+  int target, pieces;        // pieces of own rows per KV head: aimed at, and room for
+  int mtile, mtiles;         // query rows of a prefix workgroup, workgroups over the B * G query rows
+  int prefix_rows, splits;   // prefix rows per workgroup, workgroups over the prefix
+  int zrow;                  // floats per head in the scores
+  size_t off_z, off_ml, off_acc, off_pml, off_pacc, total;
+};
+CacheAttendGeom cache_attend_geometry(const wave_cache& cache, int Hq, int P, bool accumulate);
+wave_status launch_cache_attend(const void* q, int Hq, const wave_cache& cache, const void* prefix_k,
+                                const void* prefix_v, int P, float decay, float* weights_out, float* out, float* lse,
+                                void* ws, hipStream_t st);
+struct CacheEvictGeom {
+  int moves;                 // room for moved rows per unit
+  size_t off_count, off_hole, off_mover, off_source, total;
+};
+CacheEvictGeom cache_evict_geometry(const wave_cache& from, int n_keep);
+wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int n_keep, int n_sink, int n_local,
+                               void* ws, hipStream_t st);
+
 // splitmix64-keyed Fisher-Yates seed points, shared by the host hook and the device kernel.
 __host__ __device__ inline uint64_t splitmix64_next(uint64_t& state) {
   state += 0x9E3779B97F4A7C15ull;
