@@ -107,18 +107,26 @@ struct Step<bf16_t, D> {
     }
     return r;
   }
-  // A weight as two bf16 numbers: the nearest, and the nearest to what that left.  Each is off by at most 2^-9 of its own,
-  // so the weight by 2^-18: with one bf16 number alone the outputs, which are fp32, would be off by 2^-9 a term.
+  // A weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the product with
+  // the values loses nothing.  (Two numbers, each the nearest, hold 16 bits; outputs are then off by 2e-6 of their norm,
+  // twice what the fp32 sums cost.)
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
-    bf16x8 hi, lo;
+    uint32_t w[3][4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) hi[j] = (__bf16)p[j];
+    for (int j = 0; j < 4; ++j) {
+      float x = p[2 * j], y = p[2 * j + 1];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) lo[j] = (__bf16)(p[j] - (float)hi[j]);
+      for (int n = 0; n < 3; ++n) {
+        w[n][j] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+        x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+      }
+    }
 #pragma unroll
-    for (int a = 0; a < CH; ++a) {
-      o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], hi, o[a], 0, 0, 0);
-      o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], lo, o[a], 0, 0, 0);
+    for (int n = 2; n >= 0; --n) {
+      const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]));
+#pragma unroll
+      for (int a = 0; a < CH; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], b, o[a], 0, 0, 0);
     }
   }
 };
@@ -166,15 +174,18 @@ struct Step<float, D> {
         for (int u = 0; u < CV; ++u) v.x[i][u] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   static __device__ __forceinline__ void scores(const K& k, const Q& q, float (&s)[NS]) {
-    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    // four chains: a sum of 128 products in one is off by twice as much
+    f32x4 a[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < KC; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[i][j], q.x[i][j], a, 0, 0, 0);
+      for (int j = 0; j < 4; ++j) a[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[i][j], q.x[i][j], a[j], 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = a[i];
+    for (int i = 0; i < 4; ++i) s[i] = (a[0][i] + a[1][i]) + (a[2][i] + a[3][i]);
   }
-  static __device__ __forceinline__ const Vt& transpose(const V& v) { return v; }
+  static __device__ __forceinline__ Vt transpose(const V& v) { return v; }
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -234,31 +245,46 @@ __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0
                                             int c) {
   typedef Step<T, D> S;
   const int last = end - 1;
-  for (; k0 < end; k0 += stride) {
-    const typename S::K k = S::load_k(K, k0, last, g, c);
-    typename S::V v = S::load_v(V, k0, last, g, c);
+  if (k0 >= end) return;
+  typename S::K k = S::load_k(K, k0, last, g, c);
+  typename S::V v = S::load_v(V, k0, last, g, c);
+  for (;;) {
+    const int next = k0 + stride;
     const bool ragged = k0 + S::KEYS > end;
-    if (ragged) S::mask_v(v, k0, last, g);
+    float s[MQ][S::NS];
+#pragma unroll
+    for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
+    // The next rows' loads go out as soon as the registers are free: a wave has loads in flight all the time.  They are made
+    // behind the end too (the last row again), since a wait behind a load that may not have been made waits for all of them.
+    k = S::load_k(K, next, last, g, c);
+    if (ragged) {
+      S::mask_v(v, k0, last, g);
+#pragma unroll
+      for (int t = 0; t < MQ; ++t)
+#pragma unroll
+        for (int i = 0; i < S::NS; ++i)
+          if (k0 + S::key(g, i) > last) s[t][i] = neg_inf();
+    }
+    if (MQ == 1 && z) {
+#pragma unroll
+      for (int i = 0; i < S::NS; i += 4)
+        *reinterpret_cast<f32x4*>(z + k0 + S::key(g, i)) = f32x4{s[0][i], s[0][i + 1], s[0][i + 2], s[0][i + 3]};
+    }
     const typename S::Vt vt = S::transpose(v);
+    v = S::load_v(V, next, last, g, c);
 #pragma unroll
     for (int t = 0; t < MQ; ++t) {
-      float s[S::NS];
-      S::scores(k, q[t], s);
-      if (ragged) {
-#pragma unroll
-        for (int i = 0; i < S::NS; ++i)
-          if (k0 + S::key(g, i) > last) s[i] = neg_inf();
-      }
-      if (MQ == 1 && z) {
-#pragma unroll
-        for (int i = 0; i < S::NS; ++i)
-          if (k0 + S::key(g, i) <= last) z[k0 + S::key(g, i)] = s[i];
-      }
-      st[t].weigh(s, scale);
-      S::accumulate(vt, s, st[t].o);
+      st[t].weigh(s[t], scale);
+      S::accumulate(vt, s[t], st[t].o);
     }
+    if (next >= end) return;
+    k0 = next;
   }
 }
+
+// What a partial result leaves of its softmax.  A sum that is no number may have no reference, where every score was none:
+// it has to survive the joining.
+__device__ __forceinline__ float2 partial_ml(float m, float l) { return make_float2(l == l ? m : -neg_inf(), l); }
 
 // The four waves' states of one tile of columns joined in LDS; columns below `cols` are left by all 256 threads as one
 // partial result each: (m, l) at ml[col], the sum at acc + col * D.
@@ -302,8 +328,7 @@ __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, Join
       tot += f * js.l[w][col];
     }
     acc[(size_t)col * D + ch] = sum;
-    // (a sum that is no number may have no reference, where every score was none: it has to survive the joining)
-    if (ch == 0) ml[col] = tot == tot ? make_float2(m, tot) : make_float2(-neg_inf(), tot);
+    if (ch == 0) ml[col] = partial_ml(m, tot);
   }
 }
 
@@ -377,7 +402,7 @@ struct AttendArgs {
 
 // Own rows: one workgroup per piece, all G heads of its unit as columns; the four waves take every fourth step.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void own_rows_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256, 2) void own_rows_kernel(const AttendArgs a) {
   typedef Step<T, D> S;
   __shared__ JoinShared js;
   __shared__ __attribute__((aligned(16))) float lds[4 * 16 * (D + 4)];
@@ -401,7 +426,7 @@ __global__ __launch_bounds__(256) void own_rows_kernel(const AttendArgs a) {
 
 // Prefix: one workgroup per (KV head, range of prefix rows, MQ tiles of the B * G query rows).
 template <typename T, int D, int MQ>
-__global__ __launch_bounds__(256) void prefix_rows_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256, MQ == 1 ? 2 : 1) void prefix_rows_kernel(const AttendArgs a) {
   typedef Step<T, D> S;
   __shared__ JoinShared js;
   __shared__ __attribute__((aligned(16))) float lds[4 * 16 * (D + 4)];
@@ -430,6 +455,143 @@ __global__ __launch_bounds__(256) void prefix_rows_kernel(const AttendArgs a) {
       join_waves<T, D>(st[t], min(16, M - first), js, lds, wave, g, c, a.pml + at, a.pacc + at * D);
     }
     __syncthreads();
+  }
+}
+
+// Prefix with more query rows than a tile (bf16): four waves with MQ tiles of columns each go through the same rows, which
+// they share in LDS.  While they work on a tile of 64 rows the next one is on its way there, straight from memory.  Chunk
+// x (16 bytes) of row r lies at x ^ f(r): the lanes of an operand read, which have one chunk of sixteen key rows, or two
+// neighbouring chunks of eight value rows, then hit all banks.  The values' operand comes transposed (ds_read_b64_tr_b16:
+// sixteen lanes read four rows of sixteen channels, and each gets the four values of its channel).
+template <int D>
+struct SharedTile {
+  static constexpr int ROWS = 64, ROW = D * 2, CHUNKS = ROW / 16, BYTES = ROWS * ROW;
+  static constexpr int FILLS = BYTES / 1024 / 4;  // wave-wide loads of each wave
+  static __device__ __forceinline__ int fk(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ int fv(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+  // rows r0 .. of src (the last one again behind the end) into lds; V: which of the two arrangements
+  template <bool V>
+  static __device__ __forceinline__ void fill(char* lds, const char* src, int r0, int last, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < FILLS; ++i) {
+      const int piece = wave * FILLS + i, r = piece * (1024 / ROW) + lane / CHUNKS;
+      const int x = lane % CHUNKS ^ (V ? fv(r) : fk(r));
+      const char* from = src + (size_t)min(r0 + r, last) * ROW + x * 16;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                       (__attribute__((address_space(3))) void*)(lds + piece * 1024), 16, 0, 0);
+    }
+  }
+};
+
+template <int D, int MQ>
+__global__ __launch_bounds__(256, 2) void prefix_shared_kernel(const AttendArgs a) {
+  typedef Step<bf16_t, D> S;
+  typedef SharedTile<D> L;
+  constexpr int BLOCKS = D / 16;  // of sixteen channels
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  __shared__ __attribute__((aligned(1024))) char lk0[L::BYTES], lk1[L::BYTES], lv0[L::BYTES], lv1[L::BYTES];
+  const int hs = blockIdx.x % (a.Hkv * a.splits), tile = blockIdx.x / (a.Hkv * a.splits);
+  const int h = hs % a.Hkv, split = hs / a.Hkv;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int M = a.B * a.G, m0 = (tile * 4 + wave) * MQ * 16;
+  typename S::Q q[MQ];
+  State<bf16_t, D> st[MQ];
+#pragma unroll
+  for (int t = 0; t < MQ; ++t) {
+    const int m = min(m0 + t * 16 + c, M - 1), b = m / a.G;
+    q[t] = S::load_q(a.q + ((size_t)b * a.Hq + h * a.G + (m - b * a.G)) * L::ROW, g);
+    st[t].init();
+  }
+  const int start = split * a.prefix_rows, end = min(a.P, start + a.prefix_rows), last = end - 1;
+  const char* K = a.prefix_k + (size_t)h * a.P * L::ROW;
+  const char* V = a.prefix_v + (size_t)h * a.P * L::ROW;
+  int ka[S::KC], va[BLOCKS];  // this lane's places in a tile, of row c and of row g * 4 + c / 4
+#pragma unroll
+  for (int x = 0; x < S::KC; ++x) ka[x] = c * L::ROW + ((x * 4 + g) ^ L::fk(c)) * 16;
+#pragma unroll
+  for (int x = 0; x < BLOCKS; ++x) {
+    const int r = g * 4 + (c >> 2);
+    va[x] = r * L::ROW + ((x * 2 + ((c & 3) >> 1)) ^ L::fv(r)) * 16 + (c & 1) * 8;
+  }
+  auto fill = [&](char* lk, char* lv, int r0) {
+    L::template fill<false>(lk, K, r0, last, wave, lane);
+    L::template fill<true>(lv, V, r0, last, wave, lane);
+  };
+  auto filled = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // this wave's loads into LDS (vmcnt 0)
+    __syncthreads();
+  };
+  auto work = [&](const char* lk, const char* lv, int r0) {
+#pragma unroll
+    for (int half = 0; half < L::ROWS; half += 32) {
+      const int k0 = r0 + half;
+      if (k0 >= end) break;
+      typename S::K k;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int x = 0; x < S::KC; ++x) k.x[t][x] = load16(lk + ka[x] + (half + t * 16) * L::ROW);
+      s16x4 v[BLOCKS][2];
+#pragma unroll
+      for (int x = 0; x < BLOCKS; ++x)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          v[x][t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(lv + va[x] + (half + t * 16) * L::ROW));
+      float s[MQ][S::NS];
+#pragma unroll
+      for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
+      if (k0 + 32 > end) {
+        // (rows behind the end are the last row again: their weight is zero, and zero times a number that is none must not
+        // show, so the values go too)
+#pragma unroll
+        for (int x = 0; x < BLOCKS; ++x)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (k0 + S::key(g, j) > last) v[x][j >> 2][j & 3] = 0;
+#pragma unroll
+        for (int t = 0; t < MQ; ++t)
+#pragma unroll
+          for (int i = 0; i < S::NS; ++i)
+            if (k0 + S::key(g, i) > last) s[t][i] = neg_inf();
+      }
+      typename S::Vt vt;
+#pragma unroll
+      for (int x = 0; x < BLOCKS; ++x) {
+        const uint2 lo = __builtin_bit_cast(uint2, v[x][0]), hi = __builtin_bit_cast(uint2, v[x][1]);
+        vt.x[x] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+      }
+#pragma unroll
+      for (int t = 0; t < MQ; ++t) {
+        st[t].weigh(s[t], a.scale);
+        S::accumulate(vt, s[t], st[t].o);
+      }
+    }
+  };
+  fill(lk0, lv0, start);
+  filled();
+  for (int r0 = start;; r0 += 2 * L::ROWS) {
+    if (r0 + L::ROWS < end) fill(lk1, lv1, r0 + L::ROWS);
+    work(lk0, lv0, r0);
+    if (r0 + L::ROWS >= end) break;
+    filled();
+    if (r0 + 2 * L::ROWS < end) fill(lk0, lv0, r0 + 2 * L::ROWS);
+    work(lk1, lv1, r0 + L::ROWS);
+    if (r0 + 2 * L::ROWS >= end) break;
+    filled();
+  }
+#pragma unroll
+  for (int t = 0; t < MQ; ++t) {
+    const int m = m0 + t * 16 + c;
+    float l = st[t].l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (m < M) {
+      const size_t at = ((size_t)split * a.Hkv + h) * M + m;
+      if (g == 0) a.pml[at] = partial_ml(st[t].m, l);
+#pragma unroll
+      for (int x = 0; x < BLOCKS; ++x) *reinterpret_cast<f32x4*>(a.pacc + at * D + x * 16 + g * 4) = st[t].o[x];
+    }
   }
 }
 
@@ -526,18 +688,15 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   }
 }
 
-template <typename T, int D, int MQ>
-void launch_prefix(const AttendArgs& a, int mtiles, hipStream_t st) {
-  WAVE_LAUNCH("prefix_rows", (prefix_rows_kernel<T, D, MQ>), a.Hkv * a.splits * mtiles, 256, 0, st, a);
-}
-
 template <typename T, int D>
 wave_status attend_td(const AttendArgs& a, const CacheAttendGeom& g, hipStream_t st) {
   if (a.P > 0) {
-    switch (g.mtile / 16) {
-      case 1: launch_prefix<T, D, 1>(a, g.mtiles, st); break;
-      case 2: launch_prefix<T, D, 2>(a, g.mtiles, st); break;
-      default: launch_prefix<T, D, 4>(a, g.mtiles, st); break;
+    const unsigned grid = a.Hkv * a.splits * g.mtiles;
+    if (g.mtile == 16) WAVE_LAUNCH("prefix_rows", (prefix_rows_kernel<T, D, 1>), grid, 256, 0, st, a);
+    if (g.mtile == 32) WAVE_LAUNCH("prefix_rows", (prefix_rows_kernel<T, D, 2>), grid, 256, 0, st, a);
+    if constexpr (sizeof(T) == 2) {
+      if (g.mtile == 64) WAVE_LAUNCH("prefix_shared", (prefix_shared_kernel<D, 1>), grid, 256, 0, st, a);
+      if (g.mtile == 128) WAVE_LAUNCH("prefix_shared", (prefix_shared_kernel<D, 2>), grid, 256, 0, st, a);
     }
   }
   WAVE_LAUNCH("own_rows", (own_rows_kernel<T, D>), a.Hkv * g.pieces, 256, 0, st, a);
@@ -552,20 +711,20 @@ wave_status attend_td(const AttendArgs& a, const CacheAttendGeom& g, hipStream_t
 CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool accumulate) {
   CacheAttendGeom g{};
   const int G = Hq / c.Hkv;
-  // Own rows: about three pieces a CU over all KV heads; every sequence may end in a piece that is not full.
-  g.target = 768 / c.Hkv > 1 ? 768 / c.Hkv : 1;
+  // Own rows: about six pieces a CU over all KV heads; every sequence may end in a piece that is not full.
+  g.target = 1536 / c.Hkv > 1 ? 1536 / c.Hkv : 1;
   const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
   g.pieces = (int)((long long)g.target + c.B < most ? g.target + c.B : most);
   const int M = c.B * G;
-  g.mtile = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+  g.mtile = M <= 16 ? 16 : c.dtype == WAVE_F32 ? 32 : M <= 64 ? 64 : 128;
   g.mtiles = (M + g.mtile - 1) / g.mtile;
   if (P > 0) {
-    const int want = 768 / (c.Hkv * g.mtiles) > 1 ? 768 / (c.Hkv * g.mtiles) : 1;
+    const int want = 512 / (c.Hkv * g.mtiles) > 1 ? 512 / (c.Hkv * g.mtiles) : 1;
     const long long rows = ((long long)P + want - 1) / want;
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);
   }
-  g.zrow = (c.capacity + 15) / 16 * 16;
+  g.zrow = (c.capacity + 31) / 32 * 32;  // whole steps
   size_t o = 0;
   g.off_z = o;     o = align_up(o + (accumulate ? sizeof(float) * (size_t)c.B * Hq * g.zrow : 0));
   g.off_ml = o;    o = align_up(o + sizeof(float) * 2 * (size_t)Hq * g.pieces);
