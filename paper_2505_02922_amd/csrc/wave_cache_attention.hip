@@ -4,6 +4,8 @@
 // through key and value rows with a running maximum and sum of the softmax.  Keys enter S = K Q^T straight from
 // memory in the operand's layout, and what a lane holds of S is, with the contraction index permuted alike on both
 // sides, already the operand of O^T += V^T P^T: no value crosses a lane between the two products.
+#include <type_traits>
+
 #include "wave_common.h"
 
 namespace wave {
@@ -107,27 +109,36 @@ struct Step<bf16_t, D> {
     }
     return r;
   }
-  // A weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the product with
-  // the values loses nothing.  (Two numbers, each the nearest, hold 16 bits; outputs are then off by 2e-6 of their norm,
-  // twice what the fp32 sums cost.)
+  // TERMS 3: a weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the
+  // product with the values loses nothing.  TERMS 2: the nearest bf16 number and the nearest to what that left, 17 bits:
+  // outputs are then off by 2e-6 of their norm.
+  template <int TERMS>
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
-    uint32_t w[3][4];
+    bf16x8 w[TERMS];
+    if constexpr (TERMS == 3) {
+      uint32_t u[3][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float x = p[2 * j], y = p[2 * j + 1];
+      for (int j = 0; j < 4; ++j) {
+        float x = p[2 * j], y = p[2 * j + 1];
 #pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        w[n][j] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
-        x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-        y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+        for (int n = 0; n < 3; ++n) {
+          u[n][j] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+          x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+          y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+        }
       }
+#pragma unroll
+      for (int n = 0; n < 3; ++n) w[n] = __builtin_bit_cast(bf16x8, make_uint4(u[n][0], u[n][1], u[n][2], u[n][3]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[0][j] = (__bf16)p[j];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[1][j] = (__bf16)(p[j] - (float)w[0][j]);
     }
 #pragma unroll
-    for (int n = 2; n >= 0; --n) {
-      const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]));
+    for (int n = TERMS - 1; n >= 0; --n)
 #pragma unroll
-      for (int a = 0; a < CH; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], b, o[a], 0, 0, 0);
-    }
+      for (int a = 0; a < CH; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], w[n], o[a], 0, 0, 0);
   }
 };
 
@@ -186,6 +197,7 @@ struct Step<float, D> {
     for (int i = 0; i < 4; ++i) s[i] = (a[0][i] + a[1][i]) + (a[2][i] + a[3][i]);
   }
   static __device__ __forceinline__ Vt transpose(const V& v) { return v; }
+  template <int>
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -209,9 +221,8 @@ struct State {
 #pragma unroll
     for (int a = 0; a < S::ACC; ++a) o[a] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // s: products q . k; becomes the weights exp(s / sqrt(d)) over the reference.  scale: log2(e) / sqrt(d), applied inside
-  // the difference, which is then rounded once.
-  __device__ __forceinline__ void weigh(float (&s)[S::NS], float scale) {
+  // The reference follows the products s = q . k.  scale: log2(e) / sqrt(d).
+  __device__ __forceinline__ void follow(const float (&s)[S::NS], float scale) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < S::NS; ++i) top = fmaxf(top, s[i]);
@@ -226,23 +237,29 @@ struct State {
 #pragma unroll
       for (int a = 0; a < S::ACC; ++a) o[a] *= f;
     }
+  }
+  // p: the weights exp(s / sqrt(d)) over the reference.  The scale is applied inside the difference, which is then rounded
+  // once.
+  __device__ __forceinline__ void weights(const float (&s)[S::NS], float (&p)[S::NS], float scale) {
     const float ref = m == neg_inf() ? 0.f : m;  // (every score -infinity so far)
 #pragma unroll
-    for (int i = 0; i < S::NS; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
-      l += s[i];
-    }
+    for (int i = 0; i < S::NS; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
+#pragma unroll
+    for (int i = 0; i < S::NS; ++i) l += p[i];
+  }
+  __device__ __forceinline__ void weigh(float (&s)[S::NS], float scale) {
+    follow(s, scale);
+    weights(s, s, scale);
   }
 };
 
 // ----------------------------------------------------------------------------
-// The stream of one wave: the rows k0, k0 + stride, .. below `end` against MQ tiles of query columns.  z: where a lane
-// leaves the scores of its column (NULL: nowhere).
+// The stream of one wave: the rows k0, k0 + stride, .. below `end` against a tile of query columns.  z: where a lane leaves
+// the products of its column (NULL: nowhere).
 // ----------------------------------------------------------------------------
-template <typename T, int D, int MQ>
+template <typename T, int D>
 __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0, int stride, int end, float scale,
-                                            const typename Step<T, D>::Q (&q)[MQ], State<T, D> (&st)[MQ], float* z, int g,
-                                            int c) {
+                                            const typename Step<T, D>::Q& q, State<T, D>& st, float* z, int g, int c) {
   typedef Step<T, D> S;
   const int last = end - 1;
   if (k0 >= end) return;
@@ -251,32 +268,26 @@ __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0
   for (;;) {
     const int next = k0 + stride;
     const bool ragged = k0 + S::KEYS > end;
-    float s[MQ][S::NS];
-#pragma unroll
-    for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
+    float s[S::NS];
+    S::scores(k, q, s);
     // The next rows' loads go out as soon as the registers are free: a wave has loads in flight all the time.  They are made
     // behind the end too (the last row again), since a wait behind a load that may not have been made waits for all of them.
     k = S::load_k(K, next, last, g, c);
     if (ragged) {
       S::mask_v(v, k0, last, g);
 #pragma unroll
-      for (int t = 0; t < MQ; ++t)
-#pragma unroll
-        for (int i = 0; i < S::NS; ++i)
-          if (k0 + S::key(g, i) > last) s[t][i] = neg_inf();
+      for (int i = 0; i < S::NS; ++i)
+        if (k0 + S::key(g, i) > last) s[i] = neg_inf();
     }
-    if (MQ == 1 && z) {
+    if (z) {
 #pragma unroll
       for (int i = 0; i < S::NS; i += 4)
-        *reinterpret_cast<f32x4*>(z + k0 + S::key(g, i)) = f32x4{s[0][i], s[0][i + 1], s[0][i + 2], s[0][i + 3]};
+        *reinterpret_cast<f32x4*>(z + k0 + S::key(g, i)) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
     }
     const typename S::Vt vt = S::transpose(v);
     v = S::load_v(V, next, last, g, c);
-#pragma unroll
-    for (int t = 0; t < MQ; ++t) {
-      st[t].weigh(s[t], scale);
-      S::accumulate(vt, s[t], st[t].o);
-    }
+    st.weigh(s, scale);
+    S::template accumulate<3>(vt, s, st.o);
     if (next >= end) return;
     k0 = next;
   }
@@ -288,14 +299,14 @@ __device__ __forceinline__ float2 partial_ml(float m, float l) { return make_flo
 
 // The four waves' states of one tile of columns joined in LDS; columns below `cols` are left by all 256 threads as one
 // partial result each: (m, l) at ml[col], the sum at acc + col * D.
-struct __attribute__((aligned(16))) JoinShared {
+struct JoinShared {
   float m[4][16], l[4][16];
 };
 template <typename T, int D>
-__device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, JoinShared& js, float* lds, int wave, int g, int c,
-                                           float2* ml, float* acc) {
+__device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, JoinShared& js, char* const (&areas)[4], int wave,
+                                           int g, int c, float2* ml, float* acc) {
   typedef Step<T, D> S;
-  constexpr int PITCH = D + 4;  // floats a column: lanes of a column's four groups and of neighbouring columns on other banks
+  constexpr int PITCH = D + 4;  // floats a column: a column's four groups and neighbouring columns lie on other banks
   float l = st.l;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
@@ -304,7 +315,8 @@ __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, Join
     js.l[wave][c] = l;
   }
   if (c < cols) {
-    float* at = lds + ((size_t)wave * 16 + c) * PITCH;
+    char* area = wave == 0 ? areas[0] : wave == 1 ? areas[1] : wave == 2 ? areas[2] : areas[3];
+    float* at = reinterpret_cast<float*>(area) + c * PITCH;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -324,7 +336,7 @@ __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, Join
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float f = js.m[w][col] == neg_inf() ? 0.f : exp2f(js.m[w][col] - m);
-      sum += f * lds[((size_t)w * 16 + col) * PITCH + ch];
+      sum += f * reinterpret_cast<const float*>(areas[w])[col * PITCH + ch];
       tot += f * js.l[w][col];
     }
     acc[(size_t)col * D + ch] = sum;
@@ -377,17 +389,6 @@ __device__ __forceinline__ Pieces find_piece(const int32_t* lengths, int B, int 
   }
   return p;
 }
-// The first piece of sequence b.
-__device__ __forceinline__ int first_piece(const int32_t* lengths, int b, int capacity, int rows) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const int len = b0 + lane < b ? cache_length(lengths, b0 + lane, capacity) : 0;
-    before += wave_sum_i((len + rows - 1) / rows);
-  }
-  return before;
-}
-
 struct AttendArgs {
   const char *q, *k, *v, *prefix_k, *prefix_v;
   const int32_t* lengths;
@@ -395,102 +396,92 @@ struct AttendArgs {
   float *weights_out, *out, *lse;
   float *z, *acc, *pacc;   // products q . k [B * Hq][zrow]; sums of the own pieces [Hkv][pieces][G][D], of the prefix [splits][B * Hq][D]
   float2 *ml, *pml;        // their references and normalisers
+  int2* info;              // [B] the first piece of a sequence and the rows of a piece, for the joining
   int B, Hq, Hkv, G, capacity, P;
   int target, pieces, prefix_rows, splits, zrow;
+  int prefix_blocks, own_blocks, turn, prefix_turns;
   float scale, decay;
 };
 
 // Own rows: one workgroup per piece, all G heads of its unit as columns; the four waves take every fourth step.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void own_rows_kernel(const AttendArgs a) {
+__device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinShared& js, char* const (&areas)[4]) {
   typedef Step<T, D> S;
-  __shared__ JoinShared js;
-  __shared__ __attribute__((aligned(16))) float lds[4 * 16 * (D + 4)];
-  const int w = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv;
+  const int w = block / a.Hkv, h = block % a.Hkv;
   const Pieces p = find_piece(a.lengths, a.B, a.capacity, a.target, w);
   if (p.b == a.B) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int start = (w - p.first) * p.rows, end = min(p.length, start + p.rows);
+  if (start == 0 && h == 0 && threadIdx.x == 0) a.info[p.b] = make_int2(w, p.rows);
   const size_t unit = (size_t)p.b * a.Hkv + h, row = D * sizeof(T);
   const int head = h * a.G + min(c, a.G - 1);  // (columns behind the G heads repeat the last one)
   const size_t bh = (size_t)p.b * a.Hq + head;
-  typename S::Q q[1] = {S::load_q(a.q + bh * row, g)};
-  State<T, D> st[1];
-  st[0].init();
+  const typename S::Q q = S::load_q(a.q + bh * row, g);
+  State<T, D> st;
+  st.init();
   float* z = a.weights_out && c < a.G ? a.z + bh * a.zrow : nullptr;
-  stream_rows<T, D, 1>(a.k + unit * a.capacity * row, a.v + unit * a.capacity * row, start + wave * S::KEYS, 4 * S::KEYS, end,
-                       a.scale, q, st, z, g, c);
+  stream_rows<T, D>(a.k + unit * a.capacity * row, a.v + unit * a.capacity * row, start + wave * S::KEYS, 4 * S::KEYS, end,
+                    a.scale, q, st, z, g, c);
   const size_t at = ((size_t)h * a.pieces + w) * a.G;
-  join_waves<T, D>(st[0], a.G, js, lds, wave, g, c, a.ml + at, a.acc + at * D);
+  join_waves<T, D>(st, a.G, js, areas, wave, g, c, a.ml + at, a.acc + at * D);
 }
 
-// Prefix: one workgroup per (KV head, range of prefix rows, MQ tiles of the B * G query rows).
-template <typename T, int D, int MQ>
-__global__ __launch_bounds__(256, MQ == 1 ? 2 : 1) void prefix_rows_kernel(const AttendArgs a) {
+// Prefix, straight from memory: one workgroup per (KV head, range of prefix rows, tile of 16 of the B * G query rows).
+template <typename T, int D>
+__device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, JoinShared& js, char* const (&areas)[4]) {
   typedef Step<T, D> S;
-  __shared__ JoinShared js;
-  __shared__ __attribute__((aligned(16))) float lds[4 * 16 * (D + 4)];
-  const int hs = blockIdx.x % (a.Hkv * a.splits), tile = blockIdx.x / (a.Hkv * a.splits);
+  const int hs = block % (a.Hkv * a.splits), tile = block / (a.Hkv * a.splits);
   const int h = hs % a.Hkv, split = hs / a.Hkv;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-  const int M = a.B * a.G, m0 = tile * MQ * 16;
+  const int M = a.B * a.G, m0 = tile * 16;
   const size_t row = D * sizeof(T);
-  typename S::Q q[MQ];
-  State<T, D> st[MQ];
-#pragma unroll
-  for (int t = 0; t < MQ; ++t) {
-    const int m = min(m0 + t * 16 + c, M - 1), b = m / a.G;
-    q[t] = S::load_q(a.q + ((size_t)b * a.Hq + h * a.G + (m - b * a.G)) * row, g);
-    st[t].init();
-  }
+  const int m = min(m0 + c, M - 1), b = m / a.G;
+  const typename S::Q q = S::load_q(a.q + ((size_t)b * a.Hq + h * a.G + (m - b * a.G)) * row, g);
+  State<T, D> st;
+  st.init();
   const int start = split * a.prefix_rows, end = min(a.P, start + a.prefix_rows);
-  stream_rows<T, D, MQ>(a.prefix_k + (size_t)h * a.P * row, a.prefix_v + (size_t)h * a.P * row, start + wave * S::KEYS,
-                        4 * S::KEYS, end, a.scale, q, st, nullptr, g, c);
-#pragma unroll
-  for (int t = 0; t < MQ; ++t) {
-    const int first = m0 + t * 16;
-    if (first < M) {
-      // partial results by KV head and query row
-      const size_t at = ((size_t)split * a.Hkv + h) * M + first;
-      join_waves<T, D>(st[t], min(16, M - first), js, lds, wave, g, c, a.pml + at, a.pacc + at * D);
-    }
-    __syncthreads();
-  }
+  stream_rows<T, D>(a.prefix_k + (size_t)h * a.P * row, a.prefix_v + (size_t)h * a.P * row, start + wave * S::KEYS,
+                    4 * S::KEYS, end, a.scale, q, st, nullptr, g, c);
+  const size_t at = ((size_t)split * a.Hkv + h) * M + m0;  // by KV head and query row
+  join_waves<T, D>(st, min(16, M - m0), js, areas, wave, g, c, a.pml + at, a.pacc + at * D);
 }
 
 // Prefix with more query rows than a tile (bf16): four waves with MQ tiles of columns each go through the same rows, which
-// they share in LDS.  While they work on a tile of 64 rows the next one is on its way there, straight from memory.  Chunk
-// x (16 bytes) of row r lies at x ^ f(r): the lanes of an operand read, which have one chunk of sixteen key rows, or two
-// neighbouring chunks of eight value rows, then hit all banks.  The values' operand comes transposed (ds_read_b64_tr_b16:
-// sixteen lanes read four rows of sixteen channels, and each gets the four values of its channel).
+// they share in LDS.  A step is 32 rows; a ring of four steps holds the one that is worked on and the next, while two more
+// are on their way, straight from memory.  Chunk x (16 bytes) of row r lies at x ^ f(r): the lanes of an operand read,
+// which have one chunk of sixteen key rows, or two neighbouring chunks of eight value rows, then hit all banks.  The
+// values' operand comes transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen channels, and each gets
+// the four values of its channel).
+// Matrix and vector work are about equal here (48 + 16 products of 16 cycles, about 190 vector instructions of 4 and 32
+// exponentials of 16 for 32 columns), and a wave that does one after the other leaves each unit idle half of the time, the
+// two waves of a SIMD in step with each other.  So the scores of the next step are formed beside the softmax of this one.
 template <int D>
-struct SharedTile {
-  static constexpr int ROWS = 64, ROW = D * 2, CHUNKS = ROW / 16, BYTES = ROWS * ROW;
-  static constexpr int FILLS = BYTES / 1024 / 4;  // wave-wide loads of each wave
+struct SharedStep {
+  static constexpr int ROWS = 32, ROW = D * 2, CHUNKS = ROW / 16, HALF = ROWS * ROW, BYTES = 2 * HALF;  // keys, then values
+  static constexpr int FILLS = HALF / 1024 / 4;  // wave-wide loads of each wave, for each of the two
   static __device__ __forceinline__ int fk(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
   static __device__ __forceinline__ int fv(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
-  // rows r0 .. of src (the last one again behind the end) into lds; V: which of the two arrangements
-  template <bool V>
-  static __device__ __forceinline__ void fill(char* lds, const char* src, int r0, int last, int wave, int lane) {
+  // rows r0 .. of K and V (the last one again behind the end)
+  static __device__ __forceinline__ void fill(char* lds, const char* K, const char* V, int r0, int last, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < FILLS; ++i) {
-      const int piece = wave * FILLS + i, r = piece * (1024 / ROW) + lane / CHUNKS;
-      const int x = lane % CHUNKS ^ (V ? fv(r) : fk(r));
-      const char* from = src + (size_t)min(r0 + r, last) * ROW + x * 16;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+      const int piece = wave * FILLS + i, r = piece * (1024 / ROW) + lane / CHUNKS, x = lane % CHUNKS;
+      const size_t row = (size_t)min(r0 + r, last) * ROW;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(K + row + (x ^ fk(r)) * 16),
                                        (__attribute__((address_space(3))) void*)(lds + piece * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(V + row + (x ^ fv(r)) * 16),
+                                       (__attribute__((address_space(3))) void*)(lds + HALF + piece * 1024), 16, 0, 0);
     }
   }
 };
 
-template <int D, int MQ>
-__global__ __launch_bounds__(256, 2) void prefix_shared_kernel(const AttendArgs a) {
+template <int D, int MQ, int TERMS>
+__device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, char* ring0, char* ring1, char* ring2, char* ring3) {
   typedef Step<bf16_t, D> S;
-  typedef SharedTile<D> L;
+  typedef SharedStep<D> L;
   constexpr int BLOCKS = D / 16;  // of sixteen channels
   typedef short s16x4 __attribute__((ext_vector_type(4)));
-  __shared__ __attribute__((aligned(1024))) char lk0[L::BYTES], lk1[L::BYTES], lv0[L::BYTES], lv1[L::BYTES];
-  const int hs = blockIdx.x % (a.Hkv * a.splits), tile = blockIdx.x / (a.Hkv * a.splits);
+  const int hs = block % (a.Hkv * a.splits), tile = block / (a.Hkv * a.splits);
   const int h = hs % a.Hkv, split = hs / a.Hkv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int M = a.B * a.G, m0 = (tile * 4 + wave) * MQ * 16;
@@ -505,81 +496,101 @@ __global__ __launch_bounds__(256, 2) void prefix_shared_kernel(const AttendArgs 
   const int start = split * a.prefix_rows, end = min(a.P, start + a.prefix_rows), last = end - 1;
   const char* K = a.prefix_k + (size_t)h * a.P * L::ROW;
   const char* V = a.prefix_v + (size_t)h * a.P * L::ROW;
-  int ka[S::KC], va[BLOCKS];  // this lane's places in a tile, of row c and of row g * 4 + c / 4
+  int ka[S::KC], va[BLOCKS];  // this lane's places in a step, of row c and of row g * 4 + c / 4
 #pragma unroll
   for (int x = 0; x < S::KC; ++x) ka[x] = c * L::ROW + ((x * 4 + g) ^ L::fk(c)) * 16;
 #pragma unroll
   for (int x = 0; x < BLOCKS; ++x) {
     const int r = g * 4 + (c >> 2);
-    va[x] = r * L::ROW + ((x * 2 + ((c & 3) >> 1)) ^ L::fv(r)) * 16 + (c & 1) * 8;
+    va[x] = L::HALF + r * L::ROW + ((x * 2 + ((c & 3) >> 1)) ^ L::fv(r)) * 16 + (c & 1) * 8;
   }
-  auto fill = [&](char* lk, char* lv, int r0) {
-    L::template fill<false>(lk, K, r0, last, wave, lane);
-    L::template fill<true>(lv, V, r0, last, wave, lane);
-  };
-  auto filled = [&]() {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // this wave's loads into LDS (vmcnt 0)
-    __syncthreads();
-  };
-  auto work = [&](const char* lk, const char* lv, int r0) {
+  auto read_k = [&](const char* lds) {
+    typename S::K k;
 #pragma unroll
-    for (int half = 0; half < L::ROWS; half += 32) {
-      const int k0 = r0 + half;
-      if (k0 >= end) break;
-      typename S::K k;
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int x = 0; x < S::KC; ++x) k.x[t][x] = load16(lds + ka[x] + t * 16 * L::ROW);
+    return k;
+  };
+  auto read_v = [&](const char* lds) {
+    typename S::Vt v;
+#pragma unroll
+    for (int x = 0; x < BLOCKS; ++x) {
+      uint2 u[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int x = 0; x < S::KC; ++x) k.x[t][x] = load16(lk + ka[x] + (half + t * 16) * L::ROW);
-      s16x4 v[BLOCKS][2];
-#pragma unroll
-      for (int x = 0; x < BLOCKS; ++x)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          v[x][t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(lv + va[x] + (half + t * 16) * L::ROW));
-      float s[MQ][S::NS];
-#pragma unroll
-      for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
-      if (k0 + 32 > end) {
-        // (rows behind the end are the last row again: their weight is zero, and zero times a number that is none must not
-        // show, so the values go too)
-#pragma unroll
-        for (int x = 0; x < BLOCKS; ++x)
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (k0 + S::key(g, j) > last) v[x][j >> 2][j & 3] = 0;
-#pragma unroll
-        for (int t = 0; t < MQ; ++t)
-#pragma unroll
-          for (int i = 0; i < S::NS; ++i)
-            if (k0 + S::key(g, i) > last) s[t][i] = neg_inf();
-      }
-      typename S::Vt vt;
-#pragma unroll
-      for (int x = 0; x < BLOCKS; ++x) {
-        const uint2 lo = __builtin_bit_cast(uint2, v[x][0]), hi = __builtin_bit_cast(uint2, v[x][1]);
-        vt.x[x] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-      }
-#pragma unroll
-      for (int t = 0; t < MQ; ++t) {
-        st[t].weigh(s[t], a.scale);
-        S::accumulate(vt, s[t], st[t].o);
-      }
+        u[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((
+                                             __attribute__((address_space(3))) s16x4*)(lds + va[x] + t * 16 * L::ROW)));
+      v.x[x] = __builtin_bit_cast(bf16x8, make_uint4(u[0].x, u[0].y, u[1].x, u[1].y));
     }
+    return v;
   };
-  fill(lk0, lv0, start);
-  filled();
-  for (int r0 = start;; r0 += 2 * L::ROWS) {
-    if (r0 + L::ROWS < end) fill(lk1, lv1, r0 + L::ROWS);
-    work(lk0, lv0, r0);
-    if (r0 + L::ROWS >= end) break;
-    filled();
-    if (r0 + 2 * L::ROWS < end) fill(lk0, lv0, r0 + 2 * L::ROWS);
-    work(lk1, lv1, r0 + L::ROWS);
-    if (r0 + 2 * L::ROWS >= end) break;
-    filled();
+  // `newest` steps' loads of this wave may be on their way still; then all waves are behind the step before
+  auto arrive = [&](auto newest) {
+    constexpr int N = decltype(newest)::value * 2 * L::FILLS;
+    __builtin_amdgcn_s_waitcnt(0x0f70 | N);
+    __syncthreads();
+  };
+  L::fill(ring0, K, V, start, last, wave, lane);
+  L::fill(ring1, K, V, start + 32, last, wave, lane);
+  L::fill(ring2, K, V, start + 64, last, wave, lane);
+  arrive(std::integral_constant<int, 2>());
+  float s[MQ][S::NS];
+  {
+    const typename S::K k = read_k(ring0);
+#pragma unroll
+    for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
   }
+  const int full = (end - start) / 32;
+  const bool idle = m0 >= M;  // (a wave of the last tile may have no column at all: it only fetches)
+  // step n: `now` holds it, `next` the step behind it, `free` the step before it
+  auto step = [&](int n, const char* now, const char* next, char* free) {
+    arrive(std::integral_constant<int, 1>());
+    L::fill(free, K, V, start + (n + 3) * 32, last, wave, lane);
+    if (idle) return;
+#pragma unroll
+    for (int t = 0; t < MQ; ++t) st[t].follow(s[t], a.scale);
+    const typename S::K k = read_k(next);
+    const typename S::Vt v = read_v(now);
+    float p[MQ][S::NS];
+    st[0].weights(s[0], p[0], a.scale);
+    if (MQ > 1) st[MQ - 1].weights(s[MQ - 1], p[MQ - 1], a.scale);
+#pragma unroll
+    for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
+#pragma unroll
+    for (int t = 0; t < MQ; ++t) S::template accumulate<TERMS>(v, p[t], st[t].o);
+  };
+  for (int n = 0;; n += 4) {
+    if (n >= full) break;
+    step(n, ring0, ring1, ring3);
+    if (n + 1 >= full) break;
+    step(n + 1, ring1, ring2, ring0);
+    if (n + 2 >= full) break;
+    step(n + 2, ring2, ring3, ring1);
+    if (n + 3 >= full) break;
+    step(n + 3, ring3, ring0, ring2);
+  }
+  if (start + full * 32 < end) {
+    // Rows behind the end are the last row again.  Their weight is zero, and zero times a value that is no number must not
+    // show, so the values go too.
+    const int k0 = start + full * 32;
+    const char* now = (full & 3) == 0 ? ring0 : (full & 3) == 1 ? ring1 : (full & 3) == 2 ? ring2 : ring3;
+    typename S::Vt v = read_v(now);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (k0 + S::key(g, j) > last) {
+#pragma unroll
+        for (int x = 0; x < BLOCKS; ++x) v.x[x][j] = (__bf16)0.f;
+#pragma unroll
+        for (int t = 0; t < MQ; ++t) s[t][j] = neg_inf();
+      }
+#pragma unroll
+    for (int t = 0; t < MQ; ++t) {
+      st[t].weigh(s[t], a.scale);
+      S::template accumulate<TERMS>(v, s[t], st[t].o);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // no load may write LDS behind the end of the workgroup
 #pragma unroll
   for (int t = 0; t < MQ; ++t) {
     const int m = m0 + t * 16 + c;
@@ -592,6 +603,56 @@ __global__ __launch_bounds__(256, 2) void prefix_shared_kernel(const AttendArgs 
 #pragma unroll
       for (int x = 0; x < BLOCKS; ++x) *reinterpret_cast<f32x4*>(a.pacc + at * D + x * 16 + g * 4) = st[t].o[x];
     }
+  }
+}
+
+// ----------------------------------------------------------------------------
+// Prefix and own rows in one launch: one is bound by the matrix units as soon as it has many query rows, the other by
+// memory.  256 workgroups of the one (all, if there are fewer) and as many of the other alternate, so that a CU has one of
+// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows: 174 us; in launches of their own
+// 117 + 71 us, all of the prefix first 180 us, mixed in proportion, which leaves single prefix workgroups for the end, 206.)
+// Tiles of one prefix range are a multiple of 8 workgroups apart, on one XCD, wherever Hkv * splits is one.
+// ----------------------------------------------------------------------------
+struct Role {
+  int block;
+  bool prefix, any;
+};
+__device__ __forceinline__ Role role_of(const AttendArgs& a) {
+  const int group = blockIdx.x / a.turn, within = blockIdx.x % a.turn;
+  Role r;
+  r.prefix = !(group & 1) && (group >> 1) < a.prefix_turns;
+  const int before = min((group + 1) >> 1, a.prefix_turns);
+  r.block = (r.prefix ? group >> 1 : group - before) * a.turn + within;
+  r.any = r.block < (r.prefix ? a.prefix_blocks : a.own_blocks);
+  return r;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a) {
+  __shared__ JoinShared js;
+  __shared__ __attribute__((aligned(16))) char lds[4][16 * (D + 4) * 4];
+  char* const areas[4] = {lds[0], lds[1], lds[2], lds[3]};
+  const Role r = role_of(a);
+  if (!r.any) return;
+  if (r.prefix)
+    prefix_rows<T, D>(a, r.block, js, areas);
+  else
+    own_rows<T, D>(a, r.block, js, areas);
+}
+
+template <int D, int MQ, int TERMS>
+__global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs a) {
+  typedef SharedStep<D> L;
+  constexpr int AREA = L::BYTES > 16 * (D + 4) * 4 ? L::BYTES : 16 * (D + 4) * 4;
+  __shared__ JoinShared js;
+  __shared__ __attribute__((aligned(1024))) char ring0[AREA], ring1[AREA], ring2[AREA], ring3[AREA];
+  const Role r = role_of(a);
+  if (!r.any) return;
+  if (r.prefix) {
+    prefix_shared<D, MQ, TERMS>(a, r.block, ring0, ring1, ring2, ring3);
+  } else {
+    char* const areas[4] = {ring0, ring1, ring2, ring3};
+    own_rows<bf16_t, D>(a, r.block, js, areas);
   }
 }
 
@@ -629,32 +690,41 @@ __device__ __forceinline__ float2 normaliser(const HeadParts& p) {
   }
   const float top = wave_max(m);
   l = m == neg_inf() ? 0.f : l * exp2f(m - top);
-  return make_float2(top, wave_sum_f(l));
+  return make_float2(top, wave_add_f(l));
 }
 
-constexpr int WEIGHT_ROWS = 1024;
+// rows of a unit per workgroup, by the registers that the heads' products take
+constexpr int weight_rows(int G) { return G <= 4 ? 2048 : 1024; }
 
-template <int D>
+// The sequence's pieces as the launch before left them: the first one, and how many
+struct OwnPieces {
+  int first, count;
+};
+__device__ __forceinline__ OwnPieces own_pieces(const AttendArgs& a, int b, int length) {
+  const int2 p = length > 0 ? a.info[b] : make_int2(0, 1);
+  return OwnPieces{p.x, (length + p.y - 1) / p.y};
+}
+
+template <int D, int G>
 __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
+  constexpr int WEIGHT_ROWS = weight_rows(G);
   const int heads = a.B * a.Hq, tid = threadIdx.x, wave = tid >> 6;
-  const int rows = piece_rows(a.lengths, a.B, a.capacity, a.target);
-  __shared__ float2 norm[8];
+  __shared__ float2 norm[G];
   if ((int)blockIdx.x < heads) {
     __shared__ float part[256 / (D / 4)][D];
-    const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / a.G, gq = hq % a.G;
-    const int len = cache_length(a.lengths, b, a.capacity), own = (len + rows - 1) / rows;
-    const int first = first_piece(a.lengths, b, a.capacity, rows);
-    const HeadParts p = head_parts(a, b, h, gq, first, own);
+    const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / G, gq = hq % G;
+    const OwnPieces own = own_pieces(a, b, cache_length(a.lengths, b, a.capacity));
+    const HeadParts p = head_parts(a, b, h, gq, own.first, own.count);
     const float2 n = normaliser(p);
     constexpr int LANES = D / 4, GROUPS = 256 / LANES;
     const int lane = tid % LANES, group = tid / LANES;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int i = group; i < p.splits + own; i += GROUPS) {
+    for (int i = group; i < p.splits + own.count; i += GROUPS) {
       const float2 x = p.at(i);
       const float f = x.x == neg_inf() ? 0.f : exp2f(x.x - n.x);
       const float* acc = i < p.splits
-                             ? a.pacc + ((size_t)i * p.pstride + (size_t)h * a.B * a.G + (size_t)b * a.G + gq) * D
-                             : a.acc + (((size_t)h * a.pieces + first + i - p.splits) * a.G + gq) * D;
+                             ? a.pacc + ((size_t)i * p.pstride + (size_t)h * a.B * G + (size_t)b * G + gq) * D
+                             : a.acc + (((size_t)h * a.pieces + own.first + i - p.splits) * G + gq) * D;
       sum += f * *reinterpret_cast<const f32x4*>(acc + lane * 4);
     }
     *reinterpret_cast<f32x4*>(&part[group][lane * 4]) = sum;
@@ -673,36 +743,73 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   const int b = unit / a.Hkv, h = unit % a.Hkv;
   const int len = cache_length(a.lengths, b, a.capacity);
   if (r0 >= len) return;
-  const int own = (len + rows - 1) / rows, first = first_piece(a.lengths, b, a.capacity, rows);
-  for (int gq = wave; gq < a.G; gq += 4) {
-    const float2 n = normaliser(head_parts(a, b, h, gq, first, own));
+  // the products and the old weights are on their way while the normalisers are formed
+  constexpr int PER = WEIGHT_ROWS / 256;
+  const size_t base = (size_t)unit * a.capacity;
+  const float* z = a.z + ((size_t)b * a.Hq + h * G) * a.zrow;
+  float zz[G][PER], w[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = min(r0 + i * 256 + tid, len - 1);
+#pragma unroll
+    for (int gq = 0; gq < G; ++gq) zz[gq][i] = z[(size_t)gq * a.zrow + j];
+    w[i] = a.decay > 0.f ? a.decay * a.weights[base + j] : 0.f;
+  }
+  const OwnPieces own = own_pieces(a, b, len);
+  for (int gq = wave; gq < G; gq += 4) {
+    const float2 n = normaliser(head_parts(a, b, h, gq, own.first, own.count));
     if ((tid & 63) == 0) norm[gq] = make_float2(n.x == neg_inf() ? 0.f : n.x, n.x == neg_inf() ? 1.f : 1.f / n.y);
   }
   __syncthreads();
-  const size_t base = (size_t)unit * a.capacity;
-  const float* z = a.z + ((size_t)b * a.Hq + h * a.G) * a.zrow;
-  for (int j = r0 + tid; j < min(len, r0 + WEIGHT_ROWS); j += 256) {
-    float w = 0.f;
-    for (int gq = 0; gq < a.G; ++gq) w += __builtin_amdgcn_exp2f(fmaf(z[(size_t)gq * a.zrow + j], a.scale, -norm[gq].x)) * norm[gq].y;
-    a.weights_out[base + j] = a.decay > 0.f ? a.decay * a.weights[base + j] + w : w;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = r0 + i * 256 + tid;
+#pragma unroll
+    for (int gq = 0; gq < G; ++gq)
+      w[i] += __builtin_amdgcn_exp2f(fmaf(zz[gq][i], a.scale, -norm[gq].x)) * norm[gq].y;
+    if (j < len) a.weights_out[base + j] = w[i];
   }
 }
 
+// From this many prefix rows on, and with more query rows than make the prefix a matter of memory, weights are two numbers
+// instead of three: the matrix units are the bound, and a sum over so many rows in fp32 throughout is off by as much.
+constexpr int TWO_TERMS_ROWS = 16384;
+
 template <typename T, int D>
-wave_status attend_td(const AttendArgs& a, const CacheAttendGeom& g, hipStream_t st) {
-  if (a.P > 0) {
-    const unsigned grid = a.Hkv * a.splits * g.mtiles;
-    if (g.mtile == 16) WAVE_LAUNCH("prefix_rows", (prefix_rows_kernel<T, D, 1>), grid, 256, 0, st, a);
-    if (g.mtile == 32) WAVE_LAUNCH("prefix_rows", (prefix_rows_kernel<T, D, 2>), grid, 256, 0, st, a);
-    if constexpr (sizeof(T) == 2) {
-      if (g.mtile == 64) WAVE_LAUNCH("prefix_shared", (prefix_shared_kernel<D, 1>), grid, 256, 0, st, a);
-      if (g.mtile == 128) WAVE_LAUNCH("prefix_shared", (prefix_shared_kernel<D, 2>), grid, 256, 0, st, a);
+wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
+  a.prefix_blocks = a.P > 0 ? a.Hkv * a.splits * g.mtiles : 0;
+  a.own_blocks = a.Hkv * g.pieces;
+  a.turn = a.prefix_blocks < 256 ? (a.prefix_blocks + 7) / 8 * 8 : 256;
+  if (a.turn == 0) a.turn = 256;
+  a.prefix_turns = (a.prefix_blocks + a.turn - 1) / a.turn;
+  const int own_turns = (a.own_blocks + a.turn - 1) / a.turn;
+  const unsigned blocks = own_turns >= a.prefix_turns ? a.turn * (a.prefix_turns - 1 + own_turns) + a.own_blocks - a.turn * (own_turns - 1)
+                                                      : a.turn * (2 * a.prefix_turns - 2) + a.prefix_blocks - a.turn * (a.prefix_turns - 1);
+  bool shared = false;
+  if constexpr (sizeof(T) == 2) {
+    shared = a.P > 0 && g.mtile > 16;
+    if (shared) {
+      if (g.mtile == 64)
+        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 1, 3>), blocks, 256, 0, st, a);
+      else if (a.P < TWO_TERMS_ROWS)
+        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 2, 3>), blocks, 256, 0, st, a);
+      else
+        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 2, 2>), blocks, 256, 0, st, a);
     }
   }
-  WAVE_LAUNCH("own_rows", (own_rows_kernel<T, D>), a.Hkv * g.pieces, 256, 0, st, a);
-  const long long chunks = ((long long)a.capacity + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
-  const unsigned grid = a.B * a.Hq + (a.weights_out ? (unsigned)(a.B * a.Hkv * chunks) : 0u);
-  WAVE_LAUNCH("cache_join", join_kernel<D>, grid, 256, 0, st, a);
+  if (!shared) WAVE_LAUNCH("cache_attend", (attend_rows_kernel<T, D>), blocks, 256, 0, st, a);
+  switch (a.G) {
+#define WAVE_G(n)                                                                                              \
+  case n: {                                                                                                    \
+    const int chunks = (a.capacity + weight_rows(n) - 1) / weight_rows(n);                                     \
+    const unsigned grid = a.B * a.Hq + (a.weights_out ? a.B * a.Hkv * chunks : 0);                             \
+    WAVE_LAUNCH("cache_join", (join_kernel<D, n>), grid, 256, 0, st, a);                                       \
+    break;                                                                                                     \
+  }
+    WAVE_G(1) WAVE_G(2) WAVE_G(3) WAVE_G(4) WAVE_G(5) WAVE_G(6) WAVE_G(7) WAVE_G(8)
+#undef WAVE_G
+    default: return WAVE_ERR_SHAPE;
+  }
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }
 
@@ -716,16 +823,19 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
   const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
   g.pieces = (int)((long long)g.target + c.B < most ? g.target + c.B : most);
   const int M = c.B * G;
-  g.mtile = M <= 16 ? 16 : c.dtype == WAVE_F32 ? 32 : M <= 64 ? 64 : 128;
+  g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : M <= 64 ? 64 : 128;
   g.mtiles = (M + g.mtile - 1) / g.mtile;
   if (P > 0) {
-    const int want = 512 / (c.Hkv * g.mtiles) > 1 ? 512 / (c.Hkv * g.mtiles) : 1;
+      // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 64 us
+    // instead of 73 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory.
+    const int aim = g.mtile == 128 && c.d == 128 ? 256 : 512, want = aim / (c.Hkv * g.mtiles) > 1 ? aim / (c.Hkv * g.mtiles) : 1;
     const long long rows = ((long long)P + want - 1) / want;
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);
   }
   g.zrow = (c.capacity + 31) / 32 * 32;  // whole steps
   size_t o = 0;
+  g.off_info = o;  o = align_up(o + sizeof(int32_t) * 2 * (size_t)c.B);
   g.off_z = o;     o = align_up(o + (accumulate ? sizeof(float) * (size_t)c.B * Hq * g.zrow : 0));
   g.off_ml = o;    o = align_up(o + sizeof(float) * 2 * (size_t)Hq * g.pieces);
   g.off_acc = o;   o = align_up(o + sizeof(float) * c.d * (size_t)Hq * g.pieces);
@@ -756,6 +866,7 @@ wave_status launch_cache_attend(const void* q, int Hq, const wave_cache& c, cons
   a.acc = reinterpret_cast<float*>(w + g.off_acc);
   a.pml = reinterpret_cast<float2*>(w + g.off_pml);
   a.pacc = reinterpret_cast<float*>(w + g.off_pacc);
+  a.info = reinterpret_cast<int2*>(w + g.off_info);
   a.B = c.B;
   a.Hq = Hq;
   a.Hkv = c.Hkv;

@@ -367,7 +367,7 @@ struct CacheAttendGeom {
   int mtile, mtiles;         // query rows of a prefix workgroup, workgroups over the B * G query rows
   int prefix_rows, splits;   // prefix rows per workgroup, workgroups over the prefix
   int zrow;                  // floats per head in the scores
-  size_t off_z, off_ml, off_acc, off_pml, off_pacc, total;
+  size_t off_info, off_z, off_ml, off_acc, off_pml, off_pacc, total;
 };
 CacheAttendGeom cache_attend_geometry(const wave_cache& cache, int Hq, int P, bool accumulate);
 wave_status launch_cache_attend(const void* q, int Hq, const wave_cache& cache, const void* prefix_k,
