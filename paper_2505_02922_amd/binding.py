@@ -428,25 +428,38 @@ def _require(ok: bool, status: int, where: str) -> None:
         raise WaveError(status, where)
 
 
-def _require_on_gpu(device: torch.device, where: str, *tensors: Optional[torch.Tensor]) -> None:
-    """Every tensor on the one GPU `device` (a kernel would fault on another's memory)."""
-    _require(device.type == "cuda" and all(t is None or t.device == device for t in tensors), 1, where)
+def _together(where: str, index: int, *tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor on GPU `index` (a kernel would fault on memory that is elsewhere)."""
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise WaveError(1, where)
+    if index < 0:
+        raise WaveError(1, where)
 
 
-def _require_dense(where: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...]) -> None:
+def _as_is(where: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...]) -> torch.Tensor:
     """What a call writes, or keeps from call to call, is taken as it is: never a copy of it."""
-    _require(t.dtype == dtype, 3, where)
-    _require(tuple(t.shape) == tuple(shape), 2, where)
-    _require(t.is_contiguous(), 1, where)
+    if t.dtype != dtype:
+        raise WaveError(3, where)
+    if t.shape != shape:
+        raise WaveError(2, where)
+    if not t.is_contiguous():
+        raise WaveError(1, where)
+    return t
 
 
-def _enqueue(where: str, device: torch.device, *args) -> None:
-    """Calls a C entry point with `device`'s current stream as its last argument, on that device."""
-    if device.index == torch.cuda.current_device():
-        st = getattr(lib(), where)(*args, torch.cuda.current_stream().cuda_stream)
+def _address(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _enqueue(where: str, index: int, *args) -> None:
+    """Calls a C entry point with GPU `index`'s current stream as its last argument, on that GPU."""
+    call = getattr(lib(), where)
+    if index == torch._C._cuda_getDevice():
+        st = call(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
-        with torch.cuda.device(device):
-            st = getattr(lib(), where)(*args, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(index):
+            st = call(*args, torch._C._cuda_getCurrentRawStream(index))
     if st != 0:
         raise WaveError(st, where)
 
@@ -469,20 +482,21 @@ def wave_rotary_apply(x: torch.Tensor, coords: torch.Tensor, rotary: wave_rotary
     """x [B, H, N, d] f32 or bf16, coords [n_axes, B, N] int32 -> x rotated (into `out`, which may be x
     itself: rotated in place)."""
     where = "wave_rotary_apply"
-    _require(x.dim() == 4 and coords.dim() == 3, 2, where)
-    B, H, N, d = x.shape
+    shape = x.shape
+    _require(len(shape) == 4, 2, where)
+    B, H, N, d = shape
     _require(coords.dtype == torch.int32, 3, where)
-    _require(tuple(coords.shape) == (rotary.n_axes, B, N), 2, where)
-    _require_on_gpu(x.device, where, coords, out)
+    _require(coords.shape == (rotary.n_axes, B, N), 2, where)
+    index = x.get_device()
+    _together(where, index, coords, out)
+    x = x.contiguous()
     if out is None:
-        x = x.contiguous()
         out = torch.empty_like(x)
     else:
-        _require_dense(where, out, x.dtype, x.shape)
-        x = x.contiguous()
+        _as_is(where, out, x.dtype, shape)
     coords = coords.contiguous()
     if x.numel():
-        _enqueue(where, x.device, x.data_ptr(), coords.data_ptr(), ctypes.byref(rotary), _dtype_code(x.dtype),
+        _enqueue(where, index, x.data_ptr(), coords.data_ptr(), ctypes.byref(rotary), _dtype_code(x.dtype),
                  B, H, N, d, out.data_ptr())
     return out
 
@@ -491,13 +505,13 @@ class Cache:
     """A wave_cache struct plus the torch tensors that own its arrays: k and v [B, Hkv, capacity, d],
     positions and weights [B, Hkv, capacity], lengths and tokens [B]."""
 
-    def __init__(self, c: wave_cache, tensors: Dict[str, Optional[torch.Tensor]], dtype: torch.dtype,
-                 device: torch.device):
+    def __init__(self, c: wave_cache, tensors: Dict[str, Optional[torch.Tensor]], dtype: torch.dtype):
         self.c = c
         self.t = tensors
         self.dtype = dtype
-        self.device = device
         self.B, self.Hkv, self.d, self.capacity = c.B, c.Hkv, c.d, c.capacity
+        self.ref = ctypes.byref(c)
+        self.index = tensors["k"].get_device()
 
     def __getattr__(self, name):
         t = self.__dict__.get("t", {})
@@ -513,21 +527,21 @@ def cache_from_tensors(k: torch.Tensor, v: torch.Tensor, positions: Optional[tor
     where = "cache_from_tensors"
     _require(k.dim() == 4, 2, where)
     B, Hkv, capacity, d = k.shape
-    _require_dense(where, k, k.dtype, (B, Hkv, capacity, d))
-    _require_dense(where, v, k.dtype, (B, Hkv, capacity, d))
+    _as_is(where, k, k.dtype, (B, Hkv, capacity, d))
+    _as_is(where, v, k.dtype, (B, Hkv, capacity, d))
     for t, dt in ((positions, torch.int32), (weights, torch.float32)):
         if t is not None:
-            _require_dense(where, t, dt, (B, Hkv, capacity))
+            _as_is(where, t, dt, (B, Hkv, capacity))
     for t in (lengths, tokens):
         if t is not None:
-            _require_dense(where, t, torch.int32, (B,))
+            _as_is(where, t, torch.int32, (B,))
     _require(all(t is None or t.device == k.device for t in (v, positions, weights, lengths, tokens)), 1, where)
     tensors = {"k": k, "v": v, "positions": positions, "weights": weights, "lengths": lengths, "tokens": tokens}
     c = wave_cache()
     c.dtype, c.B, c.Hkv, c.d, c.capacity = _dtype_code(k.dtype), B, Hkv, d, capacity
     for name, t in tensors.items():
         setattr(c, name, _ptr(t))
-    return Cache(c, tensors, k.dtype, k.device)
+    return Cache(c, tensors, k.dtype)
 
 
 def alloc_cache(dtype: torch.dtype, B: int, Hkv: int, d: int, capacity: int, device="cuda") -> Cache:
@@ -548,43 +562,43 @@ def wave_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, q: Optiona
     behind each sequence's rows and advances lengths and tokens, in place unless other tensors are given.
     Returns q rotated (q_out, which may be q)."""
     where = "wave_cache_append"
-    _require(k.dim() == 4 and k.shape == v.shape and k.shape[:2] == (cache.B, cache.Hkv) and k.shape[3] == cache.d, 2, where)
-    _require(k.dtype == v.dtype == cache.dtype, 3, where)
-    B, _, n, d = k.shape
-    Hq = 0
+    B, d, dtype = cache.B, cache.d, cache.dtype
+    shape = k.shape
+    _require(len(shape) == 4 and shape[0] == B and shape[1] == cache.Hkv and shape[3] == d and v.shape == shape, 2, where)
+    _require(k.dtype == dtype and v.dtype == dtype, 3, where)
+    n, Hq = shape[2], 0
     if q is not None:
-        _require(q.dim() == 4 and q.shape[0] == B and tuple(q.shape[2:]) == (n, d), 2, where)
-        _require(q.dtype == cache.dtype, 3, where)
+        _require(q.dim() == 4 and q.shape[0] == B and q.shape[2:] == (n, d), 2, where)
+        _require(q.dtype == dtype, 3, where)
         Hq = q.shape[1]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if counts is None else \
-                torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        _require_dense(where, q_out, q.dtype, q.shape)
+            new = torch.empty if counts is None else torch.zeros
+            q_out = new(q.shape, dtype=dtype, device=q.device)
+        _as_is(where, q_out, dtype, q.shape)
         q = q.contiguous()
+    else:
+        q_out = None
     if coords is not None:
         _require(coords.dtype == torch.int32, 3, where)
         _require(rotary is not None, 1, where)
-        _require(tuple(coords.shape) == (rotary.n_axes, B, n), 2, where)
+        _require(coords.shape == (rotary.n_axes, B, n), 2, where)
         coords = coords.contiguous()
     if counts is not None:
         _require(counts.dtype == torch.int32, 3, where)
-        _require(tuple(counts.shape) == (B,), 2, where)
+        _require(counts.shape == (B,), 2, where)
         counts = counts.contiguous()
-    lengths_out = cache.lengths if lengths_out is None else lengths_out
-    tokens_out = cache.tokens if tokens_out is None else tokens_out
-    for t in (lengths_out, tokens_out):
-        if t is not None:
-            _require_dense(where, t, torch.int32, (B,))
-    _require_on_gpu(cache.device, where, k, v, q, q_out, coords, counts, lengths_out, tokens_out)
+    lengths_out = cache.t["lengths"] if lengths_out is None else _as_is(where, lengths_out, torch.int32, (B,))
+    tokens_out = cache.t["tokens"] if tokens_out is None else _as_is(where, tokens_out, torch.int32, (B,))
+    _together(where, cache.index, k, v, q, q_out, coords, counts, lengths_out, tokens_out)
     k, v = k.contiguous(), v.contiguous()
-    _enqueue(where, cache.device, ctypes.byref(cache.c), _ptr(k), _ptr(v), _ptr(q), Hq, n, _ptr(counts),
-             ctypes.byref(rotary) if rotary is not None else None, _ptr(coords), _ptr(q_out) if q is not None else None,
-             _ptr(lengths_out), _ptr(tokens_out))
-    return q_out if q is not None else None
+    _enqueue(where, cache.index, cache.ref, k.data_ptr(), v.data_ptr(), _address(q), Hq, n, _address(counts),
+             None if rotary is None else ctypes.byref(rotary), _address(coords), _address(q_out), lengths_out.data_ptr(),
+             _address(tokens_out))
+    return q_out
 
 
 def wave_cache_attention_workspace(cache: Cache, Hq: int, P: int, accumulate: bool) -> int:
-    return int(lib().wave_cache_attention_workspace(ctypes.byref(cache.c), Hq, P, 1 if accumulate else 0))
+    return int(lib().wave_cache_attention_workspace(cache.ref, Hq, P, 1 if accumulate else 0))
 
 
 def wave_cache_attention_decode(q: torch.Tensor, cache: Cache, prefix_k: Optional[torch.Tensor] = None,
@@ -595,36 +609,34 @@ def wave_cache_attention_decode(q: torch.Tensor, cache: Cache, prefix_k: Optiona
     sequence's rows, under one softmax.  weights_out (cache.weights: in place) receives decay * weights +
     what each row got in this step.  Returns (out [B,Hq,d] f32, lse [B,Hq] f32)."""
     where = "wave_cache_attention_decode"
-    _require(q.dim() == 3 and q.shape[0] == cache.B and q.shape[2] == cache.d, 2, where)
-    _require(q.dtype == cache.dtype, 3, where)
+    shape, dtype, P = q.shape, cache.dtype, 0
+    _require(len(shape) == 3 and shape[0] == cache.B and shape[2] == cache.d, 2, where)
+    _require(q.dtype == dtype, 3, where)
     _require((prefix_k is None) == (prefix_v is None), 1, where)
-    B, Hq, d = q.shape
-    P = 0
+    B, Hq, d = shape
     if prefix_k is not None:
-        _require(prefix_k.dim() == 3 and prefix_k.shape == prefix_v.shape, 2, where)
-        _require(prefix_k.shape[0] == cache.Hkv and prefix_k.shape[2] == d, 2, where)
-        _require(prefix_k.dtype == prefix_v.dtype == cache.dtype, 3, where)
-        P = prefix_k.shape[1]
+        rows = prefix_k.shape
+        _require(len(rows) == 3 and rows[0] == cache.Hkv and rows[2] == d and prefix_v.shape == rows, 2, where)
+        _require(prefix_k.dtype == dtype and prefix_v.dtype == dtype, 3, where)
+        P = rows[1]
         prefix_k, prefix_v = prefix_k.contiguous(), prefix_v.contiguous()
     if weights_out is not None:
-        _require_dense(where, weights_out, torch.float32, (B, cache.Hkv, cache.capacity))
-    if out is None:
-        out = torch.empty(B, Hq, d, dtype=torch.float32, device=q.device)
-    if lse is None:
-        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
-    _require_dense(where, out, torch.float32, (B, Hq, d))
-    _require_dense(where, lse, torch.float32, (B, Hq))
+        _as_is(where, weights_out, torch.float32, (B, cache.Hkv, cache.capacity))
+    out = torch.empty(B, Hq, d, dtype=torch.float32, device=q.device) if out is None else \
+        _as_is(where, out, torch.float32, shape)
+    lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if lse is None else \
+        _as_is(where, lse, torch.float32, (B, Hq))
     if ws is None:
-        ws = workspace(wave_cache_attention_workspace(cache, Hq, P, weights_out is not None), cache.device)
-    _require_on_gpu(cache.device, where, q, prefix_k, prefix_v, weights_out, out, lse, ws)
+        ws = workspace(wave_cache_attention_workspace(cache, Hq, P, weights_out is not None), cache.t["k"].device)
+    _together(where, cache.index, q, prefix_k, prefix_v, weights_out, out, lse, ws)
     q = q.contiguous()
-    _enqueue(where, cache.device, q.data_ptr(), Hq, ctypes.byref(cache.c), _ptr(prefix_k), _ptr(prefix_v), P, decay,
-             _ptr(weights_out), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+    _enqueue(where, cache.index, q.data_ptr(), Hq, cache.ref, _address(prefix_k), _address(prefix_v), P, decay,
+             _address(weights_out), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.nbytes)
     return out, lse
 
 
 def wave_cache_evict_workspace(cache: Cache, n_keep: int) -> int:
-    return int(lib().wave_cache_evict_workspace(ctypes.byref(cache.c), n_keep))
+    return int(lib().wave_cache_evict_workspace(cache.ref, n_keep))
 
 
 def wave_cache_evict(cache: Cache, n_keep: int, n_sink: int, n_local: int, to: Optional[Cache] = None,
@@ -634,10 +646,10 @@ def wave_cache_evict(cache: Cache, n_keep: int, n_sink: int, n_local: int, to: O
     where = "wave_cache_evict"
     to = cache if to is None else to
     if ws is None:
-        ws = workspace(wave_cache_evict_workspace(cache, n_keep), cache.device)
-    _require_on_gpu(cache.device, where, to.k, ws)
-    _enqueue(where, cache.device, ctypes.byref(cache.c), ctypes.byref(to.c), n_keep, n_sink, n_local, ws.data_ptr(),
-             ws.numel() * ws.element_size())
+        ws = workspace(wave_cache_evict_workspace(cache, n_keep), cache.t["k"].device)
+    _require(to.index == cache.index, 1, where)
+    _together(where, cache.index, ws)
+    _enqueue(where, cache.index, cache.ref, to.ref, n_keep, n_sink, n_local, ws.data_ptr(), ws.nbytes)
     return to
 
 

@@ -59,13 +59,14 @@ struct Step<bf16_t, D> {
     }
     return k;
   }
+  template <bool ONCE>
   static __device__ __forceinline__ V load_v(const char* base, int k0, int last, int g, int c) {
     V v;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const char* at = base + (size_t)min(k0 + key(g, j), last) * (D * 2) + c * (CH * 2);
       if constexpr (CH == 8) {
-        const uint4 u = load16(at);
+        const uint4 u = ONCE ? load16_stream(at) : load16(at);
         v.x[j][0] = u.x; v.x[j][1] = u.y; v.x[j][2] = u.z; v.x[j][3] = u.w;
       } else {
         const uint2 u = *reinterpret_cast<const uint2*>(at);
@@ -154,6 +155,9 @@ struct Step<float, D> {
   static __device__ __forceinline__ int key(int g, int s) { return g * 4 + s; }
   static __device__ __forceinline__ int channel(int g, int a, int i) { return (a >> 2) * 64 + (g * 4 + i) * 4 + (a & 3); }
   static __device__ __forceinline__ f32x4 load(const char* p) { return *reinterpret_cast<const f32x4*>(p); }
+  static __device__ __forceinline__ f32x4 load_once(const char* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+  }
 
   static __device__ __forceinline__ Q load_q(const char* row, int g) {
     Q q;
@@ -168,13 +172,16 @@ struct Step<float, D> {
     for (int s = 0; s < KC; ++s) k.x[s] = load(row + (s * 16 + g * 4) * 4);
     return k;
   }
+  template <bool ONCE>
   static __device__ __forceinline__ V load_v(const char* base, int k0, int last, int g, int c) {
     V v;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int u = 0; u < CV; ++u)
-        v.x[i][u] = load(base + (size_t)min(k0 + g * 4 + i, last) * (D * 4) + (u * 64 + c * 4) * 4);
+      for (int u = 0; u < CV; ++u) {
+        const char* at = base + (size_t)min(k0 + g * 4 + i, last) * (D * 4) + (u * 64 + c * 4) * 4;
+        v.x[i][u] = ONCE ? load_once(at) : load(at);
+      }
     return v;
   }
   static __device__ __forceinline__ void mask_v(V& v, int k0, int last, int g) {
@@ -255,16 +262,18 @@ struct State {
 
 // ----------------------------------------------------------------------------
 // The stream of one wave: the rows k0, k0 + stride, .. below `end` against a tile of query columns.  z: where a lane leaves
-// the products of its column (NULL: nowhere).
+// the products of its column (NULL: nowhere).  ONCE: nobody else reads these rows, so value rows, which a load instruction
+// takes whole, pass by the caches (1.12 GB: 222 instead of 235 us); key rows must not, two instructions share each of their
+// lines.
 // ----------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0, int stride, int end, float scale,
                                             const typename Step<T, D>::Q& q, State<T, D>& st, float* z, int g, int c) {
   typedef Step<T, D> S;
   const int last = end - 1;
   if (k0 >= end) return;
   typename S::K k = S::load_k(K, k0, last, g, c);
-  typename S::V v = S::load_v(V, k0, last, g, c);
+  typename S::V v = S::template load_v<ONCE>(V, k0, last, g, c);
   for (;;) {
     const int next = k0 + stride;
     const bool ragged = k0 + S::KEYS > end;
@@ -285,7 +294,7 @@ __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0
         *reinterpret_cast<f32x4*>(z + k0 + S::key(g, i)) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
     }
     const typename S::Vt vt = S::transpose(v);
-    v = S::load_v(V, next, last, g, c);
+    v = S::template load_v<ONCE>(V, next, last, g, c);
     st.weigh(s, scale);
     S::template accumulate<3>(vt, s, st.o);
     if (next >= end) return;
@@ -420,8 +429,8 @@ __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinSha
   State<T, D> st;
   st.init();
   float* z = a.weights_out && c < a.G ? a.z + bh * a.zrow : nullptr;
-  stream_rows<T, D>(a.k + unit * a.capacity * row, a.v + unit * a.capacity * row, start + wave * S::KEYS, 4 * S::KEYS, end,
-                    a.scale, q, st, z, g, c);
+  stream_rows<T, D, true>(a.k + unit * a.capacity * row, a.v + unit * a.capacity * row, start + wave * S::KEYS, 4 * S::KEYS, end,
+                          a.scale, q, st, z, g, c);
   const size_t at = ((size_t)h * a.pieces + w) * a.G;
   join_waves<T, D>(st, a.G, js, areas, wave, g, c, a.ml + at, a.acc + at * D);
 }
@@ -440,8 +449,8 @@ __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, Join
   State<T, D> st;
   st.init();
   const int start = split * a.prefix_rows, end = min(a.P, start + a.prefix_rows);
-  stream_rows<T, D>(a.prefix_k + (size_t)h * a.P * row, a.prefix_v + (size_t)h * a.P * row, start + wave * S::KEYS,
-                    4 * S::KEYS, end, a.scale, q, st, nullptr, g, c);
+  stream_rows<T, D, false>(a.prefix_k + (size_t)h * a.P * row, a.prefix_v + (size_t)h * a.P * row, start + wave * S::KEYS,
+                           4 * S::KEYS, end, a.scale, q, st, nullptr, g, c);
   const size_t at = ((size_t)split * a.Hkv + h) * M + m0;  // by KV head and query row
   join_waves<T, D>(st, min(16, M - m0), js, areas, wave, g, c, a.pml + at, a.pacc + at * D);
 }
