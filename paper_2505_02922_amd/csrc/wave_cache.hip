@@ -236,9 +236,12 @@ __global__ __launch_bounds__(256) void advance_kernel(const AppendArgs a) {
 }
 
 // ----------------------------------------------------------------------------
-// Eviction.  evict_select_kernel: one workgroup per unit finds the n_keep-th largest key by three histogram sweeps
-// (11, 11 and 10 bits), then lists, in ascending order, the holes (rows below n_keep that leave) and the movers (rows
-// from n_keep on that stay); there are as many of one as of the other.  evict_move_kernel copies K and V rows.
+// Eviction.  The n_keep-th largest key of a unit comes from three histograms (11, 11 and 10 bits, LDS atomics: integers, so
+// the order of the counting does not show); then holes (rows below n_keep that leave) and movers (rows from n_keep on that
+// stay) are listed in ascending order; there are as many of one as of the other.  evict_move_kernel copies the rows.
+// Short caches: one workgroup per unit with the keys in registers.  Long ones (more than 16384 rows): slices of 8192 rows
+// with a launch for each histogram, since one workgroup would be alone with the unit's atomics (120K rows of 16 units: one
+// workgroup each 330 us).
 // ----------------------------------------------------------------------------
 struct EvictArgs {
   const int32_t *positions, *lengths, *tokens;
@@ -247,8 +250,14 @@ struct EvictArgs {
   float* to_weights;
   const char *k, *v;
   char *to_k, *to_v;
-  int32_t *count, *hole, *mover, *source;  // source: NULL where K and V stay in place
+  // per unit: moved and kept rows; the lists of in-place moves; where K and V are written apart (else NULL) the old row of
+  // every new one, -1 - i for the i-th mover's place
+  int32_t *count, *hole, *mover, *source;
+  uint32_t *hist_a, *hist_b;               // [units][slices][2048]
+  int4* state;                             // [units] bits of the threshold so far, how many rows with them are kept
+  int32_t* above;                          // [units][slices] rows of a slice above the threshold's bits so far
   int Hkv, capacity, to_capacity, n_keep, n_sink, n_local, moves;
+  int slices, keep_slices;                 // slices of a unit; those of the rows below n_keep come first
 };
 
 // Order of the rows as integers: what has to stay above every weight, what is no number below.
@@ -256,159 +265,371 @@ __device__ __forceinline__ uint32_t evict_key(float w, int position, int n_sink,
   if (position < n_sink || position >= local) return 0xffffffffu;
   if (w != w) return 0u;
   const uint32_t u = __float_as_uint(w + 0.f);  // -0 counts as 0
-  return ((u >> 31) ? ~u : (u | 0x80000000u)) ;
+  return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
-constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
+constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64, EVICT_BUCKETS = 2048;
+constexpr int SLICE_PER = 8, SLICE_ROWS = SLICE_PER * EVICT_THREADS;
+__device__ __forceinline__ constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
 
-__global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(const EvictArgs a) {
-  __shared__ uint32_t hist[2048];
-  __shared__ int wave_total[EVICT_WAVES][2];
-  __shared__ uint32_t bucket_at;
-  __shared__ int above_at;
-  const int unit = blockIdx.x, b = unit / a.Hkv, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int len = min(max(a.lengths[b], 0), a.capacity);
-  const long long local = (long long)a.tokens[b] - a.n_local;
-  const int32_t* pos = a.positions + (size_t)unit * a.capacity;
-  const float* wts = a.weights + (size_t)unit * a.capacity;
-  int32_t* to_pos = a.to_positions + (size_t)unit * a.to_capacity;
-  float* to_wts = a.to_weights + (size_t)unit * a.to_capacity;
-  int32_t* source = a.source ? a.source + (size_t)unit * a.n_keep : nullptr;
-  const bool copy_pos = to_pos != pos, copy_wts = to_wts != wts;
-  const int keep = min(len, a.n_keep);
-  if (tid == 0) {
-    a.count[2 * unit] = 0;
-    a.count[2 * unit + 1] = keep;
+struct EvictUnit {
+  int unit, b, len, keep;
+  long long local;
+  const int32_t* pos;
+  const float* wts;
+};
+__device__ __forceinline__ EvictUnit evict_unit(const EvictArgs& a, int unit) {
+  EvictUnit u;
+  u.unit = unit;
+  u.b = unit / a.Hkv;
+  u.len = min(max(a.lengths[u.b], 0), a.capacity);
+  u.keep = min(u.len, a.n_keep);
+  u.local = (long long)a.tokens[u.b] - a.n_local;
+  u.pos = a.positions + (size_t)unit * a.capacity;
+  u.wts = a.weights + (size_t)unit * a.capacity;
+  return u;
+}
+// keys of the rows r0 + i * 1024 + tid below r1 (others: 0, and no row)
+template <int PER>
+__device__ __forceinline__ void evict_keys(const EvictArgs& a, const EvictUnit& u, int r0, int r1, uint32_t (&key)[PER]) {
+  float w[PER];
+  int p[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = min(r0 + i * EVICT_THREADS + (int)threadIdx.x, r1 - 1);
+    w[i] = u.wts[j];
+    p[i] = u.pos[j];
   }
-  if (len <= a.n_keep) {
-    for (int j = tid; j < len; j += EVICT_THREADS) {
-      if (copy_pos) to_pos[j] = pos[j];
-      if (copy_wts) to_wts[j] = wts[j];
-      if (source) source[j] = j;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) key[i] = evict_key(w[i], p[i], a.n_sink, u.local);
+}
+
+struct EvictShared {
+  uint32_t hist[EVICT_BUCKETS];
+  int wave_total[EVICT_WAVES];
+  int table[16 * EVICT_WAVES];
+  int bucket, above;
+};
+// Counts the keys' digit `pass` where the digits before are `prefix`.
+template <int PER>
+__device__ __forceinline__ void evict_count(EvictShared& sh, const uint32_t (&key)[PER], int r0, int r1, int pass, uint32_t prefix) {
+  for (int i = threadIdx.x; i < EVICT_BUCKETS; i += EVICT_THREADS) sh.hist[i] = 0;
+  __syncthreads();
+  const int shift = digit_shift(pass), bits = digit_bits(pass);
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (r0 + i * EVICT_THREADS + (int)threadIdx.x < r1 && (pass == 0 || key[i] >> (shift + bits) == prefix))
+      atomicAdd(&sh.hist[(key[i] >> shift) & ((1 << bits) - 1)], 1u);
+  __syncthreads();
+}
+// Given the counts c0, c1 of this thread's buckets 2047 - 2 tid and 2046 - 2 tid: the bucket in which the count from the
+// top reaches `need`, and the count above it.
+__device__ __forceinline__ int2 evict_bucket(EvictShared& sh, int c0, int c1, int need) {
+  const int tid = threadIdx.x, wave = tid >> 6, top = EVICT_BUCKETS - 1 - 2 * tid;
+  const int incl = wave_incl_scan(c0 + c1);
+  if ((tid & 63) == 63) sh.wave_total[wave] = incl;
+  __syncthreads();
+  int before = incl - c0 - c1;
+  for (int w = 0; w < wave; ++w) before += sh.wave_total[w];
+  if (before < need && before + c0 >= need) {
+    sh.bucket = top;
+    sh.above = before;
+  } else if (before + c0 < need && before + c0 + c1 >= need) {
+    sh.bucket = top - 1;
+    sh.above = before + c0;
+  }
+  __syncthreads();
+  const int2 r = make_int2(sh.bucket, sh.above);
+  __syncthreads();
+  return r;
+}
+// Exclusive sums, over (i, wave) in this order, of one number each wave has for every i; all threads call it.
+template <int PER>
+__device__ __forceinline__ int evict_scan(EvictShared& sh, const int (&mine)[PER], int (&before)[PER]) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  constexpr int ALL = PER * EVICT_WAVES, EACH = (ALL + 63) / 64;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (lane == 0) sh.table[i * EVICT_WAVES + wave] = mine[i];
+  __syncthreads();
+  if (wave == 0) {
+    int x[EACH], sum = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      x[e] = lane * EACH + e < ALL ? sh.table[lane * EACH + e] : 0;
+      sum += x[e];
+    }
+    int run = wave_incl_scan(sum);
+    if (lane == 63) sh.above = run;
+    run -= sum;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      if (lane * EACH + e < ALL) sh.table[lane * EACH + e] = run;
+      run += x[e];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) before[i] = sh.table[i * EVICT_WAVES + wave];
+  const int total = sh.above;
+  __syncthreads();
+  return total;
+}
+// Lists the holes and movers among the rows r0 + i * 1024 + tid below r1.  need: how many rows with the threshold's key are
+// kept, equal_before: how many of them lie before r0; hole_before, mover_before: what the lists hold from rows before r0.
+// Returns holes | movers << 16 of these rows.
+template <int PER>
+__device__ __forceinline__ int evict_list(EvictShared& sh, const EvictArgs& a, const EvictUnit& u, const uint32_t (&key)[PER], int r0,
+                                          int r1, uint32_t threshold, int need, int equal_before, int hole_before,
+                                          int mover_before) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const uint64_t below = (1ull << lane) - 1;
+  int mine[PER], before[PER];
+  uint64_t eq[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    eq[i] = __ballot(r0 + i * EVICT_THREADS + tid < r1 && key[i] == threshold);
+    mine[i] = __popcll(eq[i]);
+  }
+  evict_scan<PER>(sh, mine, before);
+  uint64_t hb[PER], mb[PER];
+  uint32_t kept_bits = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = r0 + i * EVICT_THREADS + tid;
+    const int rank = equal_before + before[i] + __popcll(eq[i] & below);
+    const bool kept = j < r1 && (key[i] > threshold || (key[i] == threshold && rank < need));
+    if (kept) kept_bits |= 1u << i;
+    hb[i] = __ballot(j < u.keep && !kept && j < r1);
+    mb[i] = __ballot(j >= u.keep && kept);
+    mine[i] = __popcll(hb[i]) | (__popcll(mb[i]) << 16);
+  }
+  const int total = evict_scan<PER>(sh, mine, before);
+  int32_t* holes = a.hole + (size_t)u.unit * a.moves;
+  int32_t* movers = a.mover + (size_t)u.unit * a.moves;
+  int32_t* source = a.source ? a.source + (size_t)u.unit * a.n_keep : nullptr;
+  int32_t* to_pos = a.to_positions + (size_t)u.unit * a.to_capacity;
+  float* to_wts = a.to_weights + (size_t)u.unit * a.to_capacity;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = r0 + i * EVICT_THREADS + tid;
+    const bool kept = (kept_bits >> i) & 1u;
+    if (j < r1 && j < u.keep && !kept) {
+      const int at = hole_before + (before[i] & 0xffff) + __popcll(hb[i] & below);
+      if (source)
+        source[j] = -1 - at;
+      else
+        holes[at] = j;
+    }
+    if (j >= u.keep && kept) movers[mover_before + (before[i] >> 16) + __popcll(mb[i] & below)] = j;
+    if (kept && j < u.keep) {
+      if (source) {
+        source[j] = j;
+      } else {
+        if (to_pos != u.pos) to_pos[j] = u.pos[j];
+        if (to_wts != u.wts) to_wts[j] = u.wts[j];
+      }
+    }
+  }
+  return total;
+}
+
+template <int PER>
+__global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(const EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x;
+  const EvictUnit u = evict_unit(a, blockIdx.x);
+  if (u.len == 0 || (u.len <= a.n_keep && !a.source && a.to_positions == a.positions && a.to_weights == a.weights)) {
+    if (tid == 0) {  // nothing to do
+      a.count[2 * u.unit] = 0;
+      a.count[2 * u.unit + 1] = u.keep;
     }
     return;
   }
-  if (keep == 0) return;
-  auto key_of = [&](int j) { return evict_key(wts[j], pos[j], a.n_sink, local); };
-  // the keep-th largest key: its upper bits one histogram at a time
-  uint32_t prefix = 0;
-  int need = keep;  // how many of the rows that share the prefix are kept
-  const int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = shifts[pass], buckets = 1 << widths[pass];
-    for (int i = tid; i < 2048; i += EVICT_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int j = tid; j < len; j += EVICT_THREADS) {
-      const uint32_t key = key_of(j);
-      if (pass == 0 || (key >> (shift + widths[pass])) == prefix) atomicAdd(&hist[(key >> shift) & (buckets - 1)], 1u);
-    }
-    __syncthreads();
-    // thread t has the buckets 2 t and 2 t + 1, counted from the top
-    const int top = 2047 - 2 * tid;
-    const int c0 = (int)hist[top], c1 = (int)hist[top - 1];
-    const int incl = wave_incl_scan(c0 + c1);
-    if (lane == 63) wave_total[wave][0] = incl;
-    __syncthreads();
-    int before = incl - c0 - c1;
-    for (int w = 0; w < wave; ++w) before += wave_total[w][0];
-    if (before < need && before + c0 >= need) {
-      bucket_at = (uint32_t)top;
-      above_at = before;
-    } else if (before + c0 < need && before + c0 + c1 >= need) {
-      bucket_at = (uint32_t)top - 1;
-      above_at = before + c0;
-    }
-    __syncthreads();
-    prefix = pass == 0 ? bucket_at : (prefix << widths[pass]) | bucket_at;
-    need -= above_at;
-    __syncthreads();
-  }
-  const uint32_t threshold = prefix;  // `need` of the rows with this key are kept, the lowest ones
-  int32_t* holes = a.hole + (size_t)unit * a.moves;
-  int32_t* movers = a.mover + (size_t)unit * a.moves;
-  int equal_before = 0, listed = 0;  // rows with the threshold's key so far; holes, and from row n_keep on movers
-  int n_holes = 0;
-  for (int j0 = 0; j0 < len; j0 += EVICT_THREADS) {
-    const int j = j0 + tid;
-    const uint32_t key = j < len ? key_of(j) : 0u;
-    const bool equal = j < len && key == threshold;
-    const uint64_t eq = __ballot(equal), below = (1ull << lane) - 1;
-    if (lane == 0) wave_total[wave][0] = __popcll(eq);
-    __syncthreads();
-    int rank = equal_before + __popcll(eq & below);
-    int eq_all = 0;
-    for (int w = 0; w < EVICT_WAVES; ++w) {
-      if (w < wave) rank += wave_total[w][0];
-      eq_all += wave_total[w][0];
-    }
-    equal_before += eq_all;
-    const bool kept = j < len && (key > threshold || (equal && rank < need));
-    const bool hole = j < keep && !kept, mover = j >= keep && kept;
-    const uint64_t hb = __ballot(hole), mb = __ballot(mover);
-    if (lane == 0) wave_total[wave][1] = __popcll(hb) | (__popcll(mb) << 16);
-    __syncthreads();
-    int hole_at = n_holes + __popcll(hb & below), mover_at = listed + __popcll(mb & below), all = 0;
-    for (int w = 0; w < EVICT_WAVES; ++w) {
-      if (w < wave) {
-        hole_at += wave_total[w][1] & 0xffff;
-        mover_at += wave_total[w][1] >> 16;
+  uint32_t key[PER];
+  evict_keys<PER>(a, u, 0, u.len, key);
+  uint32_t threshold = 0;
+  int need = u.len;  // nothing leaves: every key is at least 0
+  if (u.len > a.n_keep) {
+    need = u.keep;
+    threshold = 0xffffffffu;
+    if (need > 0) {
+      threshold = 0;
+      for (int pass = 0; pass < 3; ++pass) {
+        evict_count<PER>(sh, key, 0, u.len, pass, threshold);
+        const int top = EVICT_BUCKETS - 1 - 2 * tid;
+        const int2 at = evict_bucket(sh, (int)sh.hist[top], (int)sh.hist[top - 1], need);
+        threshold = (threshold << digit_bits(pass)) | (uint32_t)at.x;
+        need -= at.y;
       }
-      all += wave_total[w][1];
-    }
-    n_holes += all & 0xffff;
-    listed += all >> 16;
-    if (hole) holes[hole_at] = j;
-    if (mover) movers[mover_at] = j;
-    if (kept && j < keep) {
-      if (copy_pos) to_pos[j] = pos[j];
-      if (copy_wts) to_wts[j] = wts[j];
-      if (source) source[j] = j;
     }
   }
-  __syncthreads();  // the lists are complete and no key is read any more
-  for (int i = tid; i < n_holes; i += EVICT_THREADS) {
-    const int h = holes[i], m = movers[i];
-    to_pos[h] = pos[m];
-    to_wts[h] = wts[m];
-    if (source) source[h] = m;
+  const int total = evict_list<PER>(sh, a, u, key, 0, u.len, threshold, need, 0, 0, 0);
+  if (tid == 0) {
+    a.count[2 * u.unit] = total & 0xffff;
+    a.count[2 * u.unit + 1] = u.keep;
   }
-  if (tid == 0) a.count[2 * unit] = n_holes;
+}
+
+// Rows of slice s: those below the budget and those from it on are cut on their own, so that a slice has holes or movers.
+__device__ __forceinline__ int2 slice_rows(const EvictArgs& a, const EvictUnit& u, int s) {
+  const bool low = s < a.keep_slices;
+  const int from = low ? 0 : u.keep, to = low ? u.keep : u.len;
+  const int r0 = min((long long)from + (long long)(low ? s : s - a.keep_slices) * SLICE_ROWS, (long long)to);
+  return make_int2(r0, min(r0 + SLICE_ROWS, to));
+}
+__device__ __forceinline__ int2 slices_bucket(EvictShared& sh, const EvictArgs& a, const uint32_t* hist, int need) {
+  const int top = EVICT_BUCKETS - 1 - 2 * (int)threadIdx.x;
+  int c0 = 0, c1 = 0;
+  for (int s = 0; s < a.slices; ++s) {
+    const uint2 c = *reinterpret_cast<const uint2*>(hist + (size_t)s * EVICT_BUCKETS + top - 1);
+    c0 += (int)c.y;
+    c1 += (int)c.x;
+  }
+  return evict_bucket(sh, c0, c1, need);
+}
+
+// Histogram number PASS of a slice; the threshold's digit before comes from the histograms of all slices of the unit.
+template <int PASS>
+__global__ __launch_bounds__(EVICT_THREADS) void evict_slice_kernel(const EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int unit = blockIdx.x / a.slices, s = blockIdx.x % a.slices, tid = threadIdx.x;
+  const EvictUnit u = evict_unit(a, unit);
+  if (u.len <= a.n_keep || u.keep == 0) return;
+  const int2 r = slice_rows(a, u, s);
+  uint32_t key[SLICE_PER];
+  if (r.x < r.y) evict_keys<SLICE_PER>(a, u, r.x, r.y, key);
+  uint32_t prefix = 0;
+  const size_t at = (size_t)unit * a.slices;
+  if (PASS > 0) {
+    const int4 st = PASS == 1 ? make_int4(0, u.keep, 0, 0) : a.state[2 * unit + PASS - 2];
+    const int2 found = slices_bucket(sh, a, (PASS == 1 ? a.hist_a : a.hist_b) + at * EVICT_BUCKETS, st.y);
+    const uint32_t old = (uint32_t)st.x;
+    prefix = (old << digit_bits(PASS - 1)) | (uint32_t)found.x;
+    if (s == 0 && tid == 0) a.state[2 * unit + PASS - 1] = make_int4((int)prefix, st.y - found.y, 0, 0);
+    // this slice's rows that are above by their digit before
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < SLICE_PER; ++i) {
+      const uint32_t upper = r.x < r.y ? key[i] >> digit_shift(PASS - 1) : 0u;
+      const bool row = r.x + i * EVICT_THREADS + tid < r.y;
+      above += __popcll(__ballot(row && (PASS == 1 || upper >> digit_bits(PASS - 1) == old) && upper > prefix));
+    }
+    if ((tid & 63) == 0) sh.table[tid >> 6] = above;
+    __syncthreads();
+    if (tid == 0) {
+      int sum = PASS == 1 ? 0 : a.above[at + s];
+      for (int w = 0; w < EVICT_WAVES; ++w) sum += sh.table[w];
+      a.above[at + s] = sum;
+    }
+  }
+  evict_count<SLICE_PER>(sh, key, r.x, r.y, PASS, prefix);
+  uint32_t* out = (PASS == 1 ? a.hist_b : a.hist_a) + (at + s) * EVICT_BUCKETS;
+  for (int i = tid; i < EVICT_BUCKETS; i += EVICT_THREADS) out[i] = sh.hist[i];
+}
+
+__global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int unit = blockIdx.x / a.slices, s = blockIdx.x % a.slices, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const EvictUnit u = evict_unit(a, unit);
+  const int2 r = slice_rows(a, u, s);
+  uint32_t key[SLICE_PER];
+  if (r.x < r.y) evict_keys<SLICE_PER>(a, u, r.x, r.y, key);
+  const bool all = u.len <= a.n_keep, none = u.keep == 0;
+  const size_t at = (size_t)unit * a.slices;
+  uint32_t threshold = all ? 0u : 0xffffffffu;
+  int need = all ? u.len : 0, equal_before = 0, hole_before = 0, mover_before = 0, holes = 0;
+  if (!all && !none) {
+    const int4 st = a.state[2 * unit + 1];
+    const uint32_t* hist = a.hist_a + at * EVICT_BUCKETS;
+    const int2 found = slices_bucket(sh, a, hist, st.y);
+    threshold = ((uint32_t)st.x << digit_bits(2)) | (uint32_t)found.x;
+    need = st.y - found.y;
+    // Sixteen slices at a time: their rows above and at the threshold, a wave each; then what lies before this slice.
+    int seen_equal = 0, kept_low = 0, kept_high_before = 0, kept_low_before = 0;
+    for (int s0 = 0; s0 < a.slices; s0 += EVICT_WAVES) {
+      int above = 0;
+      if (s0 + wave < a.slices)
+        for (int i = lane; i < 1 << digit_bits(2); i += 64)
+          above += i > found.x ? (int)hist[(size_t)(s0 + wave) * EVICT_BUCKETS + i] : 0;
+      above = wave_sum_i(above);
+      if (lane == 0 && s0 + wave < a.slices) {
+        sh.table[2 * wave] = above + a.above[at + s0 + wave];
+        sh.table[2 * wave + 1] = (int)hist[(size_t)(s0 + wave) * EVICT_BUCKETS + found.x];
+      }
+      __syncthreads();
+      for (int w = 0; w < EVICT_WAVES && s0 + w < a.slices; ++w) {
+        const int x = s0 + w, equal = sh.table[2 * w + 1];
+        const int kept = sh.table[2 * w] + min(max(need - seen_equal, 0), equal);
+        if (x == s) equal_before = seen_equal;
+        if (x < s) (x < a.keep_slices ? kept_low_before : kept_high_before) += kept;
+        if (x < a.keep_slices) kept_low += kept;
+        seen_equal += equal;
+      }
+      __syncthreads();
+    }
+    hole_before = s < a.keep_slices ? r.x - kept_low_before : 0;
+    mover_before = kept_high_before;
+    holes = u.keep - kept_low;
+  }
+  if (s == 0 && tid == 0) {
+    a.count[2 * unit] = holes;
+    a.count[2 * unit + 1] = u.keep;
+  }
+  if (r.x < r.y)
+    evict_list<SLICE_PER>(sh, a, u, key, r.x, r.y, threshold, need, equal_before, hole_before, mover_before);
 }
 
 constexpr int MOVE_ROWS = 64;  // rows of K and of V of one workgroup
 
-// In place: pair i of the lists.  Apart: row i of the new cache.  D * es / 16 lanes carry a row, four rows of each of K
-// and V in flight a thread.
+// In place: move i of the lists.  Apart: row i of the new cache.  ROW / 16 lanes carry a row, four rows of each of K and V
+// in flight a thread.
 template <int ROW>
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a, int chunks) {
-  constexpr int LPR = ROW / 16, GROUPS = 256 / LPR;
+  constexpr int LPR = ROW / 16, GROUPS = 256 / LPR, U = 4;
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks, b = unit / a.Hkv;
   const int moved = a.count[2 * unit], keep = a.count[2 * unit + 1];
   if (chunk == 0 && unit % a.Hkv == 0 && threadIdx.x == 0) {
     a.to_lengths[b] = keep;
     a.to_tokens[b] = a.tokens[b];
   }
-  const int total = a.source ? keep : moved;
-  const int lane = threadIdx.x % LPR, end = min(total, (chunk + 1) * MOVE_ROWS);
-  constexpr int U = 4;
+  const int lane = threadIdx.x % LPR, end = min(a.source ? keep : moved, (chunk + 1) * MOVE_ROWS);
+  const size_t from_unit = (size_t)unit * a.capacity, to_unit = (size_t)unit * a.to_capacity;
+  const int32_t* movers = a.mover + (size_t)unit * a.moves;
   for (int i0 = chunk * MOVE_ROWS + (int)threadIdx.x / LPR; i0 < end; i0 += U * GROUPS) {
-    uint4 kk[U], vv[U];
-    int dst[U];
+    int src[U], dst[U], pos[U];
+    float w[U];
+    uint4 k[U], v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = min(i0 + u * GROUPS, end - 1);
-      const int src = a.source ? a.source[(size_t)unit * a.n_keep + i] : a.mover[(size_t)unit * a.moves + i];
+      src[u] = a.source ? a.source[(size_t)unit * a.n_keep + i] : movers[i];
       dst[u] = a.source ? i : a.hole[(size_t)unit * a.moves + i];
-      const size_t at = ((size_t)unit * a.capacity + src) * ROW + lane * 16;
-      kk[u] = load16_stream(a.k + at);
-      vv[u] = load16_stream(a.v + at);
+    }
+    if (a.source) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (src[u] < 0) src[u] = movers[-1 - src[u]];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t at = (from_unit + src[u]) * ROW + lane * 16;
+      k[u] = load16_stream(a.k + at);
+      v[u] = load16_stream(a.v + at);
+      pos[u] = a.positions[from_unit + src[u]];
+      w[u] = a.weights[from_unit + src[u]];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i0 + u * GROUPS < end) {
-        const size_t at = ((size_t)unit * a.to_capacity + dst[u]) * ROW + lane * 16;
-        store16(a.to_k + at, kk[u]);
-        store16(a.to_v + at, vv[u]);
+        const size_t row = to_unit + dst[u];
+        store16(a.to_k + row * ROW + lane * 16, k[u]);
+        store16(a.to_v + row * ROW + lane * 16, v[u]);
+        if (lane == 0) {
+          a.to_positions[row] = pos[u];
+          a.to_weights[row] = w[u];
+        }
       }
   }
 }
@@ -484,16 +705,30 @@ wave_status launch_cache_append(const wave_cache& c, const void* k_new, const vo
 CacheEvictGeom cache_evict_geometry(const wave_cache& c, int n_keep) {
   CacheEvictGeom g{};
   const size_t units = (size_t)c.B * c.Hkv;
-  g.moves = n_keep < c.capacity ? (n_keep < c.capacity - n_keep ? n_keep : c.capacity - n_keep) : 0;
+  const int kept = n_keep < c.capacity ? n_keep : c.capacity, rest = c.capacity - kept;
+  g.moves = kept < rest ? kept : rest;
+  if (c.capacity > 16 * EVICT_THREADS) {
+    g.keep_slices = (int)(((long long)kept + SLICE_ROWS - 1) / SLICE_ROWS);
+    g.slices = g.keep_slices + (int)(((long long)rest + SLICE_ROWS - 1) / SLICE_ROWS);
+  }
   const size_t list = align_up(units * g.moves * sizeof(int32_t));
-  const size_t kept = n_keep < c.capacity ? n_keep : c.capacity;
+  const size_t hist = align_up(units * g.slices * EVICT_BUCKETS * sizeof(uint32_t));
   size_t o = 0;
   g.off_count = o;   o = align_up(o + units * 2 * sizeof(int32_t));
   g.off_hole = o;    o += list;
   g.off_mover = o;   o += list;
   g.off_source = o;  o = align_up(o + units * kept * sizeof(int32_t));
+  g.off_hist_a = o;  o += hist;
+  g.off_hist_b = o;  o += hist;
+  g.off_state = o;   o = align_up(o + (g.slices ? units * 2 * sizeof(int4) : 0));
+  g.off_above = o;   o = align_up(o + units * g.slices * sizeof(int32_t));
   g.total = o;
   return g;
+}
+
+template <int PER>
+static void launch_evict_select(const EvictArgs& a, int units, hipStream_t st) {
+  WAVE_LAUNCH("evict_select", evict_select_kernel<PER>, units, EVICT_THREADS, 0, st, a);
 }
 
 wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int n_keep, int n_sink, int n_local,
@@ -517,6 +752,10 @@ wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int
   a.hole = reinterpret_cast<int32_t*>(w + g.off_hole);
   a.mover = reinterpret_cast<int32_t*>(w + g.off_mover);
   a.source = to.k == from.k ? nullptr : reinterpret_cast<int32_t*>(w + g.off_source);
+  a.hist_a = reinterpret_cast<uint32_t*>(w + g.off_hist_a);
+  a.hist_b = reinterpret_cast<uint32_t*>(w + g.off_hist_b);
+  a.state = reinterpret_cast<int4*>(w + g.off_state);
+  a.above = reinterpret_cast<int32_t*>(w + g.off_above);
   a.Hkv = from.Hkv;
   a.capacity = from.capacity;
   a.to_capacity = to.capacity;
@@ -524,10 +763,25 @@ wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int
   a.n_sink = n_sink;
   a.n_local = n_local;
   a.moves = g.moves;
+  a.slices = g.slices;
+  a.keep_slices = g.keep_slices;
   const int units = from.B * from.Hkv, rows = a.source ? a.n_keep : g.moves;
   const int chunks = rows > 0 ? (rows + MOVE_ROWS - 1) / MOVE_ROWS : 1;
-  if ((long long)units * chunks >= (1ll << 24)) return WAVE_ERR_SHAPE;
-  WAVE_LAUNCH("evict_select", evict_select_kernel, units, EVICT_THREADS, 0, st, a);
+  if ((long long)units * chunks >= (1ll << 24) || (long long)units * g.slices >= (1ll << 22)) return WAVE_ERR_SHAPE;
+  if (g.slices > 0) {
+    const int grid = units * g.slices;
+    WAVE_LAUNCH("evict_slice", evict_slice_kernel<0>, grid, EVICT_THREADS, 0, st, a);
+    WAVE_LAUNCH("evict_slice", evict_slice_kernel<1>, grid, EVICT_THREADS, 0, st, a);
+    WAVE_LAUNCH("evict_slice", evict_slice_kernel<2>, grid, EVICT_THREADS, 0, st, a);
+    WAVE_LAUNCH("evict_emit", evict_emit_kernel, grid, EVICT_THREADS, 0, st, a);
+  } else {
+    const int per = (from.capacity + EVICT_THREADS - 1) / EVICT_THREADS;
+    if (per <= 2) launch_evict_select<2>(a, units, st);
+    else if (per <= 3) launch_evict_select<3>(a, units, st);
+    else if (per <= 5) launch_evict_select<5>(a, units, st);
+    else if (per <= 8) launch_evict_select<8>(a, units, st);
+    else launch_evict_select<16>(a, units, st);
+  }
   switch (from.d * (from.dtype == WAVE_BF16 ? 2 : 4)) {
     case 128: WAVE_LAUNCH("evict_move", evict_move_kernel<128>, units * chunks, 256, 0, st, a, chunks); break;
     case 256: WAVE_LAUNCH("evict_move", evict_move_kernel<256>, units * chunks, 256, 0, st, a, chunks); break;

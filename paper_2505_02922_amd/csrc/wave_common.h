@@ -375,7 +375,8 @@ wave_status launch_cache_attend(const void* q, int Hq, const wave_cache& cache, 
                                 void* ws, hipStream_t st);
 struct CacheEvictGeom {
   int moves;                 // room for moved rows per unit
-  size_t off_count, off_hole, off_mover, off_source, total;
+  int slices, keep_slices;   // long caches: slices of a unit, and of its rows below the budget
+  size_t off_count, off_hole, off_mover, off_source, off_hist_a, off_hist_b, off_state, off_above, total;
 };
 CacheEvictGeom cache_evict_geometry(const wave_cache& from, int n_keep);
 wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int n_keep, int n_sink, int n_local,

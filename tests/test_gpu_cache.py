@@ -407,6 +407,27 @@ def test_evict_long():
     _check_evict(cache, before, [130999], 16385, 4, 1024, cache, before)
 
 
+@pytest.mark.parametrize("n_keep,n_sink,n_local", [(0, 0, 0), (1, 0, 1), (8192, 4, 100), (8193, 4, 4000), (16000, 0, 0), (19999, 1, 1)])
+@pytest.mark.parametrize("ties", [False, True])
+def test_evict_caches_of_more_rows_than_a_workgroup_holds(n_keep, n_sink, n_local, ties):
+    """In place and apart; full, half full, short and empty sequences in the same call."""
+    lengths = [20001, 9000, 0, 16385]
+    cache = _filled_cache("bf16", 4, 1, 64, 20001, lengths, n_keep)
+    if ties:
+        few = torch.tensor([0.0, -0.0, 0.25, 0.25, math.nan])
+        cache.weights.copy_(few[torch.randint(0, 5, tuple(cache.weights.shape), generator=_gen(1))])
+    before = {name: t.clone() for name, t in cache.t.items()}
+    to = wb.alloc_cache(torch.bfloat16, 4, 1, 64, max(n_keep, 1) + 3)
+    dst = {name: t.clone() for name, t in to.t.items()}
+    wb.wave_cache_evict(cache, n_keep, n_sink, n_local, to=to)
+    _check_evict(cache, before, lengths, n_keep, n_sink, n_local, to, dst)
+    mixed = wb.cache_from_tensors(cache.k, cache.v, torch.full_like(cache.positions, -9), torch.zeros_like(cache.weights),
+                                  cache.lengths, torch.zeros_like(cache.tokens))
+    dst = {name: t.clone() for name, t in mixed.t.items()}
+    wb.wave_cache_evict(cache, n_keep, n_sink, n_local, to=mixed)
+    _check_evict(cache, before, lengths, n_keep, n_sink, n_local, mixed, dst)
+
+
 # --------------------------------------------------------------------------- together
 
 
