@@ -482,10 +482,16 @@ __device__ __forceinline__ int2 slice_rows(const EvictArgs& a, const EvictUnit& 
 __device__ __forceinline__ int2 slices_bucket(EvictShared& sh, const EvictArgs& a, const uint32_t* hist, int need) {
   const int top = EVICT_BUCKETS - 1 - 2 * (int)threadIdx.x;
   int c0 = 0, c1 = 0;
-  for (int s = 0; s < a.slices; ++s) {
-    const uint2 c = *reinterpret_cast<const uint2*>(hist + (size_t)s * EVICT_BUCKETS + top - 1);
-    c0 += (int)c.y;
-    c1 += (int)c.x;
+  for (int s0 = 0; s0 < a.slices; s0 += 8) {
+    uint2 c[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      c[k] = *reinterpret_cast<const uint2*>(hist + (size_t)min(s0 + k, a.slices - 1) * EVICT_BUCKETS + top - 1);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      c0 += s0 + k < a.slices ? (int)c[k].y : 0;
+      c1 += s0 + k < a.slices ? (int)c[k].x : 0;
+    }
   }
   return evict_bucket(sh, c0, c1, need);
 }
@@ -550,9 +556,16 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictAr
     int seen_equal = 0, kept_low = 0, kept_high_before = 0, kept_low_before = 0;
     for (int s0 = 0; s0 < a.slices; s0 += EVICT_WAVES) {
       int above = 0;
-      if (s0 + wave < a.slices)
-        for (int i = lane; i < 1 << digit_bits(2); i += 64)
-          above += i > found.x ? (int)hist[(size_t)(s0 + wave) * EVICT_BUCKETS + i] : 0;
+      uint4 c[4];  // 1024 buckets
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        c[k] = load16(hist + (size_t)min(s0 + wave, a.slices - 1) * EVICT_BUCKETS + (k * 64 + lane) * 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = (k * 64 + lane) * 4;
+        above += (i > found.x ? (int)c[k].x : 0) + (i + 1 > found.x ? (int)c[k].y : 0) + (i + 2 > found.x ? (int)c[k].z : 0) +
+                 (i + 3 > found.x ? (int)c[k].w : 0);
+      }
       above = wave_sum_i(above);
       if (lane == 0 && s0 + wave < a.slices) {
         sh.table[2 * wave] = above + a.above[at + s0 + wave];
@@ -581,56 +594,38 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictAr
     evict_list<SLICE_PER>(sh, a, u, key, r.x, r.y, threshold, need, equal_before, hole_before, mover_before);
 }
 
-constexpr int MOVE_ROWS = 64;  // rows of K and of V of one workgroup
-
-// In place: move i of the lists.  Apart: row i of the new cache.  ROW / 16 lanes carry a row, four rows of each of K and V
-// in flight a thread.
+// In place: move i of the lists.  Apart: row i of the new cache.  ROW / 16 lanes carry a row of K and of V, one row a thread
+// (283 MB of scattered rows: 50 us, 63 us with four in flight a thread and a quarter of the workgroups).
+template <int ROW>
+constexpr int kMoveRows = 256 / (ROW / 16);
 template <int ROW>
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a, int chunks) {
-  constexpr int LPR = ROW / 16, GROUPS = 256 / LPR, U = 4;
+  constexpr int LPR = ROW / 16;
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks, b = unit / a.Hkv;
   const int moved = a.count[2 * unit], keep = a.count[2 * unit + 1];
   if (chunk == 0 && unit % a.Hkv == 0 && threadIdx.x == 0) {
     a.to_lengths[b] = keep;
     a.to_tokens[b] = a.tokens[b];
   }
-  const int lane = threadIdx.x % LPR, end = min(a.source ? keep : moved, (chunk + 1) * MOVE_ROWS);
-  const size_t from_unit = (size_t)unit * a.capacity, to_unit = (size_t)unit * a.to_capacity;
+  const int i = chunk * kMoveRows<ROW> + (int)threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  if (i >= (a.source ? keep : moved)) return;
   const int32_t* movers = a.mover + (size_t)unit * a.moves;
-  for (int i0 = chunk * MOVE_ROWS + (int)threadIdx.x / LPR; i0 < end; i0 += U * GROUPS) {
-    int src[U], dst[U], pos[U];
-    float w[U];
-    uint4 k[U], v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = min(i0 + u * GROUPS, end - 1);
-      src[u] = a.source ? a.source[(size_t)unit * a.n_keep + i] : movers[i];
-      dst[u] = a.source ? i : a.hole[(size_t)unit * a.moves + i];
-    }
-    if (a.source) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (src[u] < 0) src[u] = movers[-1 - src[u]];
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const size_t at = (from_unit + src[u]) * ROW + lane * 16;
-      k[u] = load16_stream(a.k + at);
-      v[u] = load16_stream(a.v + at);
-      pos[u] = a.positions[from_unit + src[u]];
-      w[u] = a.weights[from_unit + src[u]];
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u * GROUPS < end) {
-        const size_t row = to_unit + dst[u];
-        store16(a.to_k + row * ROW + lane * 16, k[u]);
-        store16(a.to_v + row * ROW + lane * 16, v[u]);
-        if (lane == 0) {
-          a.to_positions[row] = pos[u];
-          a.to_weights[row] = w[u];
-        }
-      }
+  int src, dst;
+  if (a.source) {
+    dst = i;
+    src = a.source[(size_t)unit * a.n_keep + i];
+    if (src < 0) src = movers[-1 - src];
+  } else {
+    dst = a.hole[(size_t)unit * a.moves + i];
+    src = movers[i];
+  }
+  const size_t from = (size_t)unit * a.capacity + src, to = (size_t)unit * a.to_capacity + dst;
+  const uint4 k = load16_stream(a.k + from * ROW + lane * 16), v = load16_stream(a.v + from * ROW + lane * 16);
+  store16(a.to_k + to * ROW + lane * 16, k);
+  store16(a.to_v + to * ROW + lane * 16, v);
+  if (lane == 0) {
+    a.to_positions[to] = a.positions[from];
+    a.to_weights[to] = a.weights[from];
   }
 }
 
@@ -726,6 +721,12 @@ CacheEvictGeom cache_evict_geometry(const wave_cache& c, int n_keep) {
   return g;
 }
 
+template <int ROW>
+static void launch_evict_move(const EvictArgs& a, int units, int rows, hipStream_t st) {
+  const int chunks = rows > 0 ? (rows + kMoveRows<ROW> - 1) / kMoveRows<ROW> : 1;  // (one writes the lengths)
+  WAVE_LAUNCH("evict_move", evict_move_kernel<ROW>, units * chunks, 256, 0, st, a, chunks);
+}
+
 template <int PER>
 static void launch_evict_select(const EvictArgs& a, int units, hipStream_t st) {
   WAVE_LAUNCH("evict_select", evict_select_kernel<PER>, units, EVICT_THREADS, 0, st, a);
@@ -766,8 +767,8 @@ wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int
   a.slices = g.slices;
   a.keep_slices = g.keep_slices;
   const int units = from.B * from.Hkv, rows = a.source ? a.n_keep : g.moves;
-  const int chunks = rows > 0 ? (rows + MOVE_ROWS - 1) / MOVE_ROWS : 1;
-  if ((long long)units * chunks >= (1ll << 24) || (long long)units * g.slices >= (1ll << 22)) return WAVE_ERR_SHAPE;
+  if ((long long)units * ((long long)rows / 8 + 1) >= (1ll << 24) || (long long)units * g.slices >= (1ll << 22))
+    return WAVE_ERR_SHAPE;
   if (g.slices > 0) {
     const int grid = units * g.slices;
     WAVE_LAUNCH("evict_slice", evict_slice_kernel<0>, grid, EVICT_THREADS, 0, st, a);
@@ -783,9 +784,9 @@ wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int
     else launch_evict_select<16>(a, units, st);
   }
   switch (from.d * (from.dtype == WAVE_BF16 ? 2 : 4)) {
-    case 128: WAVE_LAUNCH("evict_move", evict_move_kernel<128>, units * chunks, 256, 0, st, a, chunks); break;
-    case 256: WAVE_LAUNCH("evict_move", evict_move_kernel<256>, units * chunks, 256, 0, st, a, chunks); break;
-    default: WAVE_LAUNCH("evict_move", evict_move_kernel<512>, units * chunks, 256, 0, st, a, chunks); break;
+    case 128: launch_evict_move<128>(a, units, rows, st); break;
+    case 256: launch_evict_move<256>(a, units, rows, st); break;
+    default: launch_evict_move<512>(a, units, rows, st); break;
   }
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }
