@@ -412,8 +412,12 @@ wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const 
  *   workspace     DEVICE, 256-byte aligned, >= wave_cache_attention_workspace(...)
  * A sequence with neither prefix nor own rows has out = 0 and lse = -infinity.
  * Scores are exact products of the stored values, summed in fp32; the softmax and
- * all sums are fp32.  For bf16 caches a softmax weight meets the values as two
- * bf16 numbers that together hold 16 of its bits. */
+ * all sums are fp32.  For bf16 caches a softmax weight meets the values as three
+ * bf16 numbers that hold all its bits; behind a prefix of 16384 rows or more
+ * that more than 64 query rows per KV head (B * Hq / Hkv) share, the prefix's
+ * weights as two, which hold 17 (a weight is then off by at most 2^-17 of itself).
+ * A value that is infinite or no number makes its channel of every head that
+ * attends to its row one or the other. */
 size_t wave_cache_attention_workspace(const wave_cache *cache, int Hq, int P, int accumulate);
 wave_status wave_cache_attention_decode(const void *q, int Hq, const wave_cache *cache,
                                         const void *prefix_k, const void *prefix_v, int P, float decay,

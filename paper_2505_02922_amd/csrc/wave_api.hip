@@ -632,7 +632,9 @@ static wave_status check_cache_attention(const wave_cache* cache, int Hq, int P)
   if (st != WAVE_OK) return st;
   if (P < 0) return WAVE_ERR_ARG;
   if (Hq < cache->Hkv || Hq % cache->Hkv != 0 || Hq / cache->Hkv > 8 || P > (1 << 30)) return WAVE_ERR_SHAPE;
-  if ((long long)cache->B * cache->Hkv * (((long long)cache->capacity + 1023) / 1024) >= kMaxGrid) return WAVE_ERR_SHAPE;
+  // (the joining: a workgroup for each head and for each 1024 rows)
+  const long long chunks = ((long long)cache->capacity + 1023) / 1024;
+  if ((long long)cache->B * Hq + (long long)cache->B * cache->Hkv * chunks >= kMaxGrid) return WAVE_ERR_SHAPE;
   return WAVE_OK;
 }
 

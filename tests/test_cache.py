@@ -130,7 +130,7 @@ def test_attention_refuses():
     assert need > L.wave_cache_attention_workspace(ctypes.byref(c), 4, 100, 0) > 0 and need % 256 == 0
     assert need > L.wave_cache_attention_workspace(ctypes.byref(c), 4, 0, 1)
     for Hq, P in ((3, 0), (1, 0), (18, 0), (4, -1), (4, (1 << 30) + 1)):
-        assert L.wave_cache_attention_workspace(ctypes.byref(c), Hq, P, 0) == 0
+        assert L.wave_cache_attention_workspace(ctypes.byref(c), Hq, P, 0) == 0, (Hq, P)
     q, pk, pv, wo_, out, lse, ws = (0x4000000 + i * 0x100000 for i in range(7))
 
     def call(c=c, q=q, Hq=4, pk=pk, pv=pv, P=100, decay=1.0, wout=wo_, out=out, lse=lse, ws=ws, nbytes=need):

@@ -5,8 +5,10 @@ Tolerances count roundings (u = 2^-24 for fp32, half a step):
            step), the two products and their sum by 3 u more, of the pair's length: 8 u of it; then half a step of the type
   scores   a sum of d products in fp32: (d + 2) u of the sum of the products' magnitudes (delta below)
   weights  of a row: the exponential of that, 2 delta + 8 u
-  output   sum of p |v| times: 2 delta, 2^-18 for a weight in two bf16 numbers (bf16 only), n u for the sums of n terms,
-           16 u for the joining; and, as the errors of different rows have no sign in common, 1e-5 of the norm
+  output   sum of p |v| times: 2 delta, 2^-17 for a weight in two bf16 numbers (the nearest, at most half a step of 2^-7 off
+           in 1 .. 2, and the nearest to that rest, at most half a step of 2^-16 off; bf16 and long shared prefixes only),
+           n u for the sums of n terms, 16 u for the joining; and, as the errors of different rows have no sign in common,
+           1e-5 of the norm
 """
 import math
 
@@ -197,6 +199,7 @@ def _check_attention(dtype, q, cache, lengths, pk, pv, decay, old, out, lse, w, 
     B, Hq, d = q.shape
     Hkv, cap = cache.Hkv, cache.capacity
     G, P = Hq // Hkv, 0 if pk is None else pk.shape[1]
+    two_numbers = dtype == "bf16" and P >= 16384 and B * G > 64
     qn, K, V = q.double().cpu().numpy(), cache.k.double().cpu().numpy(), cache.v.double().cpu().numpy()
     pkn, pvn = (None, None) if pk is None else (pk.double().cpu().numpy(), pv.double().cpu().numpy())
     out, lse, oldn = out.double().cpu().numpy(), lse.double().cpu().numpy(), old.double().cpu().numpy()
@@ -218,7 +221,7 @@ def _check_attention(dtype, q, cache, lengths, pk, pv, decay, old, out, lse, w, 
                 mags = np.abs(rows) @ np.abs(qg[g]) / math.sqrt(d)
                 p = np.exp(rows @ qg[g] / math.sqrt(d) - l[g])
                 delta = (d + 2) * U * mags
-                bar = p @ (np.abs(vals) * (2 * delta[:, None] + (2.0 ** -18 if dtype == "bf16" else 0.0) + (len(p) + 16) * U)) \
+                bar = p @ (np.abs(vals) * (2 * delta[:, None] + (2.0 ** -17 if two_numbers else 0.0) + (len(p) + 16) * U)) \
                     + np.abs(o[g]) * (p @ (2 * delta) + 8 * U)
                 assert np.all(np.abs(go - o[g]) <= bar + 1e-30), (tag, b, h, g, float(np.abs(go - o[g]).max()))
                 assert abs(gl - l[g]) <= p @ delta + (len(p) + 16) * U + 4 * U * abs(l[g]), (tag, b, h, g, gl, l[g])
@@ -287,6 +290,32 @@ def test_attention_long(dtype):
         _check_attention(dtype, q, cache, lengths, pk, pv, 1.0, cache.weights, out, lse, w, f"peak {peak}")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,P", [(20, 16384), (17, 16383), (40, 16501)])
+def test_attention_long_prefix_of_many_query_rows(d, B, P):
+    """On both sides of the line from which the prefix's weights are two numbers; a last tile with waves that have no column."""
+    lengths = [b % 5 for b in range(B)]
+    cache, q, pk, pv = _inputs("bf16", B, 4, 1, d, 8, lengths, P, P, 3.0)
+    w = torch.zeros_like(cache.weights)
+    out, lse = wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w)
+    _check_attention("bf16", q, cache, lengths, pk, pv, 1.0, cache.weights, out, lse, w, f"P {P}")
+
+
+@pytest.mark.parametrize("B", [2, 8, 20])
+def test_attention_values_that_are_not_finite_show_in_their_channel(B):
+    """An infinite value in the last prefix row, and in the last own row: its channel is not finite (a weight is a sum of bf16
+    numbers of which some may be zero or negative, so infinity times it may be no number: never a finite one), the others are
+    as without it, although the rows that fill up the last step are copies of the last row; 8, 32 and 80 query rows."""
+    cache, q, pk, pv = _inputs("bf16", B, 4, 1, 128, 8, [5] * B, 77, 3, 0.5)
+    good, _ = wb.wave_cache_attention_decode(q, cache, pk, pv)
+    pv[0, 76, 5] = math.inf
+    cache.v[0, 0, 4, 9] = -math.inf
+    out, _ = wb.wave_cache_attention_decode(q, cache, pk, pv)
+    assert not torch.isfinite(out[..., 5]).any() and not torch.isfinite(out[0, :, 9]).any()
+    keep = [c for c in range(128) if c not in (5, 9)]
+    assert _same_bits(out[..., keep], good[..., keep]) and _same_bits(out[1:, :, 9], good[1:, :, 9])
+
+
 def test_attention_without_rows_anywhere():
     cache, q, _, _ = _inputs("bf16", 3, 4, 2, 128, 16, [0, 0, 0], 0, 5)
     w = torch.full_like(cache.weights, 2.0)
@@ -345,6 +374,29 @@ def test_attention_equals_full_attention_decode():
                                  torch.full((1,), 600, dtype=torch.int32, device="cuda"), None)
     o3, l3 = wb.wave_cache_attention_decode(q[:1], half, K[0, :, :400].contiguous(), V[0, :, :400].contiguous())
     assert float((o1[:1] - o3).abs().max()) < 2e-5 and float((l1[:1] - l3).abs().max()) < 2e-5
+
+
+def test_prefix_through_its_index_and_own_rows_join_by_their_normalisers():
+    """Keys of a shared prompt rotated in place, indexed, attended with every cluster retrieved, and joined with the own rows'
+    attention by log-sum-exp: the same as the prefix and the own rows in one call."""
+    g = _gen(71)
+    P, B, Hq, Hkv, d = 1100, 1, 8, 2, 128
+    rot = wb.wave_rotary_plan(d, 500000.0, [24, 20, 20], wb.WAVE_ROTARY_TURNS)
+    K, V = (torch.randn(B, Hkv, P, d, generator=g).bfloat16().cuda() for _ in range(2))
+    at = torch.arange(P, dtype=torch.int32).expand(3, B, P).contiguous().cuda()
+    wb.wave_rotary_apply(K, at, rot, out=K)
+    ix = wb.wave_index_build(K, V, 4, 64, 512, 32, 3, 0)
+    cache = wb.alloc_cache(torch.bfloat16, B, Hkv, d, 64)
+    k, v = (torch.randn(B, Hkv, 33, d, generator=g).bfloat16().cuda() for _ in range(2))
+    q = torch.randn(B, Hq, 33, d, generator=g).bfloat16().cuda()
+    cache.tokens.fill_(P)                                              # the conversation goes on behind the prompt
+    qr = wb.wave_cache_append(cache, k, v, q=q, rotary=rot)[:, :, 32].contiguous()
+    o1, l1, _ = wb.wave_attention_decode(qr, ix, ix.m)
+    o2, l2 = wb.wave_cache_attention_decode(qr, cache)
+    both = torch.logaddexp(l1, l2)
+    joined = o1 * torch.exp(l1 - both)[..., None] + o2 * torch.exp(l2 - both)[..., None]
+    o3, l3 = wb.wave_cache_attention_decode(qr, cache, K[0], V[0])
+    assert float((joined - o3).abs().max()) < 2e-5 and float((both - l3).abs().max()) < 2e-5
 
 
 # --------------------------------------------------------------------------- eviction
