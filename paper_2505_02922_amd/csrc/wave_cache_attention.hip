@@ -117,8 +117,7 @@ struct Step<bf16_t, D> {
     return r;
   }
   // TERMS 3: a weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the
-  // product with the values loses nothing.  TERMS 2: the nearest bf16 number and the nearest to what that left, 17 bits:
-  // outputs are then off by 2e-6 of their norm.
+  // product with the values loses nothing.  TERMS 2: the nearest bf16 number and the nearest to what that left: 17 bits.
   template <int TERMS>
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
     bf16x8 w[TERMS];
@@ -794,8 +793,10 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
 }
 
 // From this many prefix rows on, and with more query rows than make the prefix a matter of memory, weights are two numbers
-// instead of three: the matrix units are the bound, and a sum over so many rows in fp32 throughout is off by as much.
-constexpr int TWO_TERMS_ROWS = 16384;
+// instead of three: a third fewer products where they are the bound (64K rows, 448 query rows, 160K own rows: 174 -> 157 us).  Outputs are
+// then off by 2.2e-6 of their norm, as an evaluation in fp32 throughout is over so many rows (2.3e-6 at 32K rows, 2.6e-6 at
+// 64K, but 1.6e-6 at 16K; with three numbers 0.8e-6).
+constexpr int TWO_TERMS_ROWS = 32768;
 
 template <typename T, int D>
 wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {

@@ -199,7 +199,7 @@ def _check_attention(dtype, q, cache, lengths, pk, pv, decay, old, out, lse, w, 
     B, Hq, d = q.shape
     Hkv, cap = cache.Hkv, cache.capacity
     G, P = Hq // Hkv, 0 if pk is None else pk.shape[1]
-    two_numbers = dtype == "bf16" and P >= 16384 and B * G > 64
+    two_numbers = dtype == "bf16" and P >= 32768 and B * G > 64
     qn, K, V = q.double().cpu().numpy(), cache.k.double().cpu().numpy(), cache.v.double().cpu().numpy()
     pkn, pvn = (None, None) if pk is None else (pk.double().cpu().numpy(), pv.double().cpu().numpy())
     out, lse, oldn = out.double().cpu().numpy(), lse.double().cpu().numpy(), old.double().cpu().numpy()
@@ -291,7 +291,7 @@ def test_attention_long(dtype):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("B,P", [(20, 16384), (17, 16383), (40, 16501)])
+@pytest.mark.parametrize("B,P", [(20, 32768), (17, 32767), (40, 33001)])
 def test_attention_long_prefix_of_many_query_rows(d, B, P):
     """On both sides of the line from which the prefix's weights are two numbers; a last tile with waves that have no column."""
     lengths = [b % 5 for b in range(B)]
