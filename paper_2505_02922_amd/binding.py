@@ -430,10 +430,7 @@ def _require(ok: bool, status: int, where: str) -> None:
 
 def _together(where: str, index: int, *tensors: Optional[torch.Tensor]) -> None:
     """Every tensor on GPU `index` (a kernel would fault on memory that is elsewhere)."""
-    for t in tensors:
-        if t is not None and t.get_device() != index:
-            raise WaveError(1, where)
-    if index < 0:
+    if index < 0 or any([t.get_device() != index for t in tensors if t is not None]):
         raise WaveError(1, where)
 
 
@@ -562,33 +559,50 @@ def wave_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, q: Optiona
     behind each sequence's rows and advances lengths and tokens, in place unless other tensors are given.
     Returns q rotated (q_out, which may be q)."""
     where = "wave_cache_append"
-    B, d, dtype = cache.B, cache.d, cache.dtype
+    B, d, dtype, own = cache.B, cache.d, cache.dtype, cache.t
     shape = k.shape
-    _require(len(shape) == 4 and shape[0] == B and shape[1] == cache.Hkv and shape[3] == d and v.shape == shape, 2, where)
-    _require(k.dtype == dtype and v.dtype == dtype, 3, where)
+    if len(shape) != 4 or shape[0] != B or shape[1] != cache.Hkv or shape[3] != d or v.shape != shape:
+        raise WaveError(2, where)
+    if k.dtype != dtype or v.dtype != dtype:
+        raise WaveError(3, where)
     n, Hq = shape[2], 0
     if q is not None:
-        _require(q.dim() == 4 and q.shape[0] == B and q.shape[2:] == (n, d), 2, where)
-        _require(q.dtype == dtype, 3, where)
-        Hq = q.shape[1]
+        heads = q.shape
+        if len(heads) != 4 or heads[0] != B or heads[2] != n or heads[3] != d:
+            raise WaveError(2, where)
+        if q.dtype != dtype:
+            raise WaveError(3, where)
+        Hq = heads[1]
         if q_out is None:
             new = torch.empty if counts is None else torch.zeros
-            q_out = new(q.shape, dtype=dtype, device=q.device)
-        _as_is(where, q_out, dtype, q.shape)
+            q_out = new(heads, dtype=dtype, device=q.device)
+        else:
+            _as_is(where, q_out, dtype, heads)
         q = q.contiguous()
     else:
         q_out = None
     if coords is not None:
-        _require(coords.dtype == torch.int32, 3, where)
-        _require(rotary is not None, 1, where)
-        _require(coords.shape == (rotary.n_axes, B, n), 2, where)
+        if coords.dtype != torch.int32:
+            raise WaveError(3, where)
+        if rotary is None:
+            raise WaveError(1, where)
+        if coords.shape != (rotary.n_axes, B, n):
+            raise WaveError(2, where)
         coords = coords.contiguous()
     if counts is not None:
-        _require(counts.dtype == torch.int32, 3, where)
-        _require(counts.shape == (B,), 2, where)
+        if counts.dtype != torch.int32:
+            raise WaveError(3, where)
+        if counts.shape != (B,):
+            raise WaveError(2, where)
         counts = counts.contiguous()
-    lengths_out = cache.t["lengths"] if lengths_out is None else _as_is(where, lengths_out, torch.int32, (B,))
-    tokens_out = cache.t["tokens"] if tokens_out is None else _as_is(where, tokens_out, torch.int32, (B,))
+    if lengths_out is None:
+        lengths_out = own["lengths"]
+    else:
+        _as_is(where, lengths_out, torch.int32, (B,))
+    if tokens_out is None:
+        tokens_out = own["tokens"]
+    else:
+        _as_is(where, tokens_out, torch.int32, (B,))
     _together(where, cache.index, k, v, q, q_out, coords, counts, lengths_out, tokens_out)
     k, v = k.contiguous(), v.contiguous()
     _enqueue(where, cache.index, cache.ref, k.data_ptr(), v.data_ptr(), _address(q), Hq, n, _address(counts),
