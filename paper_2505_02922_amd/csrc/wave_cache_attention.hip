@@ -3,10 +3,7 @@
 // Both parts are the same stream: a wave holds a tile of query rows as the columns of its matrix products and goes
 // through key and value rows with a running maximum and sum of the softmax.  What a lane holds of S = K Q^T is, with the
 // contraction index permuted alike on both sides, already the operand of O^T += V^T P^T: no value crosses a lane between
-// the two products.  Rows come through LDS, in whole lines and without passing through registers: an operand takes sixteen
-// rows side by side, 64 bytes of each, which straight from memory asks for every line twice and keeps rows that are read
-// once from passing by the caches (1.12 GB of own rows: 235 us straight from memory, 209 us = 5.5 TB/s so, the rate of a plain
-// read of 1 GiB).
+// the two products.
 #include <type_traits>
 
 #include "wave_common.h"
@@ -33,30 +30,45 @@ __device__ __forceinline__ uint32_t nearest_pair(float x, float y) {
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xff800000u); }
 
 // ----------------------------------------------------------------------------
-// Rows into LDS.  A step's rows lie there one behind the other, each with its 16-byte chunks in an order of its own: chunk
-// x of row r at x ^ place(r), so that the lanes of an operand read hit all banks.  Rows behind the last are the last again.
-// A lane's address is a base that the wave shares and 32 bits of its own.
+// A step: KEYS key and value rows against 16 query columns a tile.  Lane = 16 * g + c: column c of every product, and of
+// a product's rows g * 4 .. g * 4 + 3.
 // ----------------------------------------------------------------------------
+template <typename T, int D>
+struct Step;
+
+// Where key rows have their chunks in LDS: the sixteen lanes of an operand read, which take one chunk of sixteen rows, hit
+// all banks.
+template <int ROW>
+__device__ __forceinline__ constexpr int key_place(int r) {
+  return ROW >= 256 ? r & 15 : (r >> 1) & 7;
+}
+// A step of a stream: its first row and how many rows there are behind that one, at least; rows behind the last are the last
+// again.  A lane's address is a base that the wave shares and 32 bits of its own.
 struct StepRows {
   const char* base;
-  int rest;  // rows behind the first, at most
+  int rest;
 };
 template <int ROW>
 __device__ __forceinline__ StepRows step_rows(const char* base, int k0, int last) {
   const int row = min(k0, last);
   return StepRows{base + (size_t)row * ROW, last - row};
 }
-// Pieces first .. first + COUNT - 1 of 1 KiB, one load instruction of a wave each, in the order of its lanes.  ONCE: nobody
-// else reads these rows, they pass by the caches (policy 2).
+template <int ROW>
+__device__ __forceinline__ const char* row_at(const StepRows& s, int r, int byte) {
+  return s.base + (uint32_t)(min(r, s.rest) * ROW + byte);
+}
+// Pieces first .. first + COUNT - 1 of 1 KiB of a step's rows into LDS, one load instruction of a wave each, in the order of
+// its lanes: chunk x (16 bytes) of row r lies at x ^ place(r).  ONCE: nobody else reads these rows, they pass by the caches
+// (policy 2).
 template <int ROW, int COUNT, bool ONCE, typename Place>
 __device__ __forceinline__ void rows_to_lds(char* lds, const StepRows& s, int first, int lane, Place&& place) {
   constexpr int CHUNKS = ROW / 16;
 #pragma unroll
   for (int i = 0; i < COUNT; ++i) {
-    const int r = (first + i) * (1024 / ROW) + lane / CHUNKS, x = lane % CHUNKS ^ place(r);
-    const char* from = s.base + (uint32_t)(min(r, s.rest) * ROW + x * 16);
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)(lds + (first + i) * 1024), 16, 0, ONCE ? 2 : 0);
+    const int r = (first + i) * (1024 / ROW) + lane / CHUNKS;
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)row_at<ROW>(s, r, (lane % CHUNKS ^ place(r)) * 16),
+        (__attribute__((address_space(3))) void*)(lds + (first + i) * 1024), 16, 0, ONCE ? 2 : 0);
   }
 }
 __device__ __forceinline__ void wait_for_reads() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // of LDS (lgkmcnt 0)
@@ -66,26 +78,18 @@ __device__ __forceinline__ void wait_for_loads() {  // until at most the newest 
   __builtin_amdgcn_s_waitcnt(0x0f70 | N);
 }
 
-// ----------------------------------------------------------------------------
-// A step: KEYS key and value rows against 16 query columns a tile.  Lane = 16 * g + c: column c of every product, and of
-// a product's rows g * 4 .. g * 4 + 3.
-// ----------------------------------------------------------------------------
-template <typename T, int D>
-struct Step;
-
-// bf16: v_mfma_f32_16x16x32_bf16.  S has two tiles of 16 keys; a lane has the keys t * 16 + g * 4 + i of its column, and the
-// contraction of the second product takes them in the order t * 4 + i.  The value operand, four rows of a channel a lane,
-// comes transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen channels, each gets its channel's four).
+// bf16: v_mfma_f32_16x16x32_bf16.  S has two tiles of 16 keys; a lane has the keys t * 16 + g * 4 + i of its column.  The
+// contraction of the second product takes them in the order t * 4 + i, so a lane reads CH neighbouring channels of those
+// eight value rows (16 lanes: a whole row) and pairs up the rows of each channel with v_perm.
 template <int D>
 struct Step<bf16_t, D> {
-  static constexpr int ROW = D * 2, KEYS = 32, NS = 8, KC = D / 32, ACC = D / 16, BYTES = KEYS * ROW, LOADS = BYTES / 1024;
+  static constexpr int KEYS = 32, NS = 8, KC = D / 32, CH = D / 16, ACC = CH, VLOADS = 8, ROW = D * 2, KLOADS = KEYS * ROW / 1024;
   struct Q { bf16x8 x[KC]; };
   struct K { uint4 x[2][KC]; };
-  struct V { bf16x8 x[ACC]; };  // sixteen channels each
+  struct V { uint32_t x[8][CH / 2]; };
   static __device__ __forceinline__ int key(int g, int s) { return (s >> 2) * 16 + g * 4 + (s & 3); }
-  // one chunk of sixteen key rows, two neighbouring chunks of eight value rows
-  static __device__ __forceinline__ int key_place(int r) { return ROW == 256 ? r & 15 : (r >> 1) & 7; }
-  static __device__ __forceinline__ int value_place(int r) { return ROW == 256 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+  // channel of value i of accumulator a; a lane's are contiguous in (i, a)
+  static __device__ __forceinline__ int channel(int g, int a, int i) { return (g * 4 + i) * CH + a; }
 
   static __device__ __forceinline__ Q load_q(const char* row, int g) {
     Q q;
@@ -93,27 +97,29 @@ struct Step<bf16_t, D> {
     for (int s = 0; s < KC; ++s) q.x[s] = __builtin_bit_cast(bf16x8, load16(row + (s * 32 + g * 8) * 2));
     return q;
   }
+  // from a step's key rows in LDS
   static __device__ __forceinline__ K read_k(const char* lds, int g, int c) {
     K k;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int s = 0; s < KC; ++s) k.x[t][s] = load16(lds + (t * 16 + c) * ROW + ((s * 4 + g) ^ key_place(c)) * 16);
+      for (int s = 0; s < KC; ++s)
+        k.x[t][s] = load16(lds + (t * 16 + c) * (D * 2) + ((s * 4 + g) ^ key_place<D * 2>(c)) * 16);
     return k;
   }
-  static __device__ __forceinline__ V read_v(const char* lds, int g, int c) {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    const int r = g * 4 + (c >> 2);
+  template <bool ONCE>
+  static __device__ __forceinline__ V load_v(const StepRows& rows, int g, int c) {
     V v;
 #pragma unroll
-    for (int x = 0; x < ACC; ++x) {
-      const char* at = lds + r * ROW + ((x * 2 + ((c & 3) >> 1)) ^ value_place(r)) * 16 + (c & 1) * 8;
-      uint2 u[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        u[t] = __builtin_bit_cast(
-            uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + t * 16 * ROW)));
-      v.x[x] = __builtin_bit_cast(bf16x8, make_uint4(u[0].x, u[0].y, u[1].x, u[1].y));
+    for (int j = 0; j < 8; ++j) {
+      const char* at = row_at<ROW>(rows, key(g, j), c * (CH * 2));
+      if constexpr (CH == 8) {
+        const uint4 u = ONCE ? load16_stream(at) : load16(at);
+        v.x[j][0] = u.x; v.x[j][1] = u.y; v.x[j][2] = u.z; v.x[j][3] = u.w;
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(at);
+        v.x[j][0] = u.x; v.x[j][1] = u.y;
+      }
     }
     return v;
   }
@@ -122,7 +128,7 @@ struct Step<bf16_t, D> {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int x = 0; x < ACC; ++x) v.x[x][j] = key(g, j) > rest ? (__bf16)0.f : v.x[x][j];
+      for (int u = 0; u < CH / 2; ++u) v.x[j][u] = key(g, j) > rest ? 0u : v.x[j][u];
   }
   static __device__ __forceinline__ void scores(const K& k, const Q& q, float (&s)[NS]) {
 #pragma unroll
@@ -135,10 +141,26 @@ struct Step<bf16_t, D> {
       for (int i = 0; i < 4; ++i) s[t * 4 + i] = a[i];
     }
   }
+  // V^T as the left operand, channel a of every lane's chunk
+  struct Vt { bf16x8 x[CH]; };
+  static __device__ __forceinline__ Vt transpose(const V& v) {
+    Vt r;
+#pragma unroll
+    for (int a = 0; a < CH; ++a) {
+      const uint32_t sel = (a & 1) ? 0x07060302u : 0x05040100u;
+      uint4 u;
+      u.x = __builtin_amdgcn_perm(v.x[1][a / 2], v.x[0][a / 2], sel);
+      u.y = __builtin_amdgcn_perm(v.x[3][a / 2], v.x[2][a / 2], sel);
+      u.z = __builtin_amdgcn_perm(v.x[5][a / 2], v.x[4][a / 2], sel);
+      u.w = __builtin_amdgcn_perm(v.x[7][a / 2], v.x[6][a / 2], sel);
+      r.x[a] = __builtin_bit_cast(bf16x8, u);
+    }
+    return r;
+  }
   // TERMS 3: a weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the
   // product with the values loses nothing.  TERMS 2: the nearest bf16 number and the nearest to what that left: 17 bits.
   template <int TERMS>
-  static __device__ __forceinline__ void accumulate(const V& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
+  static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
     bf16x8 w[TERMS];
     if constexpr (TERMS == 3) {
       uint32_t u[3][4];
@@ -168,7 +190,7 @@ struct Step<bf16_t, D> {
 #pragma unroll
     for (int n = TERMS - 1; n >= 0; --n)
 #pragma unroll
-      for (int a = 0; a < ACC; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], w[n], o[a], 0, 0, 0);
+      for (int a = 0; a < CH; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], w[n], o[a], 0, 0, 0);
   }
 };
 
@@ -176,15 +198,18 @@ struct Step<bf16_t, D> {
 // contraction takes key g * 4 + i from lane group g.
 template <int D>
 struct Step<float, D> {
-  static constexpr int ROW = D * 4, KEYS = 16, NS = 4, KC = D / 16, CV = D / 64, ACC = D / 16, BYTES = KEYS * ROW,
-                       LOADS = BYTES / 1024;
+  static constexpr int KEYS = 16, NS = 4, KC = D / 16, CV = D / 64, ACC = D / 16, VLOADS = 4 * CV, ROW = D * 4,
+                       KLOADS = KEYS * ROW / 1024;
   struct Q { f32x4 x[KC]; };
   struct K { f32x4 x[KC]; };
   struct V { f32x4 x[4][CV]; };
+  typedef V Vt;
   static __device__ __forceinline__ int key(int g, int s) { return g * 4 + s; }
-  static __device__ __forceinline__ int key_place(int r) { return r & 15; }
-  static __device__ __forceinline__ int value_place(int r) { return 0; }  // (an instruction reads whole rows)
+  static __device__ __forceinline__ int channel(int g, int a, int i) { return (a >> 2) * 64 + (g * 4 + i) * 4 + (a & 3); }
   static __device__ __forceinline__ f32x4 load(const char* p) { return *reinterpret_cast<const f32x4*>(p); }
+  static __device__ __forceinline__ f32x4 load_once(const char* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+  }
 
   static __device__ __forceinline__ Q load_q(const char* row, int g) {
     Q q;
@@ -195,15 +220,19 @@ struct Step<float, D> {
   static __device__ __forceinline__ K read_k(const char* lds, int g, int c) {
     K k;
 #pragma unroll
-    for (int s = 0; s < KC; ++s) k.x[s] = load(lds + c * ROW + ((s * 4 + g) ^ key_place(c)) * 16);
+    for (int s = 0; s < KC; ++s) k.x[s] = load(lds + c * (D * 4) + ((s * 4 + g) ^ key_place<D * 4>(c)) * 16);
     return k;
   }
-  static __device__ __forceinline__ V read_v(const char* lds, int g, int c) {
+  template <bool ONCE>
+  static __device__ __forceinline__ V load_v(const StepRows& rows, int g, int c) {
     V v;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int u = 0; u < CV; ++u) v.x[i][u] = load(lds + (g * 4 + i) * ROW + (u * 16 + c) * 16);
+      for (int u = 0; u < CV; ++u) {
+        const char* at = row_at<ROW>(rows, key(g, i), (u * 64 + c * 4) * 4);
+        v.x[i][u] = ONCE ? load_once(at) : load(at);
+      }
     return v;
   }
   static __device__ __forceinline__ void mask_v(V& v, int rest, int g) {
@@ -226,8 +255,9 @@ struct Step<float, D> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = (a[0][i] + a[1][i]) + (a[2][i] + a[3][i]);
   }
+  static __device__ __forceinline__ Vt transpose(const V& v) { return v; }
   template <int>
-  static __device__ __forceinline__ void accumulate(const V& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
+  static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -237,21 +267,6 @@ struct Step<float, D> {
           o[u * 4 + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x[i][u][j], p[i], o[u * 4 + j], 0, 0, 0);
   }
 };
-
-// A lane's accumulators of its column to memory: groups of four neighbouring channels.
-template <int D>
-__device__ __forceinline__ void store_column(const f32x4 (&o)[D / 16], bf16_t, float* at, int g) {
-#pragma unroll
-  for (int a = 0; a < D / 16; ++a) *reinterpret_cast<f32x4*>(at + a * 16 + g * 4) = o[a];
-}
-template <int D>
-__device__ __forceinline__ void store_column(const f32x4 (&o)[D / 16], float, float* at, int g) {
-#pragma unroll
-  for (int u = 0; u < D / 64; ++u)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(at + u * 64 + (g * 4 + i) * 4) = f32x4{o[u * 4][i], o[u * 4 + 1][i], o[u * 4 + 2][i], o[u * 4 + 3][i]};
-}
 
 // The softmax state of a tile of 16 query columns.
 template <typename T, int D>
@@ -299,31 +314,33 @@ struct State {
 
 // ----------------------------------------------------------------------------
 // The stream of one wave: the rows k0, k0 + stride, .. below `end` against a tile of query columns.  z: where a lane leaves
-// the products of its column (NULL: nowhere).  lds: the wave's own place for a step's rows, S::BYTES of keys and as many of
-// values.  The next step's rows are asked for as soon as this one's are in registers, so all but some hundred cycles of a
-// step have 16 KiB a wave on their way.
+// the products of its column (NULL: nowhere).  ONCE: nobody else reads these rows, so they pass by the caches.  lds: the
+// wave's own place for a step's key rows.  Keys go through it because an operand has sixteen rows side by side, 64 bytes of
+// each in a load: straight from memory every line is asked for twice, and must stay in the caches between.  A load of the
+// values takes whole rows.  1.12 GB of own rows: 235 us with both straight from memory, 222 with the values passing by the
+// caches, 209 us = 5.5 TB/s, what a plain read of 1 GiB reaches, so.  (Values through LDS too: the same alone, but 171
+// instead of 155 us beside a long prefix, which needs LDS itself.)
 // ----------------------------------------------------------------------------
 template <typename T, int D, bool ONCE>
 __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0, int stride, int end, float scale,
                                             const typename Step<T, D>::Q& q, State<T, D>& st, float* z, char* lds, int lane) {
   typedef Step<T, D> S;
+  constexpr int ROW = S::ROW;
   const int last = end - 1, g = lane >> 4, c = lane & 15;
   if (k0 >= end) return;
-  auto fetch = [&](int row) {
-    rows_to_lds<S::ROW, S::LOADS, ONCE>(lds, step_rows<S::ROW>(K, row, last), 0, lane, S::key_place);
-    rows_to_lds<S::ROW, S::LOADS, ONCE>(lds + S::BYTES, step_rows<S::ROW>(V, row, last), 0, lane, S::value_place);
-  };
-  fetch(k0);
-  for (;; k0 += stride) {
-    const bool more = k0 + stride < end;
-    const int rest = last - k0;
+  rows_to_lds<ROW, S::KLOADS, ONCE>(lds, step_rows<ROW>(K, k0, last), 0, lane, key_place<ROW>);
+  __builtin_amdgcn_sched_barrier(0);
+  typename S::V v = S::template load_v<ONCE>(step_rows<ROW>(V, k0, last), g, c);
+  for (;;) {
+    const int next = k0 + stride, rest = last - k0;
     __builtin_amdgcn_sched_barrier(0);
-    wait_for_loads<0>();
+    wait_for_loads<S::VLOADS>();  // the keys are here; the values, asked for after them, may not be
     const typename S::K k = S::read_k(lds, g, c);
-    typename S::V v = S::read_v(lds + S::BYTES, g, c);
-    wait_for_reads();
+    wait_for_reads();  // they are in registers: their place is free
     __builtin_amdgcn_sched_barrier(0);
-    if (more) fetch(k0 + stride);
+    // The next rows' loads go out as soon as there is room: a wave has loads in flight all the time.  They are made behind
+    // the end too, since a wait behind a load that may not have been made waits for all of them.
+    rows_to_lds<ROW, S::KLOADS, ONCE>(lds, step_rows<ROW>(K, next, last), 0, lane, key_place<ROW>);
     __builtin_amdgcn_sched_barrier(0);
     float s[S::NS];
     S::scores(k, q, s);
@@ -337,10 +354,16 @@ __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0
       for (int i = 0; i < S::NS; i += 4)
         *reinterpret_cast<f32x4*>(z + k0 + S::key(g, i)) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
     }
+    const typename S::Vt vt = S::transpose(v);
+    __builtin_amdgcn_sched_barrier(0);
+    v = S::template load_v<ONCE>(step_rows<ROW>(V, next, last), g, c);
+    __builtin_amdgcn_sched_barrier(0);
     st.weigh(s, scale);
-    S::template accumulate<3>(v, s, st.o);
-    if (!more) return;
+    S::template accumulate<3>(vt, s, st.o);
+    if (next >= end) break;
+    k0 = next;
   }
+  wait_for_loads<0>();  // nothing may come into LDS behind this
 }
 
 // What a partial result leaves of its softmax.  A sum that is no number may have no reference, where every score was none:
@@ -360,6 +383,7 @@ struct JoinShared {
 template <typename T, int D>
 __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, JoinShared& js, const Areas areas, int wave,
                                            int g, int c, float2* ml, float* acc) {
+  typedef Step<T, D> S;
   constexpr int PITCH = D + 4;  // floats a column: a column's four groups and neighbouring columns lie on other banks
   float l = st.l;
   l += __shfl_xor(l, 16);
@@ -369,7 +393,15 @@ __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, Join
     js.l[wave][c] = l;
   }
   if (c < cols) {
-    store_column<D>(st.o, T(), reinterpret_cast<float*>(areas.of(wave)) + c * PITCH, g);
+    float* at = reinterpret_cast<float*>(areas.of(wave)) + c * PITCH;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int a = 0; a < S::ACC; a += 4) {
+        // four neighbouring channels
+        const f32x4 x = {st.o[a][i], st.o[a + 1][i], st.o[a + 2][i], st.o[a + 3][i]};
+        *reinterpret_cast<f32x4*>(at + S::channel(g, a, i)) = x;
+      }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < cols * D; i += 256) {
@@ -493,16 +525,31 @@ __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, Join
 
 // Prefix with more query rows than a tile (bf16): four waves with MQ tiles of columns each go through the same rows, which
 // they share in LDS.  A step is 32 rows; a ring of four steps holds the one that is worked on and the next, while two more
-// are on their way.
+// are on their way.  The values' operand comes transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen
+// channels, and each gets the four values of its channel; a read takes two neighbouring chunks of eight rows).
 // The scores of the next step are formed beside the softmax of this one, so that matrix and vector work of a wave do not
 // wait for each other.  Measured (64K rows, 448 query rows per KV head, 60 GFLOP): 130 us.  The card lowers its clock to
 // 1.7 .. 1.8 GHz under this mixture (2.5 GHz in the own rows), and the time follows the work itself: sixteen products fewer a
 // step 24 us, no loads into LDS 14 us, no exponentials 7 us, no LDS reads of the keys or of the values 4 us each, while other
 // orders of the same instructions, a third fewer vector instructions, or two workgroups a CU instead of one change nothing.
+template <int D>
+struct SharedStep {
+  static constexpr int ROWS = 32, ROW = D * 2, CHUNKS = ROW / 16, HALF = ROWS * ROW, BYTES = 2 * HALF;  // keys, then values
+  static constexpr int FILLS = HALF / 1024 / 4;  // wave-wide loads of each wave, for each of the two
+  static __device__ __forceinline__ int fv(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+  // a wave's part of the rows r0 .. of K and V
+  static __device__ __forceinline__ void fill(char* lds, const char* K, const char* V, int r0, int last, int wave, int lane) {
+    rows_to_lds<ROW, FILLS, false>(lds, step_rows<ROW>(K, r0, last), wave * FILLS, lane, key_place<ROW>);
+    rows_to_lds<ROW, FILLS, false>(lds + HALF, step_rows<ROW>(V, r0, last), wave * FILLS, lane, fv);
+  }
+};
+
 template <int D, int MQ, int TERMS>
 __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, char* ring0, char* ring1, char* ring2, char* ring3) {
   typedef Step<bf16_t, D> S;
-  constexpr int FILLS = S::LOADS / 4;  // each wave's of the keys and of the values
+  typedef SharedStep<D> L;
+  constexpr int BLOCKS = D / 16;  // of sixteen channels
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
   const int hs = block % (a.Hkv * a.splits), tile = block / (a.Hkv * a.splits);
   const int h = hs % a.Hkv, split = hs / a.Hkv;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
@@ -512,28 +559,54 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 #pragma unroll
   for (int t = 0; t < MQ; ++t) {
     const int m = min(m0 + t * 16 + c, M - 1), b = m / a.G;
-    q[t] = S::load_q(a.q + ((size_t)b * a.Hq + h * a.G + (m - b * a.G)) * S::ROW, g);
+    q[t] = S::load_q(a.q + ((size_t)b * a.Hq + h * a.G + (m - b * a.G)) * L::ROW, g);
     st[t].init();
   }
   const int start = split * a.prefix_rows, end = min(a.P, start + a.prefix_rows), last = end - 1;
-  const char* K = a.prefix_k + (size_t)h * a.P * S::ROW;
-  const char* V = a.prefix_v + (size_t)h * a.P * S::ROW;
-  auto fill = [&](char* ring, int row) {
-    rows_to_lds<S::ROW, FILLS, false>(ring, step_rows<S::ROW>(K, row, last), wave * FILLS, lane, S::key_place);
-    rows_to_lds<S::ROW, FILLS, false>(ring + S::BYTES, step_rows<S::ROW>(V, row, last), wave * FILLS, lane, S::value_place);
+  const char* K = a.prefix_k + (size_t)h * a.P * L::ROW;
+  const char* V = a.prefix_v + (size_t)h * a.P * L::ROW;
+  int ka[S::KC], va[BLOCKS];  // this lane's places in a step, of row c and of row g * 4 + c / 4
+#pragma unroll
+  for (int x = 0; x < S::KC; ++x) ka[x] = c * L::ROW + ((x * 4 + g) ^ key_place<L::ROW>(c)) * 16;
+#pragma unroll
+  for (int x = 0; x < BLOCKS; ++x) {
+    const int r = g * 4 + (c >> 2);
+    va[x] = L::HALF + r * L::ROW + ((x * 2 + ((c & 3) >> 1)) ^ L::fv(r)) * 16 + (c & 1) * 8;
+  }
+  auto read_k = [&](const char* lds) {
+    typename S::K k;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int x = 0; x < S::KC; ++x) k.x[t][x] = load16(lds + ka[x] + t * 16 * L::ROW);
+    return k;
   };
-  // at most the newest `steps` of this wave's loads are on their way still; then all waves are behind the step before
-  auto arrive = [&](auto steps) {
-    wait_for_loads<decltype(steps)::value * 2 * FILLS>();
+  auto read_v = [&](const char* lds) {
+    typename S::Vt v;
+#pragma unroll
+    for (int x = 0; x < BLOCKS; ++x) {
+      uint2 u[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        u[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((
+                                             __attribute__((address_space(3))) s16x4*)(lds + va[x] + t * 16 * L::ROW)));
+      v.x[x] = __builtin_bit_cast(bf16x8, make_uint4(u[0].x, u[0].y, u[1].x, u[1].y));
+    }
+    return v;
+  };
+  // `newest` steps' loads of this wave may be on their way still; then all waves are behind the step before
+  auto arrive = [&](auto newest) {
+    constexpr int N = decltype(newest)::value * 2 * L::FILLS;
+    wait_for_loads<N>();
     __syncthreads();
   };
-  fill(ring0, start);
-  fill(ring1, start + 32);
-  fill(ring2, start + 64);
+  L::fill(ring0, K, V, start, last, wave, lane);
+  L::fill(ring1, K, V, start + 32, last, wave, lane);
+  L::fill(ring2, K, V, start + 64, last, wave, lane);
   arrive(std::integral_constant<int, 2>());
   float s[MQ][S::NS];
   {
-    const typename S::K k = S::read_k(ring0, g, c);
+    const typename S::K k = read_k(ring0);
 #pragma unroll
     for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
   }
@@ -542,12 +615,12 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
   // step n: `now` holds it, `next` the step behind it, `free` the step before it
   auto step = [&](int n, const char* now, const char* next, char* free) {
     arrive(std::integral_constant<int, 1>());
-    fill(free, start + (n + 3) * 32);
+    L::fill(free, K, V, start + (n + 3) * 32, last, wave, lane);
     if (idle) return;
 #pragma unroll
     for (int t = 0; t < MQ; ++t) st[t].follow(s[t], a.scale);
-    const typename S::K k = S::read_k(next, g, c);
-    const typename S::V v = S::read_v(now + S::BYTES, g, c);
+    const typename S::K k = read_k(next);
+    const typename S::Vt v = read_v(now);
     float p[MQ][S::NS];
     st[0].weights(s[0], p[0], a.scale);
     if (MQ > 1) st[MQ - 1].weights(s[MQ - 1], p[MQ - 1], a.scale);
@@ -567,14 +640,19 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
     step(n + 3, ring3, ring0, ring2);
   }
   if (start + full * 32 < end) {
+    // Rows behind the end are the last row again.  Their weight is zero, and zero times a value that is no number must not
+    // show, so the values go too.
     const int k0 = start + full * 32;
     const char* now = (full & 3) == 0 ? ring0 : (full & 3) == 1 ? ring1 : (full & 3) == 2 ? ring2 : ring3;
-    typename S::V v = S::read_v(now + S::BYTES, g, c);
-    S::mask_v(v, last - k0, g);
+    typename S::Vt v = read_v(now);
 #pragma unroll
-    for (int t = 0; t < MQ; ++t)
+    for (int j = 0; j < 8; ++j)
+      if (k0 + S::key(g, j) > last) {
 #pragma unroll
-      for (int i = 0; i < S::NS; ++i) s[t][i] = k0 + S::key(g, i) > last ? neg_inf() : s[t][i];
+        for (int x = 0; x < BLOCKS; ++x) v.x[x][j] = (__bf16)0.f;
+#pragma unroll
+        for (int t = 0; t < MQ; ++t) s[t][j] = neg_inf();
+      }
 #pragma unroll
     for (int t = 0; t < MQ; ++t) {
       st[t].weigh(s[t], a.scale);
@@ -591,7 +669,8 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
     if (m < M) {
       const size_t at = ((size_t)split * a.Hkv + h) * M + m;
       if (g == 0) a.pml[at] = partial_ml(st[t].m, l);
-      store_column<D>(st[t].o, bf16_t(), a.pacc + at * D, g);
+#pragma unroll
+      for (int x = 0; x < BLOCKS; ++x) *reinterpret_cast<f32x4*>(a.pacc + at * D + x * 16 + g * 4) = st[t].o[x];
     }
   }
 }
@@ -620,8 +699,7 @@ __device__ __forceinline__ Role role_of(const AttendArgs& a) {
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a) {
   __shared__ JoinShared js;
-  constexpr int AREA = 2 * Step<T, D>::BYTES > 16 * (D + 4) * 4 ? 2 * Step<T, D>::BYTES : 16 * (D + 4) * 4;
-  __shared__ __attribute__((aligned(1024))) char lds[4][AREA];
+  __shared__ __attribute__((aligned(16))) char lds[4][16 * (D + 4) * 4];
   const Areas areas{lds[0], lds[1], lds[2], lds[3]};
   const Role r = role_of(a);
   if (!r.any) return;
@@ -633,8 +711,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
 
 template <int D, int MQ, int TERMS>
 __global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs a) {
-  constexpr int AREA = 2 * Step<bf16_t, D>::BYTES;
-  static_assert(AREA >= 16 * (D + 4) * 4, "");
+  typedef SharedStep<D> L;
+  constexpr int AREA = L::BYTES > 16 * (D + 4) * 4 ? L::BYTES : 16 * (D + 4) * 4;
   __shared__ JoinShared js;
   __shared__ __attribute__((aligned(1024))) char ring0[AREA], ring1[AREA], ring2[AREA], ring3[AREA];
   const Role r = role_of(a);
