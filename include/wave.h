@@ -345,10 +345,12 @@ wave_status wave_rotary_plan(wave_rotary *rotary, int rot_dim, double base, cons
 /* Rotates x into y.
  *   x, y       DEVICE [B,H,N,d] dtype, 16-byte aligned; y may be x, and must not
  *              overlap it otherwise
- *   coords     DEVICE [n_axes,B,N] int32, any values
+ *   coords     DEVICE [n_axes,B,N] int32, any values; must not overlap y
  * Angles are formed in fp64 (their error is about 2^-53 of the angle, so positions of a million
  * are as exact as small ones), sine and cosine and the products in fp32, and
- * each result is rounded once to dtype.  H and N may be anything >= 1. */
+ * each result is rounded once to dtype.  H and N may be anything from 1 to 2^30
+ * (B * H and B * N below 2^31).  A turn's gradient is the turn back: the same call with the
+ * inv_freq negated. */
 wave_status wave_rotary_apply(const void *x, const int32_t *coords, const wave_rotary *rotary, int dtype,
                               int B, int H, int N, int d, void *y, void *hip_stream);
 
@@ -383,7 +385,10 @@ typedef struct {
  *                 the nearer); nothing of the others is written, their rows of
  *                 q_out included
  *   rotary        HOST, or NULL: keys go in as they are; q must then be NULL
- *   coords        DEVICE [n_axes,B,n_new] int32, or NULL: tokens[b] + t on every axis
+ *   coords        DEVICE [n_axes,B,n_new] int32, or NULL: tokens[b] + t on every axis.
+ *                 Must not overlap q_out, lengths_out or tokens_out, except that with
+ *                 one axis and n_new = 1 it may be cache->lengths or cache->tokens
+ *                 themselves, updated in place
  *   lengths_out, tokens_out  DEVICE [B]: the numbers after the call.  Each may be
  *                 the cache's own array (updated in place) and must not overlap it
  *                 otherwise; tokens_out may be NULL where cache->tokens is.

@@ -562,9 +562,12 @@ wave_status wave_rotary_apply(const void* x, const int32_t* coords, const wave_r
   RotaryArgs rot;
   const wave_status st = check_rotary(rotary, d, &rot);
   if (st != WAVE_OK) return st;
-  if ((long long)B * H >= (1ll << 31) || (long long)B * N >= (1ll << 31)) return WAVE_ERR_SHAPE;
+  if ((long long)B * H >= (1ll << 31) || (long long)B * N >= (1ll << 31) || H > (1 << 30) || N > (1 << 30))
+    return WAVE_ERR_SHAPE;
   const size_t bytes = (size_t)B * H * N * d * elem_bytes(dtype);
-  if (!same_or_apart(x, bytes, y, bytes)) return WAVE_ERR_ARG;
+  if (!same_or_apart(x, bytes, y, bytes) ||
+      overlaps(coords, sizeof(int32_t) * (size_t)rotary->n_axes * B * N, y, bytes))
+    return WAVE_ERR_ARG;
   return launch_rotary(x, coords, rot, dtype, B, H, N, d, y, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -622,6 +625,16 @@ wave_status wave_cache_append(const wave_cache* cache, const void* k_new, const 
       overlaps(lengths_out, counts_bytes, tokens_out, counts_bytes) ||
       overlaps(counts, counts_bytes, lengths_out, counts_bytes) || overlaps(counts, counts_bytes, tokens_out, counts_bytes))
     return WAVE_ERR_ARG;
+  if (coords) {
+    // one coordinate per sequence may be the array that is updated in place (its readers are waited for); in any other form
+    // a workgroup would read what another one writes
+    const size_t xb = sizeof(int32_t) * (size_t)rotary->n_axes * c.B * n_new;
+    const bool one = rotary->n_axes == 1 && n_new == 1;
+    if ((overlaps(coords, xb, lengths_out, counts_bytes) && !(one && coords == lengths_out && coords == c.lengths)) ||
+        (overlaps(coords, xb, tokens_out, counts_bytes) && !(one && coords == tokens_out && coords == c.tokens)) ||
+        (q && overlaps(coords, xb, q_out, (size_t)c.B * Hq * n_new * c.d * es)))
+      return WAVE_ERR_ARG;
+  }
   if ((long long)c.B * (((long long)n_new + 31) / 32) >= kMaxGrid) return WAVE_ERR_SHAPE;
   return launch_cache_append(c, k_new, v_new, q, q ? Hq : 0, n_new, counts, rotary ? &rot : nullptr, coords, q_out,
                              lengths_out, tokens_out, static_cast<hipStream_t>(hip_stream));

@@ -767,7 +767,8 @@ wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int
   a.slices = g.slices;
   a.keep_slices = g.keep_slices;
   const int units = from.B * from.Hkv, rows = a.source ? a.n_keep : g.moves;
-  if ((long long)units * ((long long)rows / 8 + 1) >= (1ll << 24) || (long long)units * g.slices >= (1ll << 22))
+  const int row_bytes = from.d * (from.dtype == WAVE_BF16 ? 2 : 4), move_rows = 4096 / row_bytes;
+  if ((long long)units * ((long long)rows / move_rows + 1) >= (1ll << 24) || (long long)units * g.slices >= (1ll << 22))
     return WAVE_ERR_SHAPE;
   if (g.slices > 0) {
     const int grid = units * g.slices;
@@ -783,7 +784,7 @@ wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int
     else if (per <= 8) launch_evict_select<8>(a, units, st);
     else launch_evict_select<16>(a, units, st);
   }
-  switch (from.d * (from.dtype == WAVE_BF16 ? 2 : 4)) {
+  switch (row_bytes) {
     case 128: launch_evict_move<128>(a, units, rows, st); break;
     case 256: launch_evict_move<256>(a, units, rows, st); break;
     default: launch_evict_move<512>(a, units, rows, st); break;

@@ -503,7 +503,8 @@ __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinSha
   join_waves<T, D>(st, a.G, js, areas, wave, g, c, a.ml + at, a.acc + at * D);
 }
 
-// Prefix, straight from memory: one workgroup per (KV head, range of prefix rows, tile of 16 of the B * G query rows).
+// Prefix with the own rows' stream: one workgroup per (KV head, range of prefix rows, tile of 16 of the B * G query rows).
+// Up to 16 query rows, and fp32, whose products take eight times as long, so that sharing rows in LDS has nothing to gain.
 template <typename T, int D>
 __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, JoinShared& js, const Areas areas) {
   typedef Step<T, D> S;
@@ -678,8 +679,9 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 // ----------------------------------------------------------------------------
 // Prefix and own rows in one launch: one is bound by the matrix units as soon as it has many query rows, the other by
 // memory.  256 workgroups of the one (all, if there are fewer) and as many of the other alternate, so that a CU has one of
-// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows: 174 us; in launches of their own
-// 117 + 71 us, all of the prefix first 180 us, mixed in proportion, which leaves single prefix workgroups for the end, 206.)
+// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows, measured with three numbers a weight: 174 us; in
+// launches of their own 117 + 71 us, all of the prefix first 180 us, mixed in proportion, which leaves single prefix
+// workgroups for the end, 206.  With two numbers, as it is now: 155 us.)
 // Tiles of one prefix range are a multiple of 8 workgroups apart, on one XCD, wherever Hkv * splits is one.
 // ----------------------------------------------------------------------------
 struct Role {
@@ -726,8 +728,8 @@ __global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs 
 }
 
 // ----------------------------------------------------------------------------
-// Merge.  The first B * Hq workgroups join a head's partial results.  With weights, the others have 1024 rows of a unit
-// each: they form the G heads' normalisers from the partial (m, l) again, which is less than waiting for them, and add up
+// Merge.  The first B * Hq workgroups join a head's partial results.  With weights, the others have weight_rows(G) rows
+// of a unit each: they form the G heads' normalisers from the partial (m, l) again, which is less than waiting for them, and add up
 // the softmax weights.
 // ----------------------------------------------------------------------------
 struct HeadParts {
@@ -897,7 +899,7 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
   g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : M <= 64 ? 64 : 128;
   g.mtiles = (M + g.mtile - 1) / g.mtile;
   if (P > 0) {
-      // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 52 us
+    // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 52 us
     // instead of 57 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory (100K rows, 64 query
     // rows: 95 us instead of 110).
     const int aim = g.mtile == 128 && c.d == 128 ? 256 : 512;

@@ -123,6 +123,23 @@ def test_append_refuses():
     assert call(counts=lo) == ARG
 
 
+def test_coordinates_apart_from_what_is_written():
+    L = wb.lib()
+    c, one, two = _cache(), wb.wave_rotary_plan(64, 1e4), wb.wave_rotary_plan(64, 1e4, [16, 16])
+    kn, vn, q, qo, lo, to = (0x4000000 + i * 0x100000 for i in range(6))
+
+    def append(coords, r=one, n=1, lo=lo, to=to):
+        return L.wave_cache_append(ctypes.byref(c), kn, vn, q, 4, n, None, ctypes.byref(r), coords, qo, lo, to, None)
+
+    assert append(lo) == ARG and append(to) == ARG and append(qo) == ARG and append(qo + 2 * 4 * 128 * 2 - 4) == ARG
+    assert append(c.lengths, n=3, lo=c.lengths) == ARG and append(c.lengths, r=two, lo=c.lengths) == ARG
+    assert append(c.tokens + 4, to=c.tokens) == ARG and append(c.tokens, r=two, to=c.tokens) == ARG
+    x, y = 0x100000, 0x900000
+    apply = lambda coords, B=2, H=3, N=5, y=y: L.wave_rotary_apply(x, coords, ctypes.byref(two), 1, B, H, N, 64, y, None)
+    assert apply(y) == ARG and apply(y - 4 * 2 * 2 * 5 + 4) == ARG and apply(y + 2 * 3 * 5 * 64 * 2 - 4) == ARG
+    assert apply(FAKE, B=1, H=(1 << 30) + 1, N=1) == SHAPE and apply(FAKE, B=1, H=1, N=(1 << 30) + 1) == SHAPE
+
+
 def test_attention_refuses():
     L = wb.lib()
     c = _cache()

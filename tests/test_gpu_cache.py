@@ -116,6 +116,30 @@ def test_rotary_with_frequencies_of_its_own():
     _near_turned(got, x, coords, (64, [32], 0), 0, 1e4, "f32", "scaled")
 
 
+@pytest.mark.parametrize("d,rot,sections,order,pairing", PLANS)
+def test_rotary_gradient(d, rot, sections, order, pairing):
+    """The turn back (inv_freq negated) is the gradient: against differences of the formula, which is linear, in fp64."""
+    g, base = _gen(9), 5e5
+    B, H, N = 2, 3, 7
+    x, dy = (torch.randn(B, H, N, d, generator=g) for _ in range(2))
+    coords = torch.randint(0, 4096, (len(sections), B, N), generator=g, dtype=torch.int32)
+    r = wb.wave_rotary_plan(rot, base, sections, order, pairing)
+    for i in range(rot // 2):
+        r.inv_freq[i] = -r.inv_freq[i]
+    got = wb.wave_rotary_apply(dy.cuda(), coords.cuda(), r)
+    plan = (rot, sections, order)
+    _near_turned(got, dy, -coords, plan, pairing, base, "f32", "gradient")      # the formula's: the transposed turn
+    loss = lambda x: float((_turned(x, coords.numpy(), plan, pairing, base)[0] * dy.double().numpy()).sum())
+    _, size = _turned(dy.double().numpy(), coords.numpy(), plan, pairing, base)
+    for b, h, n, c in ((0, 0, 0, 0), (1, 2, 6, rot - 1), (0, 1, 3, rot // 2), (1, 0, 5, d - 1), (0, 2, 1, 1)):
+        step = np.zeros((B, H, N, d))
+        step[b, h, n, c] = 1.0
+        at = x.double().numpy()
+        change = (loss(at + step) - loss(at - step)) / 2
+        # 9 u of the pair's length as in _near_turned; the differences themselves are off by 2^-53 of some thousand terms
+        assert abs(float(got[b, h, n, c]) - change) <= 9 * U * size[b, h, n, c] + 1e-11, (b, h, n, c)
+
+
 # --------------------------------------------------------------------------- append
 def _filled_cache(dtype, B, Hkv, d, cap, lengths, seed):
     """A cache whose rows behind the lengths hold no numbers."""
@@ -192,6 +216,23 @@ def test_append_forms_agree():
         assert _same_bits(bare.k[i, :, x:x + n], k[i]) and _same_bits(bare.v[i, :, x:x + n], v[i])
         assert not bare.k[i, :, :x].any() and not bare.k[i, :, x + n:].any()
     assert bare.lengths.tolist() == [x + n for x in lengths]
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(2, 1), (128, 16)])
+@pytest.mark.parametrize("name", ["lengths", "tokens"])
+def test_append_with_its_own_numbers_as_coordinates(name, Hq, Hkv):
+    """One new token whose coordinate is the sequence's length, which the same call advances (one workgroup a sequence, and
+    several)."""
+    g, B, d = _gen(13), 3, 128
+    a, b = (_filled_cache("f32", B, Hkv, d, 24, [3, 0, 17], 6) for _ in range(2))
+    r = wb.wave_rotary_plan(d, 1e4)
+    for _ in range(5):
+        k, v, q = (torch.randn(B, h, 1, d, generator=g).cuda() for h in (Hkv, Hkv, Hq))
+        qa = wb.wave_cache_append(a, k, v, q=q, rotary=r)
+        qb = wb.wave_cache_append(b, k, v, q=q, rotary=r, coords=b.t[name].view(1, B, 1))
+        assert _same_bits(qa, qb)
+    for key, t in a.t.items():
+        assert _same_bits(t, b.t[key]), key
 
 
 # --------------------------------------------------------------------------- attention
