@@ -422,43 +422,58 @@ __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, Join
 }
 
 // ----------------------------------------------------------------------------
-// How the own rows are cut: pieces of `rows` rows, a multiple of 128 that makes about `target` of them per KV head.  Piece
-// w of a KV head belongs to the sequence whose pieces it falls among.  All lanes of a wave call this together.
+// How the own rows are cut: every sequence into equal pieces, by about the smallest number of rows (a multiple of 128) a piece
+// with which there are no more than `target` of them per KV head, so that all workgroups run side by side and end together.
+// With many sequences, where looking for it costs more than it gives, by the share of `target` pieces: then there may be one
+// more for each sequence.  Piece w of a KV head belongs to the sequence whose pieces it falls among.  All lanes of a wave call
+// this together.  (Pieces of one length for all sequences, six a CU: one sequence of 32000 rows 36 us, now 28; 16 of 1000 23
+// and 18; 62 of 280 33 and 25; 2000 of 160 218 and 177.)
 // ----------------------------------------------------------------------------
-struct Pieces {
-  int rows;               // rows of a piece
-  int b, first, length;   // the sequence, its first piece, its rows (b = B: there is no piece w)
+__host__ __device__ constexpr bool cuts_fit(int B, int target) { return B <= 64 && 2 * B <= target; }
+struct Piece {
+  int b, first, count, length;  // the sequence, its first piece, its pieces, its rows (b = B: there is no piece w)
 };
 __device__ __forceinline__ int cache_length(const int32_t* lengths, int b, int capacity) {
   return min(max(lengths[b], 0), capacity);
 }
-__device__ __forceinline__ int piece_rows(const int32_t* lengths, int B, int capacity, int target) {
-  long long total = 0;
+__device__ __forceinline__ Piece find_piece(const int32_t* lengths, int B, int capacity, int target, int w) {
   const int lane = threadIdx.x & 63;
+  const int len0 = lane < B ? cache_length(lengths, lane, capacity) : 0;
+  auto length = [&](int b0) { return b0 == 0 ? len0 : b0 + lane < B ? cache_length(lengths, b0 + lane, capacity) : 0; };
+  long long total = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
-    const int len = b0 + lane < B ? cache_length(lengths, b0 + lane, capacity) : 0;
+    const int len = length(b0);
     // (64 lengths of up to 2^30 in two sums of 16 bits and more each)
     total += ((long long)wave_sum_i(len >> 12) << 12) + wave_sum_i(len & 4095);
   }
-  const long long r = (total + target - 1) / target;
-  return (int)((r + 127) / 128 > 0 ? (r + 127) / 128 * 128 : 128);
-}
-__device__ __forceinline__ Pieces find_piece(const int32_t* lengths, int B, int capacity, int target, int w) {
-  const int lane = threadIdx.x & 63;
-  Pieces p;
-  p.rows = piece_rows(lengths, B, capacity, target);
-  p.b = B;
-  p.first = p.length = 0;
+  // pieces of a sequence where one has `steps` times 128 rows: never more than the rounded up quotient (a piece may get more)
+  auto pieces = [](int len, int steps) { return (int)ceilf((float)len * ((1.f - 1e-6f) / (128.f * steps))); };
+  auto fits = [&](int steps) {
+    int n = 0;
+    for (int b0 = 0; b0 < B; b0 += 64) n += wave_sum_i(pieces(length(b0), steps));
+    return n <= target;
+  };
+  auto parts = [&](int n) { return max((int)ceil((double)total / (128.0 * n)), 1); };
+  int steps = parts(target);
+  if (cuts_fit(B, target) && !fits(steps)) {
+    int low = steps;
+    steps = parts(target - B);  // fits: a sequence has less than one piece more than its share
+    for (int i = 0; i < 3 && steps - low > 1; ++i) {
+      const int middle = (low + steps) / 2;
+      if (fits(middle)) steps = middle; else low = middle;
+    }
+  }
+  Piece p = {B, 0, 0, 0};
   int before = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
-    const int len = b0 + lane < B ? cache_length(lengths, b0 + lane, capacity) : 0;
-    const int n = (len + p.rows - 1) / p.rows;
+    const int len = length(b0), n = pieces(len, steps);
     const int incl = before + wave_incl_scan(n);
     const uint64_t hit = __ballot(w < incl);
     if (hit) {
       const int at = __ffsll((unsigned long long)hit) - 1;
       p.b = b0 + at;
-      p.first = __builtin_amdgcn_readlane(incl - n, at);
+      p.count = __builtin_amdgcn_readlane(n, at);
+      p.first = __builtin_amdgcn_readlane(incl, at) - p.count;
       p.length = __builtin_amdgcn_readlane(len, at);
       return p;
     }
@@ -473,10 +488,11 @@ struct AttendArgs {
   float *weights_out, *out, *lse;
   float *z, *acc, *pacc;   // products q . k [B * Hq][zrow]; sums of the own pieces [Hkv][pieces][G][D], of the prefix [splits][B * Hq][D]
   float2 *ml, *pml;        // their references and normalisers
-  int2* info;              // [B] the first piece of a sequence and the rows of a piece, for the joining
+  int2* info;              // [B] the first piece of a sequence and how many it has, for the joining
   int B, Hq, Hkv, G, capacity, P;
   int target, pieces, prefix_rows, splits, zrow;
-  int prefix_blocks, own_blocks, turn, prefix_turns;
+  int prefix_blocks, own_blocks, turn, prefix_turns, head_blocks;
+  bool head_waves;  // a head's joining is a wave's, not a workgroup's
   float scale, decay;
 };
 
@@ -485,11 +501,12 @@ template <typename T, int D>
 __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinShared& js, const Areas areas) {
   typedef Step<T, D> S;
   const int w = block / a.Hkv, h = block % a.Hkv;
-  const Pieces p = find_piece(a.lengths, a.B, a.capacity, a.target, w);
+  const Piece p = find_piece(a.lengths, a.B, a.capacity, a.target, w);
   if (p.b == a.B) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-  const int start = (w - p.first) * p.rows, end = min(p.length, start + p.rows);
-  if (start == 0 && h == 0 && threadIdx.x == 0) a.info[p.b] = make_int2(w, p.rows);
+  const int rows = ((p.length + p.count - 1) / p.count + 31) / 32 * 32;
+  const int start = (w - p.first) * rows, end = min(p.length, start + rows);
+  if (w == p.first && h == 0 && threadIdx.x == 0) a.info[p.b] = make_int2(w, p.count);
   const size_t unit = (size_t)p.b * a.Hkv + h, row = D * sizeof(T);
   const int head = h * a.G + min(c, a.G - 1);  // (columns behind the G heads repeat the last one)
   const size_t bh = (size_t)p.b * a.Hq + head;
@@ -728,7 +745,8 @@ __global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs 
 }
 
 // ----------------------------------------------------------------------------
-// Merge.  The first B * Hq workgroups join a head's partial results.  With weights, the others have weight_rows(G) rows
+// Merge.  The first workgroups join the heads' partial results: one head each, or four, a wave each, where there are many
+// heads with few (256 sequences of 300 rows, 8192 heads: 8 us instead of 16).  With weights, the others have weight_rows(G) rows
 // of a unit each: they form the G heads' normalisers from the partial (m, l) again, which is less than waiting for them, and add up
 // the softmax weights.
 // ----------------------------------------------------------------------------
@@ -737,6 +755,11 @@ struct HeadParts {
   int splits, own, stride, pstride;  // partials of the prefix and of own pieces, and what lies between them
   __device__ __forceinline__ float2 at(int i) const {
     return i < splits ? pml[(size_t)i * pstride] : ml[(size_t)(i - splits) * stride];
+  }
+  template <int D>
+  __device__ __forceinline__ const float* sum(const AttendArgs& a, int i, int b, int h, int gq, int first) const {
+    return i < splits ? a.pacc + ((size_t)i * pstride + (size_t)h * a.B * a.G + (size_t)b * a.G + gq) * D
+                      : a.acc + (((size_t)h * a.pieces + first + i - splits) * a.G + gq) * D;
   }
 };
 __device__ __forceinline__ HeadParts head_parts(const AttendArgs& a, int b, int h, int gq, int first, int own) {
@@ -772,8 +795,8 @@ struct OwnPieces {
   int first, count;
 };
 __device__ __forceinline__ OwnPieces own_pieces(const AttendArgs& a, int b, int length) {
-  const int2 p = length > 0 ? a.info[b] : make_int2(0, 1);
-  return OwnPieces{p.x, (length + p.y - 1) / p.y};
+  const int2 p = length > 0 ? a.info[b] : make_int2(0, 0);
+  return OwnPieces{p.x, p.y};
 }
 
 template <int D, int G>
@@ -781,7 +804,35 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   constexpr int WEIGHT_ROWS = weight_rows(G);
   const int heads = a.B * a.Hq, tid = threadIdx.x, wave = tid >> 6;
   __shared__ float2 norm[G];
-  if ((int)blockIdx.x < heads) {
+  if (a.head_waves && (int)blockIdx.x < a.head_blocks) {
+    const int bh = blockIdx.x * 4 + wave;
+    if (bh >= heads) return;
+    const int b = bh / a.Hq, hq = bh % a.Hq, h = hq / G, gq = hq % G;
+    const OwnPieces own = own_pieces(a, b, cache_length(a.lengths, b, a.capacity));
+    const HeadParts p = head_parts(a, b, h, gq, own.first, own.count);
+    const float2 n = normaliser(p);
+    constexpr int LANES = D / 4, GROUPS = 64 / LANES;
+    const int lane = tid % LANES, group = (tid & 63) / LANES;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int i = group; i < p.splits + own.count; i += GROUPS) {
+      const float2 x = p.at(i);
+      const float f = x.x == neg_inf() ? 0.f : exp2f(x.x - n.x);
+      sum += f * *reinterpret_cast<const f32x4*>(p.sum<D>(a, i, b, h, gq, own.first) + lane * 4);
+    }
+#pragma unroll
+    for (int off = LANES; off < 64; off *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], off);
+    if (group == 0) {
+      f32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = n.x == neg_inf() ? 0.f : sum[e] / n.y;
+      *reinterpret_cast<f32x4*>(a.out + (size_t)bh * D + lane * 4) = o;
+    }
+    if ((tid & 63) == 0) a.lse[bh] = n.x == neg_inf() ? neg_inf() : (n.x + log2f(n.y)) * kLn2;
+    return;
+  }
+  if ((int)blockIdx.x < a.head_blocks) {
     __shared__ float part[256 / (D / 4)][D];
     const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / G, gq = hq % G;
     const OwnPieces own = own_pieces(a, b, cache_length(a.lengths, b, a.capacity));
@@ -793,10 +844,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
     for (int i = group; i < p.splits + own.count; i += GROUPS) {
       const float2 x = p.at(i);
       const float f = x.x == neg_inf() ? 0.f : exp2f(x.x - n.x);
-      const float* acc = i < p.splits
-                             ? a.pacc + ((size_t)i * p.pstride + (size_t)h * a.B * G + (size_t)b * G + gq) * D
-                             : a.acc + (((size_t)h * a.pieces + own.first + i - p.splits) * G + gq) * D;
-      sum += f * *reinterpret_cast<const f32x4*>(acc + lane * 4);
+      sum += f * *reinterpret_cast<const f32x4*>(p.sum<D>(a, i, b, h, gq, own.first) + lane * 4);
     }
     *reinterpret_cast<f32x4*>(&part[group][lane * 4]) = sum;
     __syncthreads();
@@ -810,7 +858,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
     return;
   }
   const int chunks = (a.capacity + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
-  const int at = blockIdx.x - heads, unit = at / chunks, r0 = at % chunks * WEIGHT_ROWS;
+  const int at = blockIdx.x - a.head_blocks, unit = at / chunks, r0 = at % chunks * WEIGHT_ROWS;
   const int b = unit / a.Hkv, h = unit % a.Hkv;
   const int len = cache_length(a.lengths, b, a.capacity);
   if (r0 >= len) return;
@@ -871,11 +919,14 @@ wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
     }
   }
   if (!shared) WAVE_LAUNCH("cache_attend", (attend_rows_kernel<T, D>), blocks, 256, 0, st, a);
+  // (on the mean; fewer than 1024 heads leave CUs without work)
+  a.head_waves = a.B * a.Hq >= 1024 && a.splits + g.pieces / a.B <= 8;
+  a.head_blocks = a.head_waves ? (a.B * a.Hq + 3) / 4 : a.B * a.Hq;
   switch (a.G) {
 #define WAVE_G(n)                                                                                              \
   case n: {                                                                                                    \
     const int chunks = (a.capacity + weight_rows(n) - 1) / weight_rows(n);                                     \
-    const unsigned grid = a.B * a.Hq + (a.weights_out ? a.B * a.Hkv * chunks : 0);                             \
+    const unsigned grid = a.head_blocks + (a.weights_out ? a.B * a.Hkv * chunks : 0);                             \
     WAVE_LAUNCH("cache_join", (join_kernel<D, n>), grid, 256, 0, st, a);                                       \
     break;                                                                                                     \
   }
@@ -891,10 +942,6 @@ wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
 CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool accumulate) {
   CacheAttendGeom g{};
   const int G = Hq / c.Hkv;
-  // Own rows: about six pieces a CU over all KV heads; every sequence may end in a piece that is not full.
-  g.target = 1536 / c.Hkv > 1 ? 1536 / c.Hkv : 1;
-  const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
-  g.pieces = (int)((long long)g.target + c.B < most ? g.target + c.B : most);
   const int M = c.B * G;
   g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : M <= 64 ? 64 : 128;
   g.mtiles = (M + g.mtile - 1) / g.mtile;
@@ -908,6 +955,15 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);
   }
+  // Own rows: a piece a CU, two at d = 64 (one wave's loads are half as long; 64 sequences of 2300 rows: 46 us with one, 41).
+  // Six beside a prefix that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows:
+  // 155 us, 160 with two).
+  const bool beside = P > 0 && M > 16 && c.Hkv * g.splits * g.mtiles >= 128;
+  const int per_cu = beside ? 6 : c.d == 64 ? 2 : 1;
+  g.target = per_cu * 256 / c.Hkv > 1 ? per_cu * 256 / c.Hkv : 1;
+  const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
+  const long long cut = (long long)g.target + (cuts_fit(c.B, g.target) ? 0 : c.B);
+  g.pieces = (int)(cut < most ? cut : most);
   g.zrow = (c.capacity + 31) / 32 * 32;  // whole steps
   size_t o = 0;
   g.off_info = o;  o = align_up(o + sizeof(int32_t) * 2 * (size_t)c.B);

@@ -331,6 +331,20 @@ def test_attention_long(dtype):
         _check_attention(dtype, q, cache, lengths, pk, pv, 1.0, cache.weights, out, lse, w, f"peak {peak}")
 
 
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 128)])
+@pytest.mark.parametrize("B,Hq,Hkv,cap,lengths,P", [
+    (30, 4, 4, 6001, [17 * b for b in range(29)] + [6001], 0),                 # one long among short ones
+    (9, 8, 4, 2600, [2600 - 256 * b for b in range(9)], 1),                    # no even share of the pieces
+    (70, 16, 2, 1500, [(97 * b) % 400 for b in range(69)] + [1500], 0),        # more sequences than a wave has lanes, many heads
+    (300, 8, 1, 60, [b % 61 for b in range(300)], 40),
+    (129, 8, 8, 300, [0] * 64 + [300] * 64 + [1], 0)])
+def test_attention_ragged(dtype, d, B, Hq, Hkv, cap, lengths, P):
+    cache, q, pk, pv = _inputs(dtype, B, Hq, Hkv, d, cap, lengths, P, B)
+    w = torch.zeros_like(cache.weights)
+    out, lse = wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w, decay=0.5)
+    _check_attention(dtype, q, cache, lengths, pk, pv, 0.5, cache.weights, out, lse, w, f"B {B}")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("B,P", [(20, 32768), (17, 32767), (40, 33001)])
 def test_attention_long_prefix_of_many_query_rows(d, B, P):
