@@ -313,17 +313,17 @@ struct State {
 };
 
 // ----------------------------------------------------------------------------
-// The stream of one wave: the rows k0, k0 + stride, .. below `end` against a tile of query columns.  z: where a lane leaves
-// the products of its column (NULL: nowhere).  ONCE: nobody else reads these rows, so they pass by the caches.  lds: the
+// The stream of one wave: the rows k0, k0 + stride, .. below `end` against a tile of query columns.  leave: what happens to four
+// neighbouring rows' products with a lane's column.  ONCE: nobody else reads these rows, so they pass by the caches.  lds: the
 // wave's own place for a step's key rows.  Keys go through it because an operand has sixteen rows side by side, 64 bytes of
 // each in a load: straight from memory every line is asked for twice, and must stay in the caches between.  A load of the
 // values takes whole rows.  1.12 GB of own rows: 235 us with both straight from memory, 222 with the values passing by the
 // caches, 209 us = 5.5 TB/s, what a plain read of 1 GiB reaches, so.  (Values through LDS too: the same alone, but 171
 // instead of 155 us beside a long prefix, which needs LDS itself.)
 // ----------------------------------------------------------------------------
-template <typename T, int D, bool ONCE>
+template <typename T, int D, bool ONCE, typename Leave>
 __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0, int stride, int end, float scale,
-                                            const typename Step<T, D>::Q& q, State<T, D>& st, float* z, char* lds, int lane) {
+                                            const typename Step<T, D>::Q& q, State<T, D>& st, Leave&& leave, char* lds, int lane) {
   typedef Step<T, D> S;
   constexpr int ROW = S::ROW;
   const int last = end - 1, g = lane >> 4, c = lane & 15;
@@ -349,11 +349,8 @@ __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0
 #pragma unroll
       for (int i = 0; i < S::NS; ++i) s[i] = S::key(g, i) > rest ? neg_inf() : s[i];
     }
-    if (z) {
 #pragma unroll
-      for (int i = 0; i < S::NS; i += 4)
-        *reinterpret_cast<f32x4*>(z + k0 + S::key(g, i)) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
-    }
+    for (int i = 0; i < S::NS; i += 4) leave(k0 + S::key(g, i), f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]});
     const typename S::Vt vt = S::transpose(v);
     __builtin_amdgcn_sched_barrier(0);
     v = S::template load_v<ONCE>(step_rows<ROW>(V, next, last), g, c);
@@ -515,7 +512,7 @@ __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinSha
   st.init();
   float* z = a.weights_out && c < a.G ? a.z + bh * a.zrow : nullptr;
   stream_rows<T, D, true>(a.k + unit * a.capacity * row, a.v + unit * a.capacity * row, start + wave * S::KEYS, 4 * S::KEYS, end,
-                          a.scale, q, st, z, areas.of(wave), lane);
+                          a.scale, q, st, [&](int row, const f32x4& x) { if (z) *reinterpret_cast<f32x4*>(z + row) = x; }, areas.of(wave), lane);
   const size_t at = ((size_t)h * a.pieces + w) * a.G;
   join_waves<T, D>(st, a.G, js, areas, wave, g, c, a.ml + at, a.acc + at * D);
 }
@@ -536,7 +533,7 @@ __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, Join
   st.init();
   const int start = split * a.prefix_rows, end = min(a.P, start + a.prefix_rows);
   stream_rows<T, D, false>(a.prefix_k + (size_t)h * a.P * row, a.prefix_v + (size_t)h * a.P * row, start + wave * S::KEYS,
-                           4 * S::KEYS, end, a.scale, q, st, nullptr, areas.of(wave), lane);
+                           4 * S::KEYS, end, a.scale, q, st, [](int, const f32x4&) {}, areas.of(wave), lane);
   const size_t at = ((size_t)split * a.Hkv + h) * M + m0;  // by KV head and query row
   join_waves<T, D>(st, min(16, M - m0), js, areas, wave, g, c, a.pml + at, a.pacc + at * D);
 }
@@ -787,6 +784,92 @@ __device__ __forceinline__ float2 normaliser(const HeadParts& p) {
   return make_float2(top, wave_add_f(l));
 }
 
+// ----------------------------------------------------------------------------
+// Short caches: one launch, a workgroup of eight waves per unit, which go through the prefix and the unit's rows and join in
+// LDS.  There the products of the own rows stay too, for the weights.
+// ----------------------------------------------------------------------------
+constexpr int SHORT_WAVES = 8, SHORT_THREADS = SHORT_WAVES * 64;
+// rows that the waves take in one step each, and room for two
+constexpr int short_step(int dtype) { return SHORT_WAVES * (dtype == WAVE_BF16 ? Step<bf16_t, 64>::KEYS : Step<float, 64>::KEYS); }
+
+template <typename T, int D, int G>
+__global__ __launch_bounds__(SHORT_THREADS) void attend_short_kernel(const AttendArgs a) {
+  typedef Step<T, D> S;
+  constexpr int PITCH = D + 4, ZROW = 2 * SHORT_WAVES * S::KEYS + 4;
+  __shared__ __attribute__((aligned(16))) char lds[SHORT_WAVES][16 * PITCH * 4];
+  __shared__ __attribute__((aligned(16))) float products[G][ZROW];
+  __shared__ float sm[SHORT_WAVES][16], sl[SHORT_WAVES][16];
+  const int unit = blockIdx.x, b = unit / a.Hkv, h = unit % a.Hkv;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const size_t row = D * sizeof(T);
+  const int len = cache_length(a.lengths, b, a.capacity), head = b * a.Hq + h * G;
+  const typename S::Q q = S::load_q(a.q + (size_t)(head + min(c, G - 1)) * row, g);
+  State<T, D> st;
+  st.init();
+  if (a.P > 0)
+    stream_rows<T, D, false>(a.prefix_k + (size_t)h * a.P * row, a.prefix_v + (size_t)h * a.P * row, wave * S::KEYS,
+                             SHORT_WAVES * S::KEYS, a.P, a.scale, q, st, [](int, const f32x4&) {}, lds[wave], lane);
+  // the wave that the prefix leaves first takes the first own rows
+  const int turn = (wave + SHORT_WAVES - (a.P + S::KEYS - 1) / S::KEYS % SHORT_WAVES) % SHORT_WAVES;
+  const bool keep = a.weights_out && c < G;
+  stream_rows<T, D, true>(a.k + (size_t)unit * a.capacity * row, a.v + (size_t)unit * a.capacity * row, turn * S::KEYS,
+                          SHORT_WAVES * S::KEYS, len, a.scale, q, st,
+                          [&](int r, const f32x4& x) { if (keep) *reinterpret_cast<f32x4*>(&products[c][r]) = x; },
+                          lds[wave], lane);
+  float l = st.l;
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (g == 0) {
+    sm[wave][c] = st.m;
+    sl[wave][c] = l;
+  }
+  if (c < G) {
+    float* at = reinterpret_cast<float*>(lds[wave]) + c * PITCH;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < S::ACC; x += 4)
+        *reinterpret_cast<f32x4*>(at + S::channel(g, x, i)) = f32x4{st.o[x][i], st.o[x + 1][i], st.o[x + 2][i], st.o[x + 3][i]};
+  }
+  __syncthreads();
+  // a head's reference and sum; none of its scores a number above -infinity: (0, 1), and no output
+  auto normal = [&](int col, float& m, float& sum) {
+    m = sm[0][col];
+#pragma unroll
+    for (int w = 1; w < SHORT_WAVES; ++w) m = fmaxf(m, sm[w][col]);
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < SHORT_WAVES; ++w) sum += (sm[w][col] == neg_inf() ? 0.f : exp2f(sm[w][col] - m)) * sl[w][col];
+    return !(m == neg_inf() && sum == 0.f);
+  };
+  for (int i = threadIdx.x; i < G * D; i += SHORT_THREADS) {
+    const int col = i / D, ch = i % D;
+    float m, sum, o = 0.f;
+    const bool any = normal(col, m, sum);
+#pragma unroll
+    for (int w = 0; w < SHORT_WAVES; ++w)
+      o += (sm[w][col] == neg_inf() ? 0.f : exp2f(sm[w][col] - m)) * reinterpret_cast<const float*>(lds[w])[col * PITCH + ch];
+    a.out[(size_t)(head + col) * D + ch] = any ? o / sum : 0.f;
+    if (ch == 0) a.lse[head + col] = any ? (m + log2f(sum)) * kLn2 : neg_inf();
+  }
+  if (!a.weights_out) return;
+  float m[G], f[G];
+#pragma unroll
+  for (int j = 0; j < G; ++j) {
+    float sum;
+    const bool any = normal(j, m[j], sum);
+    m[j] = any ? m[j] : 0.f;
+    f[j] = any ? 1.f / sum : 1.f;
+  }
+  const size_t base = (size_t)unit * a.capacity;
+  for (int j = threadIdx.x; j < len; j += SHORT_THREADS) {
+    float w = a.decay > 0.f ? a.decay * a.weights[base + j] : 0.f;
+#pragma unroll
+    for (int x = 0; x < G; ++x) w += __builtin_amdgcn_exp2f(fmaf(products[x][j], a.scale, -m[x])) * f[x];
+    a.weights_out[base + j] = w;
+  }
+}
+
 // rows of a unit per workgroup, by the registers that the heads' products take
 constexpr int weight_rows(int G) { return G <= 4 ? 2048 : 1024; }
 
@@ -898,6 +981,16 @@ constexpr int TWO_TERMS_ROWS = 32768;
 
 template <typename T, int D>
 wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
+  if (g.one_launch) {
+    switch (a.G) {
+#define WAVE_G(n) \
+  case n: WAVE_LAUNCH("cache_attend", (attend_short_kernel<T, D, n>), a.B * a.Hkv, SHORT_THREADS, 0, st, a); break;
+      WAVE_G(1) WAVE_G(2) WAVE_G(3) WAVE_G(4) WAVE_G(5) WAVE_G(6) WAVE_G(7) WAVE_G(8)
+#undef WAVE_G
+      default: return WAVE_ERR_SHAPE;
+    }
+    return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
+  }
   a.prefix_blocks = a.P > 0 ? a.Hkv * a.splits * g.mtiles : 0;
   a.own_blocks = a.Hkv * g.pieces;
   a.turn = a.prefix_blocks < 256 ? (a.prefix_blocks + 7) / 8 * 8 : 256;
@@ -942,6 +1035,12 @@ wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
 CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool accumulate) {
   CacheAttendGeom g{};
   const int G = Hq / c.Hkv;
+  // One launch where a wave has one step to do, or two and the units do not fill the CUs twice over (62 sequences x 8 units of
+  // 280 rows: 26 us, 23 in pieces) or reading all lengths to find a piece takes longer (2000 sequences x 2 of 165: 91 us, 162).
+  // 64 rows for one sequence: 6.0 us instead of 8.3; 15 of 100 rows 7.2, 10.1; 22 of 200 behind 143 of a prefix 5.7, 10.6.
+  // With four steps and few units it is slower: one sequence of 1000 rows 14.3 us instead of 10.2.
+  const int steps = (int)(((long long)P + c.capacity + short_step(c.dtype) - 1) / short_step(c.dtype));
+  g.one_launch = steps <= 1 || (steps <= 2 && (c.B * c.Hkv <= 256 || c.B > 512));
   const int M = c.B * G;
   g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : M <= 64 ? 64 : 128;
   g.mtiles = (M + g.mtile - 1) / g.mtile;

@@ -415,6 +415,56 @@ def test_attention_extreme_scores(dtype):
     assert not o2[0, 2].any() and float(l2[0, 2]) == -math.inf
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,Hq,Hkv,lengths,P", [
+    (1, 1, 1, [1], 0), (1, 8, 1, [33], 1), (2, 6, 2, [0, 129], 0), (3, 7, 1, [128, 1, 700], 127), (5, 10, 2, [0, 70, 31, 32, 64], 129),
+    (9, 8, 1, [0] * 9, 300), (2, 2, 2, [-4, 900], 0), (17, 16, 4, list(range(17)), 65)])
+def test_attention_with_room_for_many_rows(dtype, d, B, Hq, Hkv, lengths, P):
+    """Room for 700 rows a unit: cut into pieces and joined, whatever is in use."""
+    test_attention(dtype, d, B, Hq, Hkv, 700, lengths, P)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 6, 7, 8])
+def test_attention_heads_and_room(dtype, G):
+    for B, cap in ((4, 700), (9, 250), (70, 700), (70, 120)):
+        lengths = [(13 * b) % 41 for b in range(B)]
+        cache, q, pk, pv = _inputs(dtype, B, 2 * G, 2, 64, cap, lengths, 6, G)
+        w = torch.zeros_like(cache.weights)
+        out, lse = wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w, decay=0.0)
+        _check_attention(dtype, q, cache, lengths, pk, pv, 0.0, cache.weights, out, lse, w, f"B {B} cap {cap}")
+
+
+@pytest.mark.parametrize("cap", [50, 700])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_scores_that_are_no_numbers(dtype, cap):
+    """In a short cache and in one of pieces: a head whose scores are not numbers says so, one whose scores are all -infinity
+    counts as without rows, its weights too, and the other heads are as they were."""
+    n, d = 50, 128
+    cache, q, pk, pv = _inputs(dtype, 1, 4, 1, d, cap, [n], 40, 9, 1.0)
+    cache.k[0, 0, :n] = cache.k[0, 0, :n].abs() + 0.125
+    q[0, 3] = -1.0
+    good, glse = wb.wave_cache_attention_decode(q, cache)
+    both, blse = wb.wave_cache_attention_decode(q, cache, pk, pv)
+    q[0, 1, 5] = math.nan
+    for k, v, want in ((None, None, good), (pk, pv, both)):
+        w = torch.zeros_like(cache.weights)
+        out, lse = wb.wave_cache_attention_decode(q, cache, k, v, weights_out=w)
+        assert bool(torch.isnan(out[0, 1]).all()) and bool(torch.isnan(lse[0, 1])) and bool(torch.isnan(w[0, 0, :n]).all())
+        assert _same_bits(out[0, [0, 2, 3]], want[0, [0, 2, 3]])
+    q[0, 1] = -1.0
+    cache.k[0, 0, :n] = math.inf
+    w = torch.zeros_like(cache.weights)
+    out, lse = wb.wave_cache_attention_decode(q[:, [1, 3, 1, 3]].contiguous(), cache, weights_out=w)
+    assert not out.any() and bool((lse == -math.inf).all()) and _same_bits(w[0, 0, :n], cache.weights[0, 0, :n])
+    out, lse = wb.wave_cache_attention_decode(q[:, [1, 3, 1, 3]].contiguous(), cache, pk, pv, weights_out=w)
+    alone, alse = wb.wave_cache_attention_decode(q[:, [1, 3, 1, 3]].contiguous(), wb.alloc_cache(cache.dtype, 1, 1, d, cap), pk, pv)
+    # The same sums of 40 weights, with other waves' nothing between them: up to 40 + 16 roundings each, of values up to 5.
+    assert torch.allclose(out, alone, rtol=0, atol=2 * 56 * 5 * U) and torch.allclose(lse, alse, rtol=0, atol=2 * 56 * U)
+    assert _same_bits(w[0, 0, :n], cache.weights[0, 0, :n])        # (decay 1: the old weights and nothing)
+
+
 def test_attention_equals_full_attention_decode():
     g = _gen(21)
     K, V = (torch.randn(2, 2, 1000, 128, generator=g).bfloat16().cuda() for _ in range(2))
@@ -670,14 +720,14 @@ def test_offsets_beyond_32_bits():
     kn, vn = (torch.randn(B, Hkv, n, d, generator=g).bfloat16().cuda() for _ in range(2))
     q = torch.randn(B, 4, d, generator=g).bfloat16().cuda()
     wb.wave_cache_append(cache, kn, vn)
-    small = wb.alloc_cache(torch.bfloat16, B, Hkv, d, n)
+    small = wb.alloc_cache(torch.bfloat16, B, Hkv, d, 700)   # (room for more than one launch takes: the same order of sums)
     wb.wave_cache_append(small, kn, vn)
     for c in (cache, small):
         c.out = wb.wave_cache_attention_decode(q, c, weights_out=c.weights)
         wb.wave_cache_evict(c, 100, 1, 10)
     assert _same_bits(cache.out[0], small.out[0]) and _same_bits(cache.out[1], small.out[1])
     for name in ("k", "v", "positions", "weights"):
-        assert _same_bits(cache.t[name][:, :, :n], small.t[name]), name
+        assert _same_bits(cache.t[name][:, :, :n], small.t[name][:, :, :n]), name
     # rows at the far end of the last unit
     cache.lengths.fill_(cap - 1)
     wb.wave_cache_append(cache, kn, vn)
