@@ -424,16 +424,20 @@ __device__ __forceinline__ void join_waves(const State<T, D>& st, int cols, Join
 // With many sequences, where looking for it costs more than it gives, by the share of `target` pieces: then there may be one
 // more for each sequence.  Piece w of a KV head belongs to the sequence whose pieces it falls among.  All lanes of a wave call
 // this together.  (Pieces of one length for all sequences, six a CU: one sequence of 32000 rows 36 us, now 28; 16 of 1000 23
-// and 18; 62 of 280 33 and 25; 2000 of 160 218 and 177.)
+// and 19; 16 of 400 .. 4000 40 and 36; 62 of 280 33 and 25.)
 // ----------------------------------------------------------------------------
 __host__ __device__ constexpr bool cuts_fit(int B, int target) { return B <= 64 && 2 * B <= target; }
+// Up to this many rows a piece (or for one sequence, which is cut evenly by any number), half as many pieces: less to start and
+// to join (16 sequences x 8 units of 1000 rows 19.4 us, 18.6; one of 32000 30.1, 28.2); beyond, the two workgroups of a CU keep
+// each other's loads in flight where sequences differ (8 of 7000 .. 65000 rows: 136 us with one, 132 with two).
+constexpr long long FEW_ROWS = 256;
 struct Piece {
   int b, first, count, length;  // the sequence, its first piece, its pieces, its rows (b = B: there is no piece w)
 };
 __device__ __forceinline__ int cache_length(const int32_t* lengths, int b, int capacity) {
   return min(max(lengths[b], 0), capacity);
 }
-__device__ __forceinline__ Piece find_piece(const int32_t* lengths, int B, int capacity, int target, int w) {
+__device__ __forceinline__ Piece find_piece(const int32_t* lengths, int B, int capacity, int target, int few, int w) {
   const int lane = threadIdx.x & 63;
   const int len0 = lane < B ? cache_length(lengths, lane, capacity) : 0;
   auto length = [&](int b0) { return b0 == 0 ? len0 : b0 + lane < B ? cache_length(lengths, b0 + lane, capacity) : 0; };
@@ -443,6 +447,7 @@ __device__ __forceinline__ Piece find_piece(const int32_t* lengths, int B, int c
     // (64 lengths of up to 2^30 in two sums of 16 bits and more each)
     total += ((long long)wave_sum_i(len >> 12) << 12) + wave_sum_i(len & 4095);
   }
+  if (few > 0 && (B == 1 || total <= FEW_ROWS * target)) target = few;
   // pieces of a sequence where one has `steps` times 128 rows: never more than the rounded up quotient (a piece may get more)
   auto pieces = [](int len, int steps) { return (int)ceilf((float)len * ((1.f - 1e-6f) / (128.f * steps))); };
   auto fits = [&](int steps) {
@@ -487,7 +492,7 @@ struct AttendArgs {
   float2 *ml, *pml;        // their references and normalisers
   int2* info;              // [B] the first piece of a sequence and how many it has, for the joining
   int B, Hq, Hkv, G, capacity, P;
-  int target, pieces, prefix_rows, splits, zrow;
+  int target, few, pieces, prefix_rows, splits, zrow;
   int prefix_blocks, own_blocks, turn, prefix_turns, head_blocks;
   bool head_waves;  // a head's joining is a wave's, not a workgroup's
   float scale, decay;
@@ -498,7 +503,7 @@ template <typename T, int D>
 __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinShared& js, const Areas areas) {
   typedef Step<T, D> S;
   const int w = block / a.Hkv, h = block % a.Hkv;
-  const Piece p = find_piece(a.lengths, a.B, a.capacity, a.target, w);
+  const Piece p = find_piece(a.lengths, a.B, a.capacity, a.target, a.few, w);
   if (p.b == a.B) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int rows = ((p.length + p.count - 1) / p.count + 31) / 32 * 32;
@@ -1054,15 +1059,16 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);
   }
-  // Own rows: a piece a CU, two at d = 64 (one wave's loads are half as long; 64 sequences of 2300 rows: 46 us with one, 41).
-  // Six beside a prefix that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows:
-  // 155 us, 160 with two).
+  // Own rows: as many pieces as are resident, two a CU, four at d = 64 (or half of them, see find_piece).  Six beside a prefix
+  // that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows: 153 us with two,
+  // 149).
   const bool beside = P > 0 && M > 16 && c.Hkv * g.splits * g.mtiles >= 128;
-  const int per_cu = beside ? 6 : c.d == 64 ? 2 : 1;
+  const int per_cu = beside ? 6 : c.d == 64 ? 4 : 2;
   g.target = per_cu * 256 / c.Hkv > 1 ? per_cu * 256 / c.Hkv : 1;
   const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
   const long long cut = (long long)g.target + (cuts_fit(c.B, g.target) ? 0 : c.B);
   g.pieces = (int)(cut < most ? cut : most);
+  g.few = beside ? 0 : g.target / 2;
   g.zrow = (c.capacity + 31) / 32 * 32;  // whole steps
   size_t o = 0;
   g.off_info = o;  o = align_up(o + sizeof(int32_t) * 2 * (size_t)c.B);
@@ -1104,6 +1110,7 @@ wave_status launch_cache_attend(const void* q, int Hq, const wave_cache& c, cons
   a.capacity = c.capacity;
   a.P = P;
   a.target = g.target;
+  a.few = g.few;
   a.pieces = g.pieces;
   a.prefix_rows = g.prefix_rows;
   a.splits = g.splits;

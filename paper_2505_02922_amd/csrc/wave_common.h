@@ -364,7 +364,7 @@ wave_status launch_cache_append(const wave_cache& cache, const void* k_new, cons
                                 void* q_out, int32_t* lengths_out, int32_t* tokens_out, hipStream_t st);
 struct CacheAttendGeom {
   bool one_launch;           // a short cache: one workgroup per unit, nothing in the workspace
-  int target, pieces;        // pieces of own rows per KV head: aimed at, and room for
+  int target, few, pieces;   // pieces of own rows per KV head: aimed at, aimed at where they are short (0: target), room for
   int mtile, mtiles;         // query rows of a prefix workgroup, workgroups over the B * G query rows
   int prefix_rows, splits;   // prefix rows per workgroup, workgroups over the prefix
   int zrow;                  // floats per head in the scores
