@@ -290,20 +290,25 @@ __device__ __forceinline__ EvictUnit evict_unit(const EvictArgs& a, int unit) {
   u.wts = a.weights + (size_t)unit * a.capacity;
   return u;
 }
-// keys of the rows r0 + i * 1024 + tid below r1 (others: 0, and no row)
+// Weights and positions of the rows r0 + i * 1024 + tid, of the last one below r1 where that is behind it; asked for before the
+// histograms are, and made into keys after.
 template <int PER>
-__device__ __forceinline__ void evict_keys(const EvictArgs& a, const EvictUnit& u, int r0, int r1, uint32_t (&key)[PER]) {
+struct EvictRows {
   float w[PER];
   int p[PER];
+  __device__ __forceinline__ void load(const EvictUnit& u, int r0, int r1) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int j = min(r0 + i * EVICT_THREADS + (int)threadIdx.x, r1 - 1);
-    w[i] = u.wts[j];
-    p[i] = u.pos[j];
+    for (int i = 0; i < PER; ++i) {
+      const int j = max(min(r0 + i * EVICT_THREADS + (int)threadIdx.x, r1 - 1), 0);
+      w[i] = u.wts[j];
+      p[i] = u.pos[j];
+    }
   }
+  __device__ __forceinline__ void keys(const EvictArgs& a, const EvictUnit& u, uint32_t (&key)[PER]) const {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) key[i] = evict_key(w[i], p[i], a.n_sink, u.local);
-}
+    for (int i = 0; i < PER; ++i) key[i] = evict_key(w[i], p[i], a.n_sink, u.local);
+  }
+};
 
 struct EvictShared {
   uint32_t hist[EVICT_BUCKETS];
@@ -448,7 +453,9 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(const Evict
     return;
   }
   uint32_t key[PER];
-  evict_keys<PER>(a, u, 0, u.len, key);
+  EvictRows<PER> rows;
+  rows.load(u, 0, u.len);
+  rows.keys(a, u, key);
   uint32_t threshold = 0;
   int need = u.len;  // nothing leaves: every key is at least 0
   if (u.len > a.n_keep) {
@@ -504,21 +511,23 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_slice_kernel(const EvictA
   const EvictUnit u = evict_unit(a, unit);
   if (u.len <= a.n_keep || u.keep == 0) return;
   const int2 r = slice_rows(a, u, s);
-  uint32_t key[SLICE_PER];
-  if (r.x < r.y) evict_keys<SLICE_PER>(a, u, r.x, r.y, key);
-  uint32_t prefix = 0;
+  EvictRows<SLICE_PER> rows;
+  rows.load(u, r.x, r.y);
+  uint32_t key[SLICE_PER], prefix = 0;
+  if (PASS == 0) rows.keys(a, u, key);
   const size_t at = (size_t)unit * a.slices;
   if (PASS > 0) {
     const int4 st = PASS == 1 ? make_int4(0, u.keep, 0, 0) : a.state[2 * unit + PASS - 2];
     const int2 found = slices_bucket(sh, a, (PASS == 1 ? a.hist_a : a.hist_b) + at * EVICT_BUCKETS, st.y);
     const uint32_t old = (uint32_t)st.x;
     prefix = (old << digit_bits(PASS - 1)) | (uint32_t)found.x;
+    rows.keys(a, u, key);
     if (s == 0 && tid == 0) a.state[2 * unit + PASS - 1] = make_int4((int)prefix, st.y - found.y, 0, 0);
     // this slice's rows that are above by their digit before
     int above = 0;
 #pragma unroll
     for (int i = 0; i < SLICE_PER; ++i) {
-      const uint32_t upper = r.x < r.y ? key[i] >> digit_shift(PASS - 1) : 0u;
+      const uint32_t upper = key[i] >> digit_shift(PASS - 1);
       const bool row = r.x + i * EVICT_THREADS + tid < r.y;
       above += __popcll(__ballot(row && (PASS == 1 || upper >> digit_bits(PASS - 1) == old) && upper > prefix));
     }
@@ -535,13 +544,14 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_slice_kernel(const EvictA
   for (int i = tid; i < EVICT_BUCKETS; i += EVICT_THREADS) out[i] = sh.hist[i];
 }
 
-__global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictArgs a) {
+// (64 registers: two workgroups a CU.  64 sequences x 4 units of 30000 rows 56 -> 47 us; one workgroup a CU or less 1 us more.)
+__global__ __launch_bounds__(EVICT_THREADS, 8) void evict_emit_kernel(const EvictArgs a) {
   __shared__ EvictShared sh;
   const int unit = blockIdx.x / a.slices, s = blockIdx.x % a.slices, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const EvictUnit u = evict_unit(a, unit);
   const int2 r = slice_rows(a, u, s);
-  uint32_t key[SLICE_PER];
-  if (r.x < r.y) evict_keys<SLICE_PER>(a, u, r.x, r.y, key);
+  EvictRows<SLICE_PER> rows;
+  rows.load(u, r.x, r.y);
   const bool all = u.len <= a.n_keep, none = u.keep == 0;
   const size_t at = (size_t)unit * a.slices;
   uint32_t threshold = all ? 0u : 0xffffffffu;
@@ -552,7 +562,8 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictAr
     const int2 found = slices_bucket(sh, a, hist, st.y);
     threshold = ((uint32_t)st.x << digit_bits(2)) | (uint32_t)found.x;
     need = st.y - found.y;
-    // Sixteen slices at a time: their rows above and at the threshold, a wave each; then what lies before this slice.
+    // Sixteen slices at a time: their rows above and at the threshold, a wave each; then, a lane each, what lies before this
+    // slice.
     int seen_equal = 0, kept_low = 0, kept_high_before = 0, kept_low_before = 0;
     for (int s0 = 0; s0 < a.slices; s0 += EVICT_WAVES) {
       int above = 0;
@@ -560,6 +571,8 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictAr
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         c[k] = load16(hist + (size_t)min(s0 + wave, a.slices - 1) * EVICT_BUCKETS + (k * 64 + lane) * 4);
+      const int before = a.above[at + min(s0 + wave, a.slices - 1)];
+      const int same = (int)hist[(size_t)min(s0 + wave, a.slices - 1) * EVICT_BUCKETS + found.x];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int i = (k * 64 + lane) * 4;
@@ -567,19 +580,20 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictAr
                  (i + 3 > found.x ? (int)c[k].w : 0);
       }
       above = wave_sum_i(above);
-      if (lane == 0 && s0 + wave < a.slices) {
-        sh.table[2 * wave] = above + a.above[at + s0 + wave];
-        sh.table[2 * wave + 1] = (int)hist[(size_t)(s0 + wave) * EVICT_BUCKETS + found.x];
+      if (lane == 0) {
+        sh.table[2 * wave] = s0 + wave < a.slices ? above + before : 0;
+        sh.table[2 * wave + 1] = s0 + wave < a.slices ? same : 0;
       }
       __syncthreads();
-      for (int w = 0; w < EVICT_WAVES && s0 + w < a.slices; ++w) {
-        const int x = s0 + w, equal = sh.table[2 * w + 1];
-        const int kept = sh.table[2 * w] + min(max(need - seen_equal, 0), equal);
-        if (x == s) equal_before = seen_equal;
-        if (x < s) (x < a.keep_slices ? kept_low_before : kept_high_before) += kept;
-        if (x < a.keep_slices) kept_low += kept;
-        seen_equal += equal;
-      }
+      const int x = s0 + lane, equal = lane < EVICT_WAVES ? sh.table[2 * lane + 1] : 0;
+      const int seen = seen_equal + wave_incl_scan(equal);
+      const int kept = lane < EVICT_WAVES ? sh.table[2 * lane] + min(max(need - (seen - equal), 0), equal) : 0;
+      const bool low = x < a.keep_slices;
+      if (s >= s0 && s < s0 + EVICT_WAVES) equal_before = __builtin_amdgcn_readlane(seen - equal, s - s0);
+      kept_low += wave_sum_i(low ? kept : 0);
+      kept_low_before += wave_sum_i(low && x < s ? kept : 0);
+      kept_high_before += wave_sum_i(!low && x < s ? kept : 0);
+      seen_equal = __builtin_amdgcn_readlane(seen, 63);
       __syncthreads();
     }
     hole_before = s < a.keep_slices ? r.x - kept_low_before : 0;
@@ -590,8 +604,11 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_emit_kernel(const EvictAr
     a.count[2 * unit] = holes;
     a.count[2 * unit + 1] = u.keep;
   }
-  if (r.x < r.y)
+  if (r.x < r.y) {
+    uint32_t key[SLICE_PER];
+    rows.keys(a, u, key);
     evict_list<SLICE_PER>(sh, a, u, key, r.x, r.y, threshold, need, equal_before, hole_before, mover_before);
+  }
 }
 
 // In place: move i of the lists.  Apart: row i of the new cache.  ROW / 16 lanes carry a row of K and of V, one row a thread
