@@ -516,8 +516,11 @@ __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinSha
   State<T, D> st;
   st.init();
   float* z = a.weights_out && c < a.G ? a.z + bh * a.zrow : nullptr;
+  auto leave = [&](int r, const f32x4& x) {
+    if (z) *reinterpret_cast<f32x4*>(z + r) = x;
+  };
   stream_rows<T, D, true>(a.k + unit * a.capacity * row, a.v + unit * a.capacity * row, start + wave * S::KEYS, 4 * S::KEYS, end,
-                          a.scale, q, st, [&](int row, const f32x4& x) { if (z) *reinterpret_cast<f32x4*>(z + row) = x; }, areas.of(wave), lane);
+                          a.scale, q, st, leave, areas.of(wave), lane);
   const size_t at = ((size_t)h * a.pieces + w) * a.G;
   join_waves<T, D>(st, a.G, js, areas, wave, g, c, a.ml + at, a.acc + at * D);
 }
@@ -548,10 +551,11 @@ __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, Join
 // are on their way.  The values' operand comes transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen
 // channels, and each gets the four values of its channel; a read takes two neighbouring chunks of eight rows).
 // The scores of the next step are formed beside the softmax of this one, so that matrix and vector work of a wave do not
-// wait for each other.  Measured (64K rows, 448 query rows per KV head, 60 GFLOP): 130 us.  The card lowers its clock to
-// 1.7 .. 1.8 GHz under this mixture (2.5 GHz in the own rows), and the time follows the work itself: sixteen products fewer a
-// step 24 us, no loads into LDS 14 us, no exponentials 7 us, no LDS reads of the keys or of the values 4 us each, while other
-// orders of the same instructions, a third fewer vector instructions, or two workgroups a CU instead of one change nothing.
+// wait for each other.  Measured (64K rows, 448 query rows per KV head, 62 GFLOP): 121 us, 144 with three numbers a weight.  The
+// card lowers its clock to 1.7 .. 1.8 GHz under this mixture (2.5 GHz in the own rows; products of random numbers alone: 2.0
+// PFLOP/s instead of 2.4), and the time follows the work itself: sixteen products fewer a step 23 us, no loads into LDS 14 us, no
+// exponentials 7 us, no LDS reads of the keys or of the values 4 us each, while other orders of the same instructions, a third
+// fewer vector instructions, or two workgroups a CU instead of one change nothing.
 template <int D>
 struct SharedStep {
   static constexpr int ROWS = 32, ROW = D * 2, CHUNKS = ROW / 16, HALF = ROWS * ROW, BYTES = 2 * HALF;  // keys, then values
@@ -698,9 +702,9 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 // ----------------------------------------------------------------------------
 // Prefix and own rows in one launch: one is bound by the matrix units as soon as it has many query rows, the other by
 // memory.  256 workgroups of the one (all, if there are fewer) and as many of the other alternate, so that a CU has one of
-// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows, measured with three numbers a weight: 174 us; in
-// launches of their own 117 + 71 us, all of the prefix first 180 us, mixed in proportion, which leaves single prefix
-// workgroups for the end, 206.  With two numbers, as it is now: 155 us.)
+// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows: 144 us, 121
+// and 67 alone.  Measured with three numbers a weight, 174 us then: all of the prefix first 180 us; mixed in proportion, which
+// leaves single prefix workgroups for the end, 206.)
 // Tiles of one prefix range are a multiple of 8 workgroups apart, on one XCD, wherever Hkv * splits is one.
 // ----------------------------------------------------------------------------
 struct Role {
@@ -979,8 +983,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
 }
 
 // From this many prefix rows on, and with more query rows than make the prefix a matter of memory, weights are two numbers
-// instead of three: a third fewer products where they are the bound (64K rows, 448 query rows, 160K own rows: 174 -> 157 us).  Outputs are
-// then off by 2.2e-6 of their norm, as an evaluation in fp32 throughout is over so many rows (2.3e-6 at 32K rows, 2.6e-6 at
+// instead of three: a third fewer products where they are the bound (64K rows, 448 query rows, 160K own rows: 162 -> 144 us).
+// Outputs are then off by 2.2e-6 of their norm, as an evaluation in fp32 throughout is over so many rows (2.3e-6 at 32K rows, 2.6e-6 at
 // 64K, but 1.6e-6 at 16K; with three numbers 0.8e-6).
 constexpr int TWO_TERMS_ROWS = 32768;
 
