@@ -34,15 +34,17 @@ struct Turn {
   int one, two;  // the item's chunks
   bool turns;
 
-  // position(axis) of the item's token; a circle is `1` in turns, so the nearest whole number of circles comes off
-  // without error
-  template <typename F>
-  __device__ __forceinline__ void init(const RotaryArgs& r, int item, F&& position) {
+  __device__ __forceinline__ void place(const RotaryArgs& r, int item) {
     const int rotated = r.rot / (2 * EPC);
     turns = item < rotated;
     const bool halves = turns && r.pairing == WAVE_ROTARY_HALVES;
     one = halves ? item : 2 * item;
     two = halves ? item + rotated : 2 * item + 1;
+  }
+  // position(axis) of the item's token; a circle is `1` in turns, so the nearest whole number of circles comes off
+  // without error
+  template <typename F>
+  __device__ __forceinline__ void angles(const RotaryArgs& r, int item, F&& position) {
 #pragma unroll
     for (int e = 0; e < EPC; ++e) {
       c[e] = 1.f;
@@ -117,10 +119,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(const char* x, const int32_
   const int n = tile * sh.tokens + (int)(threadIdx.x / Tu::ITEMS >> sh.lane_shift);
   if (n >= N) return;
   Tu t;
-  t.init(rot, item, [&](int axis) { return coords[((size_t)axis * B + b) * N + n]; });
+  t.place(rot, item);
   const int step = sh.head_groups << sh.lane_shift;
-  for (int h0 = (group << sh.lane_shift) + lane; h0 < H; h0 += TURN_BATCH * step) {
-    uint4 u[TURN_BATCH], v[TURN_BATCH];
+  uint4 u[TURN_BATCH], v[TURN_BATCH];
+  auto load = [&](int h0) {
 #pragma unroll
     for (int k = 0; k < TURN_BATCH; ++k) {
       const int h = min(h0 + k * step, H - 1);
@@ -128,6 +130,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(const char* x, const int32_
       u[k] = load16(row + t.one * 16);
       v[k] = load16(row + t.two * 16);
     }
+  };
+  // the first rows are on their way while the sines are formed
+  int h0 = (group << sh.lane_shift) + lane;
+  load(h0);
+  t.angles(rot, item, [&](int axis) { return coords[((size_t)axis * B + b) * N + n]; });
+  for (; h0 < H;) {
 #pragma unroll
     for (int k = 0; k < TURN_BATCH; ++k)
       if (h0 + k * step < H) {
@@ -136,6 +144,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const char* x, const int32_
         store16(row + t.one * 16, u[k]);
         store16(row + t.two * 16, v[k]);
       }
+    h0 += TURN_BATCH * step;
+    if (h0 < H) load(h0);
   }
 }
 
@@ -177,16 +187,16 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a, const R
   if (n < s.count) {
     Tu t;
     if (ROT) {
-      t.init(rot, item, [&](int axis) { return a.coords ? a.coords[((size_t)axis * a.B + b) * a.n + n] : s.first + n; });
+      t.place(rot, item);
     } else {
       t.turns = false;
       t.one = 2 * item;
       t.two = 2 * item + 1;
     }
     const int step = sh.head_groups << sh.lane_shift;
-    for (int h0 = (group << sh.lane_shift) + lane; h0 < slots; h0 += TURN_BATCH * step) {
-      uint4 u[TURN_BATCH], v[TURN_BATCH];
-      char* to[TURN_BATCH];
+    uint4 u[TURN_BATCH], v[TURN_BATCH];
+    char* to[TURN_BATCH];
+    auto load = [&](int h0) {
 #pragma unroll
       for (int i = 0; i < TURN_BATCH; ++i) {
         const int h = min(h0 + i * step, slots - 1);
@@ -199,6 +209,11 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a, const R
         to[i] = is_q ? a.q_out + at : (is_k ? a.k : a.v) + (unit * a.capacity + row) * ROW;
         if (h0 + i * step >= slots || (!is_q && n >= s.fit)) to[i] = nullptr;
       }
+    };
+    int h0 = (group << sh.lane_shift) + lane;
+    load(h0);
+    if (ROT) t.angles(rot, item, [&](int axis) { return a.coords ? a.coords[((size_t)axis * a.B + b) * a.n + n] : s.first + n; });
+    for (; h0 < slots;) {
 #pragma unroll
       for (int i = 0; i < TURN_BATCH; ++i)
         if (to[i]) {
@@ -206,6 +221,8 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a, const R
           store16(to[i] + t.one * 16, u[i]);
           store16(to[i] + t.two * 16, v[i]);
         }
+      h0 += TURN_BATCH * step;
+      if (h0 < slots) load(h0);
     }
   }
   // positions and weights: the tile's tokens of all units, by the workgroup of the first heads

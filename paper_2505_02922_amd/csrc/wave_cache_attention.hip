@@ -882,13 +882,19 @@ __global__ __launch_bounds__(SHORT_THREADS) void attend_short_kernel(const Atten
 // rows of a unit per workgroup, by the registers that the heads' products take
 constexpr int weight_rows(int G) { return G <= 4 ? 2048 : 1024; }
 
-// The sequence's pieces as the launch before left them: the first one, and how many
+// The sequence's pieces as the launch before left them: the first one, and how many.  (Both loads side by side: a sequence without
+// rows left nothing, and what is read then is not used.)
 struct OwnPieces {
-  int first, count;
+  int first, count, length;
 };
-__device__ __forceinline__ OwnPieces own_pieces(const AttendArgs& a, int b, int length) {
-  const int2 p = length > 0 ? a.info[b] : make_int2(0, 0);
-  return OwnPieces{p.x, p.y};
+__device__ __forceinline__ OwnPieces own_pieces(const AttendArgs& a, int b) {
+  const int length = a.lengths[b];
+  const int2 p = a.info[b];
+  OwnPieces o;
+  o.length = min(max(length, 0), a.capacity);
+  o.first = o.length > 0 ? p.x : 0;
+  o.count = o.length > 0 ? p.y : 0;
+  return o;
 }
 
 template <int D, int G>
@@ -900,7 +906,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
     const int bh = blockIdx.x * 4 + wave;
     if (bh >= heads) return;
     const int b = bh / a.Hq, hq = bh % a.Hq, h = hq / G, gq = hq % G;
-    const OwnPieces own = own_pieces(a, b, cache_length(a.lengths, b, a.capacity));
+    const OwnPieces own = own_pieces(a, b);
     const HeadParts p = head_parts(a, b, h, gq, own.first, own.count);
     const float2 n = normaliser(p);
     constexpr int LANES = D / 4, GROUPS = 64 / LANES;
@@ -927,16 +933,23 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   if ((int)blockIdx.x < a.head_blocks) {
     __shared__ float part[256 / (D / 4)][D];
     const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / G, gq = hq % G;
-    const OwnPieces own = own_pieces(a, b, cache_length(a.lengths, b, a.capacity));
+    const OwnPieces own = own_pieces(a, b);
     const HeadParts p = head_parts(a, b, h, gq, own.first, own.count);
-    const float2 n = normaliser(p);
     constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-    const int lane = tid % LANES, group = tid / LANES;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int i = group; i < p.splits + own.count; i += GROUPS) {
-      const float2 x = p.at(i);
-      const float f = x.x == neg_inf() ? 0.f : exp2f(x.x - n.x);
-      sum += f * *reinterpret_cast<const f32x4*>(p.sum<D>(a, i, b, h, gq, own.first) + lane * 4);
+    const int lane = tid % LANES, group = tid / LANES, parts = p.splits + own.count;
+    // a thread's first partial result is on its way while the normaliser is formed
+    float2 x = {neg_inf(), 0.f};
+    f32x4 v = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
+    auto load = [&](int i) {
+      x = p.at(i);
+      v = *reinterpret_cast<const f32x4*>(p.sum<D>(a, i, b, h, gq, own.first) + lane * 4);
+    };
+    if (group < parts) load(group);
+    const float2 n = normaliser(p);
+    for (int i = group; i < parts;) {
+      sum += (x.x == neg_inf() ? 0.f : exp2f(x.x - n.x)) * v;
+      i += GROUPS;
+      if (i < parts) load(i);
     }
     *reinterpret_cast<f32x4*>(&part[group][lane * 4]) = sum;
     __syncthreads();
@@ -952,7 +965,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   const int chunks = (a.capacity + WEIGHT_ROWS - 1) / WEIGHT_ROWS;
   const int at = blockIdx.x - a.head_blocks, unit = at / chunks, r0 = at % chunks * WEIGHT_ROWS;
   const int b = unit / a.Hkv, h = unit % a.Hkv;
-  const int len = cache_length(a.lengths, b, a.capacity);
+  const OwnPieces own = own_pieces(a, b);
+  const int len = own.length;
   if (r0 >= len) return;
   // the products and the old weights are on their way while the normalisers are formed
   constexpr int PER = WEIGHT_ROWS / 256;
@@ -966,7 +980,6 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
     for (int gq = 0; gq < G; ++gq) zz[gq][i] = z[(size_t)gq * a.zrow + j];
     w[i] = a.decay > 0.f ? a.decay * a.weights[base + j] : 0.f;
   }
-  const OwnPieces own = own_pieces(a, b, len);
   for (int gq = wave; gq < G; gq += 4) {
     const float2 n = normaliser(head_parts(a, b, h, gq, own.first, own.count));
     if ((tid & 63) == 0) norm[gq] = make_float2(n.x == neg_inf() ? 0.f : n.x, n.x == neg_inf() ? 1.f : 1.f / n.y);
