@@ -752,7 +752,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs 
 
 // ----------------------------------------------------------------------------
 // Merge.  The first workgroups join the heads' partial results: one head each, or four, a wave each, where there are many
-// heads with few (256 sequences of 300 rows, 8192 heads: 8 us instead of 16).  With weights, the others have weight_rows(G) rows
+// heads with few (256 sequences of 300 rows, 8192 heads: 8 us instead of 16; 4096 heads with nine each 9 instead of 13).  With weights, the others have weight_rows(G) rows
 // of a unit each: they form the G heads' normalisers from the partial (m, l) again, which is less than waiting for them, and add up
 // the softmax weights.
 // ----------------------------------------------------------------------------
@@ -937,18 +937,26 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
     const HeadParts p = head_parts(a, b, h, gq, own.first, own.count);
     constexpr int LANES = D / 4, GROUPS = 256 / LANES;
     const int lane = tid % LANES, group = tid / LANES, parts = p.splits + own.count;
-    // a thread's first partial result is on its way while the normaliser is formed
-    float2 x = {neg_inf(), 0.f};
-    f32x4 v = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
-    auto load = [&](int i) {
-      x = p.at(i);
-      v = *reinterpret_cast<const f32x4*>(p.sum<D>(a, i, b, h, gq, own.first) + lane * 4);
+    // a thread's first partial results are on their way while the normaliser is formed, and JB of them together (one KV head
+    // with 512 of them: 35 us one by one, 20 so)
+    constexpr int JB = 4;
+    float x[JB];
+    f32x4 v[JB], sum = {0.f, 0.f, 0.f, 0.f};
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int e = 0; e < JB; ++e) {
+        const int i = min(i0 + e * GROUPS, parts - 1);
+        x[e] = p.at(i).x;
+        v[e] = *reinterpret_cast<const f32x4*>(p.sum<D>(a, i, b, h, gq, own.first) + lane * 4);
+      }
     };
     if (group < parts) load(group);
     const float2 n = normaliser(p);
     for (int i = group; i < parts;) {
-      sum += (x.x == neg_inf() ? 0.f : exp2f(x.x - n.x)) * v;
-      i += GROUPS;
+#pragma unroll
+      for (int e = 0; e < JB; ++e)
+        if (i + e * GROUPS < parts) sum += (x[e] == neg_inf() ? 0.f : exp2f(x[e] - n.x)) * v[e];
+      i += JB * GROUPS;
       if (i < parts) load(i);
     }
     *reinterpret_cast<f32x4*>(&part[group][lane * 4]) = sum;
@@ -1035,7 +1043,7 @@ wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
   }
   if (!shared) WAVE_LAUNCH("cache_attend", (attend_rows_kernel<T, D>), blocks, 256, 0, st, a);
   // (on the mean; fewer than 1024 heads leave CUs without work)
-  a.head_waves = a.B * a.Hq >= 1024 && a.splits + g.pieces / a.B <= 8;
+  a.head_waves = a.B * a.Hq >= 1024 && a.splits + g.pieces / a.B <= 16;
   a.head_blocks = a.head_waves ? (a.B * a.Hq + 3) / 4 : a.B * a.Hq;
   switch (a.G) {
 #define WAVE_G(n)                                                                                              \
@@ -1064,14 +1072,21 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
   const int steps = (int)(((long long)P + c.capacity + short_step(c.dtype) - 1) / short_step(c.dtype));
   g.one_launch = steps <= 1 || (steps <= 2 && (c.B * c.Hkv <= 256 || c.B > 512));
   const int M = c.B * G;
-  g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : M <= 64 ? 64 : 128;
+  // Two tiles of columns a wave share its reads of keys and values, and double what a workgroup has to do.  That pays where there
+  // is work for most CUs at the smallest ranges (d = 128: 64 sequences behind 500 rows 16.6 us, with one tile 14.4; behind 8000
+  // 34.8 and 35.7); at d = 64, where a wave has half as much to read, only far beyond (64 x 7 query rows behind 8000 rows 28 us,
+  // 24; 200 x 4 behind 16000 87 and 95) or with two numbers a weight, which are made for two tiles.
+  const long long tiles128 = (long long)c.Hkv * ((M + 127) / 128) * (((long long)P + 127) / 128);
+  const bool wide = M > 64 && (tiles128 >= (c.d == 128 ? 192 : 4096) || P >= TWO_TERMS_ROWS);
+  g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : wide ? 128 : 64;
   g.mtiles = (M + g.mtile - 1) / g.mtile;
   if (P > 0) {
     // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 52 us
     // instead of 57 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory (100K rows, 64 query
-    // rows: 95 us instead of 110).
+    // rows: 95 us instead of 110).  No more than 256 ranges, each of which every head's joining reads (one KV head, 65536 rows:
+    // 28 us with 512, 20).
     const int aim = g.mtile == 128 && c.d == 128 ? 256 : 512;
-    const int want = aim / (c.Hkv * g.mtiles) > 1 ? aim / (c.Hkv * g.mtiles) : 1;
+    const int even = aim / (c.Hkv * g.mtiles) > 1 ? aim / (c.Hkv * g.mtiles) : 1, want = even < 256 ? even : 256;
     const long long rows = ((long long)P + want - 1) / want;
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);

@@ -356,6 +356,29 @@ def test_attention_long_prefix_of_many_query_rows(d, B, P):
     _check_attention("bf16", q, cache, lengths, pk, pv, 1.0, cache.weights, out, lse, w, f"P {P}")
 
 
+@pytest.mark.parametrize("d,B,Hq,Hkv,P", [(128, 33, 8, 2, 1000), (128, 33, 8, 2, 13001), (64, 33, 8, 2, 13001), (64, 64, 64, 8, 13225)])
+def test_attention_prefix_of_many_query_rows(d, B, Hq, Hkv, P):
+    """One and two tiles of columns a wave, weights in three numbers; some of the sequences are looked at."""
+    lengths = [(7 * b) % 30 for b in range(B)]
+    cache, q, pk, pv = _inputs("bf16", B, Hq, Hkv, d, 600, lengths, P, P, 3.0)
+    w = torch.zeros_like(cache.weights)
+    out, lse = wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w, decay=0.25)
+    some = [0, B // 2, B - 1]
+    pick = wb.cache_from_tensors(*(cache.t[n][some].contiguous() for n in ("k", "v", "positions", "weights", "lengths", "tokens")))
+    _check_attention("bf16", q[some], pick, [lengths[b] for b in some], pk, pv, 0.25, pick.weights, out[some], lse[some], w[some])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,Hq,P", [(1, 8, 66000), (3, 2, 40001)])
+def test_attention_of_many_partial_results(dtype, B, Hq, P):
+    """One KV head: as many ranges of the prefix, and pieces of a long sequence, as there may be."""
+    lengths = [30000, 1, 0][:B]
+    cache, q, pk, pv = _inputs(dtype, B, Hq, 1, 64, 30000, lengths, P, P, 2.0)
+    w = torch.zeros_like(cache.weights)
+    out, lse = wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w, decay=0.0)
+    _check_attention(dtype, q, cache, lengths, pk, pv, 0.0, cache.weights, out, lse, w)
+
+
 @pytest.mark.parametrize("B", [2, 8, 20])
 def test_attention_values_that_are_not_finite_show_in_their_channel(B):
     """An infinite value in the last prefix row, and in the last own row: its channel is not finite (a weight is a sum of bf16
