@@ -346,14 +346,13 @@ __device__ __forceinline__ void evict_count(EvictShared& sh, const uint32_t (&ke
   __syncthreads();
 }
 // Given the counts c0, c1 of this thread's buckets 2047 - 2 tid and 2046 - 2 tid: the bucket in which the count from the
-// top reaches `need`, and the count above it.
+// top reaches `need`, and the count above it.  (The answer's place is written again only behind a barrier of what follows.)
 __device__ __forceinline__ int2 evict_bucket(EvictShared& sh, int c0, int c1, int need) {
   const int tid = threadIdx.x, wave = tid >> 6, top = EVICT_BUCKETS - 1 - 2 * tid;
   const int incl = wave_incl_scan(c0 + c1);
   if ((tid & 63) == 63) sh.wave_total[wave] = incl;
   __syncthreads();
-  int before = incl - c0 - c1;
-  for (int w = 0; w < wave; ++w) before += sh.wave_total[w];
+  const int lane = tid & 63, before = incl - c0 - c1 + wave_sum_i(lane < wave ? sh.wave_total[lane & (EVICT_WAVES - 1)] : 0);
   if (before < need && before + c0 >= need) {
     sh.bucket = top;
     sh.above = before;
@@ -362,9 +361,7 @@ __device__ __forceinline__ int2 evict_bucket(EvictShared& sh, int c0, int c1, in
     sh.above = before + c0;
   }
   __syncthreads();
-  const int2 r = make_int2(sh.bucket, sh.above);
-  __syncthreads();
-  return r;
+  return make_int2(sh.bucket, sh.above);
 }
 // Exclusive sums, over (i, wave) in this order, of one number each wave has for every i; all threads call it.
 template <int PER>
