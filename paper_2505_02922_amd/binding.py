@@ -574,8 +574,8 @@ def wave_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, q: Optiona
             raise WaveError(3, where)
         Hq = heads[1]
         if q_out is None:
-            new = torch.empty if counts is None else torch.zeros
-            q_out = new(heads, dtype=dtype, device=q.device)
+            new = torch.empty_like if counts is None else torch.zeros_like
+            q_out = new(q, memory_format=torch.contiguous_format)
         else:
             _as_is(where, q_out, dtype, heads)
         q = q.contiguous()
@@ -636,7 +636,7 @@ def wave_cache_attention_decode(q: torch.Tensor, cache: Cache, prefix_k: Optiona
         prefix_k, prefix_v = prefix_k.contiguous(), prefix_v.contiguous()
     if weights_out is not None:
         _as_is(where, weights_out, torch.float32, (B, cache.Hkv, cache.capacity))
-    out = torch.empty(B, Hq, d, dtype=torch.float32, device=q.device) if out is None else \
+    out = torch.empty_like(q, dtype=torch.float32, memory_format=torch.contiguous_format) if out is None else \
         _as_is(where, out, torch.float32, shape)
     lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if lse is None else \
         _as_is(where, lse, torch.float32, (B, Hq))
