@@ -1091,11 +1091,11 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);
   }
-  // Own rows: as many pieces as are resident, two a CU, four at d = 64 (or half of them, see find_piece).  Six beside a prefix
-  // that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows: 153 us with two,
-  // 149).
+  // Own rows: as many pieces as are resident, two a CU, four at d = 64 (or half of them, see find_piece).  Four beside a prefix
+  // that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows: 158 us with two or
+  // three, 155 with four or six; 32K for 128 and 16K: 56 with up to four, 57 with six; 50K for 192 at d = 64 and 80K: 70 and 76).
   const bool beside = P > 0 && M > 16 && c.Hkv * g.splits * g.mtiles >= 128;
-  const int per_cu = beside ? 6 : c.d == 64 ? 4 : 2;
+  const int per_cu = beside || c.d == 64 ? 4 : 2;
   g.target = per_cu * 256 / c.Hkv > 1 ? per_cu * 256 / c.Hkv : 1;
   const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
   const long long cut = (long long)g.target + (cuts_fit(c.B, g.target) ? 0 : c.B);
