@@ -359,7 +359,8 @@ wave_status wave_rotary_apply(const void *x, const int32_t *coords, const wave_r
  * sequence b are the first lengths[b] of each of its units, in no order that
  * matters; what lies behind them is never read and may hold anything.  The
  * library reads lengths on the device: a value outside 0 .. capacity counts as
- * the nearer of the two. */
+ * the nearer of the two.  Every call returns WAVE_ERR_SHAPE for B * Hkv of 2^21
+ * and more or a capacity above 2^30. */
 typedef struct {
   int32_t dtype;            /* wave_dtype                                              */
   int32_t B, Hkv, d;
@@ -394,7 +395,9 @@ typedef struct {
  *                 otherwise; tokens_out may be NULL where cache->tokens is.
  * cache->positions, weights and tokens may be NULL (positions and NULL coords
  * need tokens).  The caller keeps lengths[b] + counts[b] <= capacity: rows that
- * do not fit are left out, and lengths and tokens advance by those that did. */
+ * do not fit are left out, and lengths and tokens advance by those that did.
+ * WAVE_ERR_SHAPE: n_new above 2^30, B * n_new of 2^31 and more, B * Hq of 2^24
+ * and more. */
 wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const void *v_new, const void *q,
                               int Hq, int n_new, const int32_t *counts, const wave_rotary *rotary,
                               const int32_t *coords, void *q_out, int32_t *lengths_out,
@@ -422,7 +425,9 @@ wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const 
  * that more than 64 query rows per KV head (B * Hq / Hkv) share, the prefix's
  * weights as two, which hold 17 (a weight is then off by at most 2^-17 of itself).
  * A value that is infinite or no number makes its channel of every head that
- * attends to its row one or the other. */
+ * attends to its row one or the other.
+ * WAVE_ERR_SHAPE: Hq / Hkv not a whole number in 1 .. 8, P above 2^30, or
+ * B * Hq + B * Hkv * ceil(capacity / 1024) of 2^24 and more. */
 size_t wave_cache_attention_workspace(const wave_cache *cache, int Hq, int P, int accumulate);
 wave_status wave_cache_attention_decode(const void *q, int Hq, const wave_cache *cache,
                                         const void *prefix_k, const void *prefix_v, int P, float decay,
@@ -445,6 +450,8 @@ wave_status wave_cache_attention_decode(const void *q, int Hq, const wave_cache 
  *                 capacity, others must not overlap.  to->capacity >= min(n_keep,
  *                 from->capacity).  Rows behind the new length are left as they are
  *   n_sink + n_local <= n_keep (WAVE_ERR_ARG otherwise)
+ *   (WAVE_ERR_SHAPE also where 64 GiB of keys and more may be written: B * Hkv * (rows * bytes of a row / 4096 + 1)
+ *   of 2^24 and more, rows = min(n_keep, capacity - n_keep) in place and n_keep into other arrays)
  *   workspace     DEVICE, 256-byte aligned, >= wave_cache_evict_workspace(...) */
 size_t wave_cache_evict_workspace(const wave_cache *from, int n_keep);
 wave_status wave_cache_evict(const wave_cache *from, const wave_cache *to, int n_keep, int n_sink,

@@ -635,7 +635,7 @@ wave_status wave_cache_append(const wave_cache* cache, const void* k_new, const 
         (q && overlaps(coords, xb, q_out, (size_t)c.B * Hq * n_new * c.d * es)))
       return WAVE_ERR_ARG;
   }
-  if ((long long)c.B * (((long long)n_new + 31) / 32) >= kMaxGrid) return WAVE_ERR_SHAPE;
+  if ((long long)c.B * n_new >= (1ll << 31)) return WAVE_ERR_SHAPE;
   return launch_cache_append(c, k_new, v_new, q, q ? Hq : 0, n_new, counts, rotary ? &rot : nullptr, coords, q_out,
                              lengths_out, tokens_out, static_cast<hipStream_t>(hip_stream));
 }

@@ -113,11 +113,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(const char* x, const int32_
                                                      int tiles, char* y) {
   typedef Turn<T, D> Tu;
   constexpr size_t ROW = D * sizeof(T);
-  const int group = blockIdx.x % sh.head_groups, bt = blockIdx.x / sh.head_groups;
+  const unsigned block = workgroup_number();
+  const int group = block % sh.head_groups, bt = block / sh.head_groups;
   const int b = bt / tiles, tile = bt % tiles;
   const int item = threadIdx.x % Tu::ITEMS, lane = (threadIdx.x / Tu::ITEMS) & ((1 << sh.lane_shift) - 1);
   const int n = tile * sh.tokens + (int)(threadIdx.x / Tu::ITEMS >> sh.lane_shift);
-  if (n >= N) return;
+  if (b >= B || n >= N) return;
   Tu t;
   t.place(rot, item);
   const int step = sh.head_groups << sh.lane_shift;
@@ -178,8 +179,10 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a, const R
                                                      bool advance) {
   typedef Turn<T, D> Tu;
   constexpr size_t ROW = D * sizeof(T);
-  const int group = blockIdx.x % sh.head_groups, bt = blockIdx.x / sh.head_groups;
+  const unsigned block = workgroup_number();
+  const int group = block % sh.head_groups, bt = block / sh.head_groups;
   const int b = bt / tiles, tile = bt % tiles;
+  if (b >= a.B) return;
   const int item = threadIdx.x % Tu::ITEMS, lane = (threadIdx.x / Tu::ITEMS) & ((1 << sh.lane_shift) - 1);
   const int n = tile * sh.tokens + (int)(threadIdx.x / Tu::ITEMS >> sh.lane_shift);
   const Share s = append_share(a, b);
@@ -665,9 +668,8 @@ wave_status rotary_td(const void* x, const int32_t* coords, const RotaryArgs& ro
                       hipStream_t st) {
   const TurnShape sh = turn_shape<Turn<T, D>::ITEMS>(N, B, H);
   const int tiles = (N + sh.tokens - 1) / sh.tokens;
-  const long long grid = (long long)B * tiles * sh.head_groups;
-  if (grid >= (1ll << 24)) return WAVE_ERR_SHAPE;
-  WAVE_LAUNCH("rotary", (rotary_kernel<T, D>), (unsigned)grid, 256, 0, st, static_cast<const char*>(x), coords, rot, B, H,
+  const dim3 grid = grid_rows((long long)B * tiles * sh.head_groups);
+  WAVE_LAUNCH("rotary", (rotary_kernel<T, D>), grid, 256, 0, st, static_cast<const char*>(x), coords, rot, B, H,
               N, sh, tiles, static_cast<char*>(y));
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }
@@ -676,16 +678,15 @@ template <typename T, int D>
 wave_status append_td(const AppendArgs& a, const RotaryArgs* rot, hipStream_t st) {
   const TurnShape sh = turn_shape<Turn<T, D>::ITEMS>(a.n, a.B, a.Hq + 2 * a.Hkv);
   const int tiles = (a.n + sh.tokens - 1) / sh.tokens;
-  const long long grid = (long long)a.B * tiles * sh.head_groups;
-  if (grid >= (1ll << 24)) return WAVE_ERR_SHAPE;
+  const dim3 grid = grid_rows((long long)a.B * tiles * sh.head_groups);
   // Numbers that go into the arrays that they come from wait for the readers: a workgroup that is alone with its
   // sequence knows, otherwise a launch of its own writes them.
   const bool in_place = a.lengths_out == a.lengths || (a.tokens_out && a.tokens_out == a.tokens);
   const bool advance = !in_place || tiles * sh.head_groups == 1;
   if (rot)
-    WAVE_LAUNCH("append", (append_kernel<T, D, true>), (unsigned)grid, 256, 0, st, a, *rot, sh, tiles, advance);
+    WAVE_LAUNCH("append", (append_kernel<T, D, true>), grid, 256, 0, st, a, *rot, sh, tiles, advance);
   else
-    WAVE_LAUNCH("append", (append_kernel<T, D, false>), (unsigned)grid, 256, 0, st, a, RotaryArgs{}, sh, tiles, advance);
+    WAVE_LAUNCH("append", (append_kernel<T, D, false>), grid, 256, 0, st, a, RotaryArgs{}, sh, tiles, advance);
   if (!advance) WAVE_LAUNCH("advance", advance_kernel, (a.B + 255) / 256, 256, 0, st, a);
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }

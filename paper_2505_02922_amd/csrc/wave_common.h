@@ -230,6 +230,15 @@ extern bool g_profile_on;
     if (::wave::g_profile_on) ::wave::profile_after(stream);                           \
   } while (0)
 
+// Workgroups by the billion: one launch dimension has fewer than 2^32 threads, so beyond a row of them the grid has rows.  A
+// kernel takes its number from workgroup_number() and leaves where there is no such piece of work (the last row is whole).
+constexpr unsigned GRID_ROW = 1u << 22;
+inline dim3 grid_rows(long long workgroups) {
+  if (workgroups <= (long long)GRID_ROW) return dim3((unsigned)workgroups);
+  return dim3(GRID_ROW, (unsigned)((workgroups + GRID_ROW - 1) / GRID_ROW));
+}
+__device__ __forceinline__ unsigned workgroup_number() { return blockIdx.y * GRID_ROW + blockIdx.x; }
+
 // Launch geometry of one decode step; shared by wave_index_plan (workspace
 // size) and wave_attention_decode (launches) so the two always agree.
 struct DecodeGeom {

@@ -242,6 +242,44 @@ def test_binding_refuses_shapes_and_types():
         assert e.value.status == status
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="made-up addresses: the launch has to fail")
+def test_documented_sizes_reach_the_launch():
+    """Sizes up to the documented limits are not refused: without a GPU the launch is what fails."""
+    HIP = 6
+    L = wb.lib()
+    r = wb.wave_rotary_plan(64, 1e4)
+    x, coords = 1 << 44, 1 << 40
+    for B, H, N, d, dt in [(1 << 24, 1, 1, 64, 1), ((1 << 31) - 1, 1, 1, 64, 1), (1, 1, 1 << 30, 64, 1), (1, 1, 1 << 30, 128, 0),
+                           (1, 1 << 30, 1, 64, 0), (2, 1, 1 << 29, 64, 0), ((1 << 24) - 1, 1, 1, 64, 1)]:
+        assert L.wave_rotary_apply(x, coords, ctypes.byref(r), dt, B, H, N, d, x, None) == HIP, (B, H, N, d, dt)
+    for B, n, Hkv, d, dt in [(1, 1 << 30, 1, 64, 1), (1, 1 << 30, 1, 128, 0), ((1 << 21) - 1, 1, 1, 64, 1), (2, (1 << 30) - 1, 1, 64, 1),
+                             (1 << 18, 4096, 7, 64, 1)]:
+        c = _cache(dtype=dt, B=B, Hkv=Hkv, d=d, capacity=8, base=1 << 30)
+        assert L.wave_cache_append(ctypes.byref(c), x, x, None, 0, n, None, ctypes.byref(r), coords, None, c.lengths, c.tokens,
+                                   None) == HIP, (B, n, Hkv, d, dt)
+    c = _cache(B=1, Hkv=1, d=128, capacity=1 << 30, base=1 << 30)
+    for n_keep, status in ((1 << 29, SHAPE), (1 << 28, SHAPE), ((1 << 28) - 16, SHAPE), ((1 << 28) - 17, HIP), (100, HIP), ((1 << 30) - 100, HIP)):
+        ws = L.wave_cache_evict_workspace(ctypes.byref(c), n_keep)
+        assert ws > 0 and L.wave_cache_evict(ctypes.byref(c), ctypes.byref(c), n_keep, 0, 0, 1 << 45, ws, None) == status, n_keep
+
+
+def test_sizes_beyond_the_documented_limits():
+    L = wb.lib()
+    r = wb.wave_rotary_plan(64, 1e4)
+    x, coords = 1 << 44, 1 << 40
+    for B, H, N in [(1 << 30, 2, 1), (1 << 30, 1, 2), (1, (1 << 30) + 1, 1), (1, 1, (1 << 30) + 1)]:
+        assert L.wave_rotary_apply(x, coords, ctypes.byref(r), 1, B, H, N, 64, x, None) == SHAPE, (B, H, N)
+    c = _cache(B=2, Hkv=1, capacity=8, base=1 << 30)
+    append = lambda n, Hq: L.wave_cache_append(ctypes.byref(c), x, x, x if Hq else None, Hq, n, None, ctypes.byref(r), coords,
+                                               x if Hq else None, c.lengths, c.tokens, None)
+    assert append(1 << 30, 0) == SHAPE and append((1 << 30) + 1, 0) == SHAPE and append(1, 1 << 23) == SHAPE
+    for bad in (_cache(B=1 << 20, Hkv=2, capacity=8), _cache(B=1, Hkv=1, capacity=(1 << 30) + 1)):
+        assert L.wave_cache_attention_workspace(ctypes.byref(bad), 2, 0, 0) == 0 and L.wave_cache_evict_workspace(ctypes.byref(bad), 4) == 0
+    for B, cap, most in ((1 << 20, 1, True), ((1 << 20) - 1, 8 * 1024, True), (1 << 20, 8 * 1024, False), ((1 << 21) - 1, 1, False)):
+        c = _cache(B=B, Hkv=1, capacity=cap)
+        assert (L.wave_cache_attention_workspace(ctypes.byref(c), 8, 0, 0) > 0) == most, (B, cap)
+
+
 # --------------------------------------------------------------------------- pins of the plain statement
 def test_turn_by_hand_and_its_laws():
     axis, freq = [0, 1], [math.pi / 2, math.pi / 6]

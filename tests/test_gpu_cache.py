@@ -140,6 +140,19 @@ def test_rotary_gradient(d, rot, sections, order, pairing):
         assert abs(float(got[b, h, n, c]) - change) <= 9 * U * size[b, h, n, c] + 1e-11, (b, h, n, c)
 
 
+@pytest.mark.parametrize("N", [1, 2])
+def test_rotary_of_more_workgroups_than_a_launch_row(N):
+    """Tokens flattened into the batch, and pairs of them: the same rows as one long sequence, which takes few workgroups."""
+    B = (1 << 24) + 3
+    x = torch.randn(B, 1, N, 64, device="cuda", dtype=torch.bfloat16)
+    coords = torch.randint(0, 1 << 20, (1, B, N), device="cuda", dtype=torch.int32)
+    r = wb.wave_rotary_plan(48, 1e4, None, 0, 1)
+    want = wb.wave_rotary_apply(x.view(1, 1, B * N, 64), coords.view(1, 1, B * N), r)
+    got = wb.wave_rotary_apply(x, coords, r)
+    assert _same_bits(got.view(-1), want.view(-1))
+    assert wb.wave_rotary_apply(x, coords, r, out=x) is x and _same_bits(x.view(-1), want.view(-1))
+
+
 # --------------------------------------------------------------------------- append
 def _filled_cache(dtype, B, Hkv, d, cap, lengths, seed):
     """A cache whose rows behind the lengths hold no numbers."""
