@@ -417,7 +417,9 @@ wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const 
  *                 otherwise; rows behind the length are left as they are.  decay in
  *                 0 .. 1; with 0 the old weights are not read
  *   out           DEVICE [B,Hq,d] fp32;  lse DEVICE [B,Hq] fp32 (natural log)
- *   workspace     DEVICE, 256-byte aligned, >= wave_cache_attention_workspace(...)
+ *   workspace     DEVICE, 256-byte aligned, >= wave_cache_attention_workspace(...);
+ *                 what a longer prefix, a larger capacity or accumulate = 1 needs is
+ *                 enough for a shorter one, a smaller one and accumulate = 0
  * A sequence with neither prefix nor own rows has out = 0 and lse = -infinity.
  * Scores are exact products of the stored values, summed in fp32; the softmax and
  * all sums are fp32.  For bf16 caches a softmax weight meets the values as three

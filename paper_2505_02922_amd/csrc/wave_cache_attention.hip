@@ -1062,6 +1062,37 @@ wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
 
 }  // namespace
 
+// How a prefix is cut where `mtile` of its M query rows go together: workgroups side by side, and the ranges aimed at.
+struct PrefixCut {
+  int mtiles, want;
+};
+static PrefixCut prefix_cut(const wave_cache& c, int M, int mtile) {
+  const int mtiles = (M + mtile - 1) / mtile;
+  // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 52 us
+  // instead of 57 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory (100K rows, 64 query
+  // rows: 95 us instead of 110).  No more than 256 ranges, each of which every head's joining reads (one KV head, 65536 rows:
+  // 28 us with 512, 20).
+  const int aim = mtile == 128 && c.d == 128 ? 256 : 512;
+  const int even = aim / (c.Hkv * mtiles) > 1 ? aim / (c.Hkv * mtiles) : 1;
+  return PrefixCut{mtiles, even < 256 ? even : 256};
+}
+// Pieces of own rows aimed at, as many as are resident: two a CU, four at d = 64 (or half of them, see find_piece).  Four beside
+// a prefix that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows: 158 us with
+// two or three, 155 with four or six; 32K for 128 and 16K: 56 with up to four, 57 with six; 50K for 192 at d = 64 and 80K: 70
+// and 76).
+static bool binds(const wave_cache& c, int M, const PrefixCut& cut, long long splits) {
+  return M > 16 && c.Hkv * splits * cut.mtiles >= 128;
+}
+static int pieces_aimed_at(const wave_cache& c, bool beside) {
+  const int per_cu = beside || c.d == 64 ? 4 : 2;
+  return per_cu * 256 / c.Hkv > 1 ? per_cu * 256 / c.Hkv : 1;
+}
+static int pieces_at_most(const wave_cache& c, int target) {
+  const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
+  const long long cut = (long long)target + (cuts_fit(c.B, target) ? 0 : c.B);
+  return (int)(cut < most ? cut : most);
+}
+
 CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool accumulate) {
   CacheAttendGeom g{};
   const int G = Hq / c.Hkv;
@@ -1078,37 +1109,38 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
   // 24; 200 x 4 behind 16000 87 and 95) or with two numbers a weight, which are made for two tiles.
   const long long tiles128 = (long long)c.Hkv * ((M + 127) / 128) * (((long long)P + 127) / 128);
   const bool wide = M > 64 && (tiles128 >= (c.d == 128 ? 192 : 4096) || P >= TWO_TERMS_ROWS);
-  g.mtile = M <= 16 || c.dtype == WAVE_F32 ? 16 : wide ? 128 : 64;
-  g.mtiles = (M + g.mtile - 1) / g.mtile;
+  const int narrow = M <= 16 || c.dtype == WAVE_F32 ? 16 : 64, widest = narrow == 64 && M > 64 ? 128 : narrow;
+  g.mtile = wide ? widest : narrow;
+  const PrefixCut cut = prefix_cut(c, M, g.mtile);
+  g.mtiles = cut.mtiles;
   if (P > 0) {
-    // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 52 us
-    // instead of 57 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory (100K rows, 64 query
-    // rows: 95 us instead of 110).  No more than 256 ranges, each of which every head's joining reads (one KV head, 65536 rows:
-    // 28 us with 512, 20).
-    const int aim = g.mtile == 128 && c.d == 128 ? 256 : 512;
-    const int even = aim / (c.Hkv * g.mtiles) > 1 ? aim / (c.Hkv * g.mtiles) : 1, want = even < 256 ? even : 256;
-    const long long rows = ((long long)P + want - 1) / want;
+    const long long rows = ((long long)P + cut.want - 1) / cut.want;
     g.prefix_rows = (int)((rows + 127) / 128 * 128);
     g.splits = (int)(((long long)P + g.prefix_rows - 1) / g.prefix_rows);
   }
-  // Own rows: as many pieces as are resident, two a CU, four at d = 64 (or half of them, see find_piece).  Four beside a prefix
-  // that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows: 158 us with two or
-  // three, 155 with four or six; 32K for 128 and 16K: 56 with up to four, 57 with six; 50K for 192 at d = 64 and 80K: 70 and 76).
-  const bool beside = P > 0 && M > 16 && c.Hkv * g.splits * g.mtiles >= 128;
-  const int per_cu = beside || c.d == 64 ? 4 : 2;
-  g.target = per_cu * 256 / c.Hkv > 1 ? per_cu * 256 / c.Hkv : 1;
-  const long long most = (long long)c.B * (((long long)c.capacity + 127) / 128);
-  const long long cut = (long long)g.target + (cuts_fit(c.B, g.target) ? 0 : c.B);
-  g.pieces = (int)(cut < most ? cut : most);
+  const bool beside = P > 0 && binds(c, M, cut, g.splits);
+  g.target = pieces_aimed_at(c, beside);
+  g.pieces = pieces_at_most(c, g.target);
   g.few = beside ? 0 : g.target / 2;
+  // The workspace has room for every shorter prefix too, which may have more ranges than this one (they are whole steps of 128
+  // rows), another tile of columns, and with it more pieces of own rows.
+  int room_splits = 0, room_pieces = pieces_at_most(c, pieces_aimed_at(c, false));
+  for (int mtile : {narrow, widest}) {
+    if (P == 0) break;
+    const PrefixCut x = prefix_cut(c, M, mtile);
+    const int ranges = (int)(((long long)P + 127) / 128), splits = x.want < ranges ? x.want : ranges;
+    if (splits > room_splits) room_splits = splits;
+    const int pieces = pieces_at_most(c, pieces_aimed_at(c, binds(c, M, x, splits)));
+    if (pieces > room_pieces) room_pieces = pieces;
+  }
   g.zrow = (c.capacity + 31) / 32 * 32;  // whole steps
   size_t o = 0;
   g.off_info = o;  o = align_up(o + sizeof(int32_t) * 2 * (size_t)c.B);
   g.off_z = o;     o = align_up(o + (accumulate ? sizeof(float) * (size_t)c.B * Hq * g.zrow : 0));
-  g.off_ml = o;    o = align_up(o + sizeof(float) * 2 * (size_t)Hq * g.pieces);
-  g.off_acc = o;   o = align_up(o + sizeof(float) * c.d * (size_t)Hq * g.pieces);
-  g.off_pml = o;   o = align_up(o + sizeof(float) * 2 * (size_t)c.B * Hq * g.splits);
-  g.off_pacc = o;  o = align_up(o + sizeof(float) * c.d * (size_t)c.B * Hq * g.splits);
+  g.off_ml = o;    o = align_up(o + sizeof(float) * 2 * (size_t)Hq * room_pieces);
+  g.off_acc = o;   o = align_up(o + sizeof(float) * c.d * (size_t)Hq * room_pieces);
+  g.off_pml = o;   o = align_up(o + sizeof(float) * 2 * (size_t)c.B * Hq * room_splits);
+  g.off_pacc = o;  o = align_up(o + sizeof(float) * c.d * (size_t)c.B * Hq * room_splits);
   g.total = o;
   return g;
 }

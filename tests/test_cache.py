@@ -175,6 +175,19 @@ def test_attention_workspace_of_a_larger_cache_is_enough(B, Hkv, G):
     assert all(a <= b for a, b in zip(by_rows, by_rows[1:])) and by_rows[0] > 0
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,Hkv,G,cap", [(8, 8, 4, 2048), (3, 2, 4, 256), (1, 1, 1, 1), (64, 4, 7, 4352), (200, 2, 8, 100), (60, 8, 1, 700),
+                                         (13, 7, 5, 90000), (1000, 8, 8, 200)])
+def test_attention_workspace_of_a_longer_prefix_is_enough(dtype, d, B, Hkv, G, cap):
+    c = _cache(dtype=dtype, B=B, Hkv=Hkv, d=d, capacity=cap)
+    lengths = sorted(set(list(range(0, 1100, 17)) + [128 * i + j for i in range(1, 700, 3) for j in (-1, 0, 1)]
+                         + [32766, 32767, 32768, 32893, 65536, 65537, 100000, 1 << 20, 1 << 30]))
+    for accumulate in (0, 1):
+        need = [wb.lib().wave_cache_attention_workspace(ctypes.byref(c), Hkv * G, P, accumulate) for P in lengths]
+        assert all(a <= b for a, b in zip(need, need[1:])) and need[0] > 0, (accumulate, [p for p, a, b in zip(lengths, need, need[1:]) if a > b])
+
+
 def test_evict_refuses():
     L = wb.lib()
     c, d = _cache(), _cache(base=0x4000000)

@@ -407,6 +407,17 @@ def test_attention_values_that_are_not_finite_show_in_their_channel(B):
     assert _same_bits(out[..., keep], good[..., keep]) and _same_bits(out[1:, :, 9], good[1:, :, 9])
 
 
+def test_attention_with_the_workspace_of_the_longest_prefix():
+    """One workspace, asked for once, for prefixes of fewer rows (which are cut into more ranges) and of none."""
+    cache, q, pk, pv = _inputs("bf16", 8, 32, 8, 128, 2048, [7 * b for b in range(8)], 8255, 4)
+    ws = wb.workspace(wb.wave_cache_attention_workspace(cache, 32, 8255, True))
+    for P in (8255, 8128, 1000, 129, 1, 0):
+        k, v = (x[:, :P].contiguous() if P else None for x in (pk, pv))
+        out, lse = wb.wave_cache_attention_decode(q, cache, k, v, ws=ws)
+        own = wb.wave_cache_attention_decode(q, cache, k, v)
+        assert _same_bits(out, own[0]) and _same_bits(lse, own[1]), P
+
+
 def test_attention_without_rows_anywhere():
     cache, q, _, _ = _inputs("bf16", 3, 4, 2, 128, 16, [0, 0, 0], 0, 5)
     w = torch.full_like(cache.weights, 2.0)
