@@ -416,7 +416,8 @@ wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const 
  *                 the normaliser).  May be cache->weights, and must not overlap it
  *                 otherwise; rows behind the length are left as they are.  decay in
  *                 0 .. 1; with 0 the old weights are not read
- *   out           DEVICE [B,Hq,d] fp32;  lse DEVICE [B,Hq] fp32 (natural log)
+ *   out           DEVICE [B,Hq,d] fp32;  lse DEVICE [B,Hq] fp32 (natural log); they and
+ *                 weights_out need no more than the alignment of a float
  *   workspace     DEVICE, 256-byte aligned, >= wave_cache_attention_workspace(...);
  *                 what a longer prefix, a larger capacity or accumulate = 1 needs is
  *                 enough for a shorter one, a smaller one and accumulate = 0

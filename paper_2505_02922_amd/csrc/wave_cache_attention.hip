@@ -14,6 +14,8 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+// four floats of a caller's array of floats, which need not lie on 16 bytes (one store all the same)
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_of_floats;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -925,7 +927,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
       f32x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = n.x == neg_inf() ? 0.f : sum[e] / n.y;
-      *reinterpret_cast<f32x4*>(a.out + (size_t)bh * D + lane * 4) = o;
+      *reinterpret_cast<f32x4_of_floats*>(a.out + (size_t)bh * D + lane * 4) = o;
     }
     if ((tid & 63) == 0) a.lse[bh] = n.x == neg_inf() ? neg_inf() : (n.x + log2f(n.y)) * kLn2;
     return;

@@ -418,6 +418,22 @@ def test_attention_with_the_workspace_of_the_longest_prefix():
         assert _same_bits(out, own[0]) and _same_bits(lse, own[1]), P
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,cap", [(3, 8, 2, 20), (3, 8, 2, 700), (64, 32, 4, 700)])
+def test_attention_into_outputs_that_lie_on_floats(B, Hq, Hkv, cap):
+    """Outputs a float behind a 16-byte line: one launch, a workgroup and a wave a head in the joining."""
+    lengths = [(5 * b) % (cap + 1) for b in range(B)]
+    cache, q, pk, pv = _inputs("bf16", B, Hq, Hkv, 64, cap, lengths, 100, 6)
+    want = wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=torch.zeros_like(cache.weights), decay=0.0)
+    w0 = torch.full_like(cache.weights, -3.0)
+    wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w0, decay=0.0)
+    for shift in (1, 2, 3):
+        room = lambda *shape: torch.full((math.prod(shape) + 4,), -3.0, device="cuda")[shift:shift + math.prod(shape)].view(*shape)
+        out, lse, w = room(B, Hq, 64), room(B, Hq), room(*cache.weights.shape)
+        assert out.data_ptr() % 16 == 4 * shift
+        wb.wave_cache_attention_decode(q, cache, pk, pv, weights_out=w, decay=0.0, out=out, lse=lse)
+        assert _same_bits(out, want[0]) and _same_bits(lse, want[1]) and _same_bits(w, w0), shift
+
+
 def test_attention_without_rows_anywhere():
     cache, q, _, _ = _inputs("bf16", 3, 4, 2, 128, 16, [0, 0, 0], 0, 5)
     w = torch.full_like(cache.weights, 2.0)
