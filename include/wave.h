@@ -424,9 +424,7 @@ wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const 
  * A sequence with neither prefix nor own rows has out = 0 and lse = -infinity.
  * Scores are exact products of the stored values, summed in fp32; the softmax and
  * all sums are fp32.  For bf16 caches a softmax weight meets the values as three
- * bf16 numbers that hold all its bits; behind a prefix of 32768 rows or more
- * that more than 64 query rows per KV head (B * Hq / Hkv) share, the prefix's
- * weights as two, which hold 17 (a weight is then off by at most 2^-17 of itself).
+ * bf16 numbers that hold all its bits.
  * A value that is infinite or no number makes its channel of every head that
  * attends to its row one or the other.
  * WAVE_ERR_SHAPE: Hq / Hkv not a whole number in 1 .. 8, P above 2^30, or

@@ -23,12 +23,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 // then at most 2^8, far from the end of any type here, and most steps leave the accumulators alone.
 constexpr float kSlack = 8.f;
 
-// the nearest bf16 numbers, x in the lower half
-__device__ __forceinline__ uint32_t nearest_pair(float x, float y) {
-  typedef __attribute__((ext_vector_type(2))) float f32x2;
-  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
-}
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xff800000u); }
 
 // ----------------------------------------------------------------------------
@@ -159,38 +153,26 @@ struct Step<bf16_t, D> {
     }
     return r;
   }
-  // TERMS 3: a weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the
-  // product with the values loses nothing.  TERMS 2: the nearest bf16 number and the nearest to what that left: 17 bits.
-  template <int TERMS>
+  // A weight's 24 bits as three bf16 numbers of eight, cut off from the top: their sum is the weight, so the product with the
+  // values loses nothing.  (Two numbers, a third fewer products, keep 17 bits: with one heavy row behind a lighter one the output
+  // is then off by 2^-18 of itself, sixty times what fp32 loses.)
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
-    bf16x8 w[TERMS];
-    if constexpr (TERMS == 3) {
-      uint32_t u[3][4];
+    uint32_t u[3][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float x = p[2 * j], y = p[2 * j + 1];
+    for (int j = 0; j < 4; ++j) {
+      float x = p[2 * j], y = p[2 * j + 1];
 #pragma unroll
-        for (int n = 0; n < 3; ++n) {
-          u[n][j] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
-          x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-          y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
-        }
+      for (int n = 0; n < 3; ++n) {
+        u[n][j] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+        x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
       }
-#pragma unroll
-      for (int n = 0; n < 3; ++n) w[n] = __builtin_bit_cast(bf16x8, make_uint4(u[n][0], u[n][1], u[n][2], u[n][3]));
-    } else {
-      uint32_t u[2][4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x = p[2 * j], y = p[2 * j + 1];
-        u[0][j] = nearest_pair(x, y);
-        u[1][j] = nearest_pair(x - __uint_as_float(u[0][j] << 16), y - __uint_as_float(u[0][j] & 0xffff0000u));
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) w[n] = __builtin_bit_cast(bf16x8, make_uint4(u[n][0], u[n][1], u[n][2], u[n][3]));
     }
+    bf16x8 w[3];
 #pragma unroll
-    for (int n = TERMS - 1; n >= 0; --n)
+    for (int n = 0; n < 3; ++n) w[n] = __builtin_bit_cast(bf16x8, make_uint4(u[n][0], u[n][1], u[n][2], u[n][3]));
+#pragma unroll
+    for (int n = 2; n >= 0; --n)
 #pragma unroll
       for (int a = 0; a < CH; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[a], w[n], o[a], 0, 0, 0);
   }
@@ -258,7 +240,6 @@ struct Step<float, D> {
     for (int i = 0; i < 4; ++i) s[i] = (a[0][i] + a[1][i]) + (a[2][i] + a[3][i]);
   }
   static __device__ __forceinline__ Vt transpose(const V& v) { return v; }
-  template <int>
   static __device__ __forceinline__ void accumulate(const Vt& v, const float (&p)[NS], f32x4 (&o)[ACC]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -358,7 +339,7 @@ __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0
     v = S::template load_v<ONCE>(step_rows<ROW>(V, next, last), g, c);
     __builtin_amdgcn_sched_barrier(0);
     st.weigh(s, scale);
-    S::template accumulate<3>(vt, s, st.o);
+    S::accumulate(vt, s, st.o);
     if (next >= end) break;
     k0 = next;
   }
@@ -553,7 +534,7 @@ __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, Join
 // are on their way.  The values' operand comes transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen
 // channels, and each gets the four values of its channel; a read takes two neighbouring chunks of eight rows).
 // The scores of the next step are formed beside the softmax of this one, so that matrix and vector work of a wave do not
-// wait for each other.  Measured (64K rows, 448 query rows per KV head, 62 GFLOP): 121 us, 144 with three numbers a weight.  The
+// wait for each other.  Measured (64K rows, 448 query rows per KV head, 62 GFLOP): 144 us.  The
 // card lowers its clock to 1.7 .. 1.8 GHz under this mixture (2.5 GHz in the own rows; products of random numbers alone: 2.0
 // PFLOP/s instead of 2.4), and the time follows the work itself: sixteen products fewer a step 23 us, no loads into LDS 14 us, no
 // exponentials 7 us, no LDS reads of the keys or of the values 4 us each, while other orders of the same instructions, a third
@@ -570,7 +551,7 @@ struct SharedStep {
   }
 };
 
-template <int D, int MQ, int TERMS>
+template <int D, int MQ>
 __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, char* ring0, char* ring1, char* ring2, char* ring3) {
   typedef Step<bf16_t, D> S;
   typedef SharedStep<D> L;
@@ -653,7 +634,7 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 #pragma unroll
     for (int t = 0; t < MQ; ++t) S::scores(k, q[t], s[t]);
 #pragma unroll
-    for (int t = 0; t < MQ; ++t) S::template accumulate<TERMS>(v, p[t], st[t].o);
+    for (int t = 0; t < MQ; ++t) S::accumulate(v, p[t], st[t].o);
   };
   for (int n = 0;; n += 4) {
     if (n >= full) break;
@@ -682,7 +663,7 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 #pragma unroll
     for (int t = 0; t < MQ; ++t) {
       st[t].weigh(s[t], a.scale);
-      S::template accumulate<TERMS>(v, s[t], st[t].o);
+      S::accumulate(v, s[t], st[t].o);
     }
   }
   wait_for_loads<0>();  // none may write LDS behind the end of the workgroup
@@ -705,7 +686,7 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 // Prefix and own rows in one launch: one is bound by the matrix units as soon as it has many query rows, the other by
 // memory.  256 workgroups of the one (all, if there are fewer) and as many of the other alternate, so that a CU has one of
 // each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows: 144 us, 121
-// and 67 alone.  Measured with three numbers a weight, 174 us then: all of the prefix first 180 us; mixed in proportion, which
+// and 67 alone.  Measured when this took 174 us: all of the prefix first 180 us; mixed in proportion, which
 // leaves single prefix workgroups for the end, 206.)
 // Tiles of one prefix range are a multiple of 8 workgroups apart, on one XCD, wherever Hkv * splits is one.
 // ----------------------------------------------------------------------------
@@ -736,7 +717,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttendArgs a)
     own_rows<T, D>(a, r.block, js, areas);
 }
 
-template <int D, int MQ, int TERMS>
+template <int D, int MQ>
 __global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs a) {
   typedef SharedStep<D> L;
   constexpr int AREA = L::BYTES > 16 * (D + 4) * 4 ? L::BYTES : 16 * (D + 4) * 4;
@@ -745,7 +726,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared_kernel(const AttendArgs 
   const Role r = role_of(a);
   if (!r.any) return;
   if (r.prefix) {
-    prefix_shared<D, MQ, TERMS>(a, r.block, ring0, ring1, ring2, ring3);
+    prefix_shared<D, MQ>(a, r.block, ring0, ring1, ring2, ring3);
   } else {
     const Areas areas{ring0, ring1, ring2, ring3};
     own_rows<bf16_t, D>(a, r.block, js, areas);
@@ -1005,12 +986,6 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
   }
 }
 
-// From this many prefix rows on, and with more query rows than make the prefix a matter of memory, weights are two numbers
-// instead of three: a third fewer products where they are the bound (64K rows, 448 query rows, 160K own rows: 162 -> 144 us).
-// Outputs are then off by 2.2e-6 of their norm, as an evaluation in fp32 throughout is over so many rows (2.3e-6 at 32K rows, 2.6e-6 at
-// 64K, but 1.6e-6 at 16K; with three numbers 0.8e-6).
-constexpr int TWO_TERMS_ROWS = 32768;
-
 template <typename T, int D>
 wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
   if (g.one_launch) {
@@ -1036,11 +1011,9 @@ wave_status attend_td(AttendArgs a, const CacheAttendGeom& g, hipStream_t st) {
     shared = a.P > 0 && g.mtile > 16;
     if (shared) {
       if (g.mtile == 64)
-        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 1, 3>), blocks, 256, 0, st, a);
-      else if (a.P < TWO_TERMS_ROWS)
-        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 2, 3>), blocks, 256, 0, st, a);
+        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 1>), blocks, 256, 0, st, a);
       else
-        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 2, 2>), blocks, 256, 0, st, a);
+        WAVE_LAUNCH("cache_attend", (attend_shared_kernel<D, 2>), blocks, 256, 0, st, a);
     }
   }
   if (!shared) WAVE_LAUNCH("cache_attend", (attend_rows_kernel<T, D>), blocks, 256, 0, st, a);
@@ -1108,9 +1081,9 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
   // Two tiles of columns a wave share its reads of keys and values, and double what a workgroup has to do.  That pays where there
   // is work for most CUs at the smallest ranges (d = 128: 64 sequences behind 500 rows 16.6 us, with one tile 14.4; behind 8000
   // 34.8 and 35.7); at d = 64, where a wave has half as much to read, only far beyond (64 x 7 query rows behind 8000 rows 28 us,
-  // 24; 200 x 4 behind 16000 87 and 95) or with two numbers a weight, which are made for two tiles.
+  // 24; 200 x 4 behind 16000 87 and 95).
   const long long tiles128 = (long long)c.Hkv * ((M + 127) / 128) * (((long long)P + 127) / 128);
-  const bool wide = M > 64 && (tiles128 >= (c.d == 128 ? 192 : 4096) || P >= TWO_TERMS_ROWS);
+  const bool wide = M > 64 && tiles128 >= (c.d == 128 ? 192 : 4096);
   const int narrow = M <= 16 || c.dtype == WAVE_F32 ? 16 : 64, widest = narrow == 64 && M > 64 ? 128 : narrow;
   g.mtile = wide ? widest : narrow;
   const PrefixCut cut = prefix_cut(c, M, g.mtile);

@@ -392,6 +392,30 @@ def test_attention_of_many_partial_results(dtype, B, Hq, P):
     _check_attention(dtype, q, cache, lengths, pk, pv, 0.0, cache.weights, out, lse, w)
 
 
+@pytest.mark.parametrize("d,c", [(64, 0.625), (128, 0.4375)])
+@pytest.mark.parametrize("B,P", [(1, 32768), (16, 32768), (17, 32768), (40, 33001), (17, 4000)])
+def test_attention_weights_keep_their_bits_behind_any_prefix(d, c, B, P):
+    """Two rows of the prefix have all the weight, one of them nearly all of it, 2^5 .. 2^8 over the reference that the other one
+    has set: a weight that lost bits shows in the output, whatever the length and the number of query rows are.  The scores are exact
+    (16 bits a product, up to 128 equal ones), the weights' exponents off by 4 roundings of up to 8, 22 u of the weight, and
+    the exponential by 2 u: that moves the output by 24 u p0 p1 |v1 - v0|; the products with the values, their sums, the joining
+    and the quotient are 16 roundings at most."""
+    g = _gen(P + B)
+    cache = wb.alloc_cache(torch.bfloat16, B, 1, d, 8)
+    f = (0.7 + 0.4 * torch.rand(B, 4, 1, generator=g)).bfloat16()
+    k = torch.full((1, P, d), -100.0)
+    k[0, 3], k[0, 100] = 0.0, c
+    v = torch.randn(1, P, d, generator=g).bfloat16()
+    out, lse = wb.wave_cache_attention_decode(f.expand(B, 4, d).contiguous().cuda(), cache, k.bfloat16().cuda(), v.cuda())
+    z = f.double() * c * math.sqrt(d)
+    p1, v0, v1 = torch.sigmoid(z), v[0, 3].double(), v[0, 100].double()
+    p0 = 1 - p1
+    bar = 16 * U * (p0 * v0.abs() + p1 * v1.abs()) + 24 * U * p0 * p1 * (v1 - v0).abs()
+    err = (out.double().cpu() - (p0 * v0 + p1 * v1)).abs()
+    assert bool((err <= bar).all()), float((err / bar).max())
+    assert torch.allclose(lse.double().cpu(), torch.log1p(torch.exp(z))[..., 0], rtol=0, atol=64 * U)
+
+
 @pytest.mark.parametrize("B", [2, 8, 20])
 def test_attention_values_that_are_not_finite_show_in_their_channel(B):
     """An infinite value in the last prefix row, and in the last own row: its channel is not finite (a weight is a sum of bf16
