@@ -113,7 +113,7 @@ struct Step<bf16_t, D> {
         const uint4 u = ONCE ? load16_stream(at) : load16(at);
         v.x[j][0] = u.x; v.x[j][1] = u.y; v.x[j][2] = u.z; v.x[j][3] = u.w;
       } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(at);
+        const uint2 u = ONCE ? load8_stream(at) : *reinterpret_cast<const uint2*>(at);
         v.x[j][0] = u.x; v.x[j][1] = u.y;
       }
     }
