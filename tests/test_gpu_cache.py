@@ -644,6 +644,18 @@ def test_evict(dtype, d, B, Hkv, cap, lengths, n_keep, n_sink, n_local, ties):
     _check_evict(cache, before, lengths, n_keep, n_sink, n_local, mixed, dst)
 
 
+@pytest.mark.parametrize("keys", list(range(1, 17)))
+def test_evict_every_number_of_keys_a_thread(keys):
+    """Rooms at both ends of each: the last row with a key of its own, and one row less."""
+    for cap in (1024 * (keys - 1) + 1, 1024 * keys):
+        lengths = [cap, cap - 1, cap // 2]
+        cache = _filled_cache("bf16", 3, 1, 64, cap, lengths, keys)
+        before = {name: t.clone() for name, t in cache.t.items()}
+        n_keep = max(cap * 2 // 3, 1)
+        wb.wave_cache_evict(cache, n_keep, min(1, n_keep), 0)
+        _check_evict(cache, before, lengths, n_keep, min(1, n_keep), 0, cache, before)
+
+
 def test_evict_long():
     cache = _filled_cache("bf16", 1, 2, 64, 131000, [130999], 3)
     before = {name: t.clone() for name, t in cache.t.items()}
