@@ -387,14 +387,16 @@ typedef struct {
  *                 q_out included
  *   rotary        HOST, or NULL: keys go in as they are; q must then be NULL
  *   coords        DEVICE [n_axes,B,n_new] int32, or NULL: tokens[b] + t on every axis.
- *                 Must not overlap q_out, lengths_out or tokens_out, except that with
- *                 one axis and n_new = 1 it may be cache->lengths or cache->tokens
- *                 themselves, updated in place
+ *                 Must not overlap what the call writes (the cache's k, v, positions and
+ *                 weights, q_out, lengths_out, tokens_out), except that with one axis and
+ *                 n_new = 1 it may be cache->lengths or cache->tokens themselves, updated
+ *                 in place
  *   lengths_out, tokens_out  DEVICE [B]: the numbers after the call.  Each may be
  *                 the cache's own array (updated in place) and must not overlap it
  *                 otherwise; tokens_out may be NULL where cache->tokens is.
  * cache->positions, weights and tokens may be NULL (positions and NULL coords
- * need tokens).  The caller keeps lengths[b] + counts[b] <= capacity: rows that
+ * need tokens).  What the call writes must not overlap what it reads or writes otherwise.
+ * The caller keeps lengths[b] + counts[b] <= capacity: rows that
  * do not fit are left out, and lengths and tokens advance by those that did.
  * WAVE_ERR_SHAPE: n_new above 2^30, B * n_new of 2^31 and more, B * Hq of 2^24
  * and more. */

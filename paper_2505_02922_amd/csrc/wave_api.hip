@@ -605,18 +605,23 @@ wave_status wave_cache_append(const wave_cache* cache, const void* k_new, const 
   }
   const size_t es = elem_bytes(c.dtype), cb = cache_bytes(c), counts_bytes = sizeof(int32_t) * (size_t)c.B;
   const size_t kvb = (size_t)c.B * c.Hkv * n_new * c.d * es;
+  // the cache's rows and what is kept of them, which workgroups write in no order
+  const size_t rb = cache_rows(c) * sizeof(int32_t);
+  auto in_rows = [&](const void* p, size_t bytes) {
+    return overlaps(p, bytes, c.k, cb) || overlaps(p, bytes, c.v, cb) || overlaps(p, bytes, c.positions, rb) ||
+           overlaps(p, bytes, c.weights, rb);
+  };
   if (q) {
     if (Hq < 1) return WAVE_ERR_ARG;
     if ((long long)c.B * Hq >= kMaxGrid) return WAVE_ERR_SHAPE;
     if (!q_out || !aligned16(q) || !aligned16(q_out)) return WAVE_ERR_ARG;
     const size_t qb = (size_t)c.B * Hq * n_new * c.d * es;
-    if (!same_or_apart(q, qb, q_out, qb) || overlaps(q_out, qb, c.k, cb) || overlaps(q_out, qb, c.v, cb) ||
-        overlaps(q_out, qb, k_new, kvb) || overlaps(q_out, qb, v_new, kvb) || overlaps(q, qb, c.k, cb) ||
-        overlaps(q, qb, c.v, cb))
+    if (!same_or_apart(q, qb, q_out, qb) || in_rows(q, qb) || in_rows(q_out, qb) || overlaps(q_out, qb, k_new, kvb) ||
+        overlaps(q_out, qb, v_new, kvb) || overlaps(q_out, qb, counts, counts_bytes))
       return WAVE_ERR_ARG;
   }
-  if (overlaps(k_new, kvb, c.k, cb) || overlaps(k_new, kvb, c.v, cb) || overlaps(v_new, kvb, c.k, cb) ||
-      overlaps(v_new, kvb, c.v, cb))
+  if (in_rows(k_new, kvb) || in_rows(v_new, kvb) || in_rows(counts, counts_bytes) || in_rows(lengths_out, counts_bytes) ||
+      in_rows(tokens_out, counts_bytes))
     return WAVE_ERR_ARG;
   if (!same_or_apart(lengths_out, counts_bytes, c.lengths, counts_bytes) ||
       !same_or_apart(tokens_out, counts_bytes, c.tokens, counts_bytes) ||
@@ -630,7 +635,7 @@ wave_status wave_cache_append(const wave_cache* cache, const void* k_new, const 
     // a workgroup would read what another one writes
     const size_t xb = sizeof(int32_t) * (size_t)rotary->n_axes * c.B * n_new;
     const bool one = rotary->n_axes == 1 && n_new == 1;
-    if ((overlaps(coords, xb, lengths_out, counts_bytes) && !(one && coords == lengths_out && coords == c.lengths)) ||
+    if (in_rows(coords, xb) || (overlaps(coords, xb, lengths_out, counts_bytes) && !(one && coords == lengths_out && coords == c.lengths)) ||
         (overlaps(coords, xb, tokens_out, counts_bytes) && !(one && coords == tokens_out && coords == c.tokens)) ||
         (q && overlaps(coords, xb, q_out, (size_t)c.B * Hq * n_new * c.d * es)))
       return WAVE_ERR_ARG;

@@ -140,6 +140,29 @@ def test_coordinates_apart_from_what_is_written():
     assert apply(FAKE, B=1, H=(1 << 30) + 1, N=1) == SHAPE and apply(FAKE, B=1, H=1, N=(1 << 30) + 1) == SHAPE
 
 
+def test_append_refuses_to_write_what_it_reads():
+    """Every array that the call reads or writes, in each of the cache's arrays (which workgroups write in no order), and
+    what else it writes in one another; the call that all of them are changed from is not refused."""
+    L = wb.lib()
+    c, r = _cache(), wb.wave_rotary_plan(64, 1e4)
+    kn, vn, q, qo, lo, to, xy, cnt = (0x4000000 + i * 0x100000 for i in range(8))
+
+    def call(kn=kn, vn=vn, q=q, coords=xy, counts=cnt, qo=qo, lo=lo, to=to):
+        return L.wave_cache_append(ctypes.byref(c), kn, vn, q, 4, 3, counts, ctypes.byref(r), coords, qo, lo, to, None)
+
+    if not torch.cuda.is_available():     # made-up addresses: the launch has to fail
+        assert call() == 6 and call(counts=None, coords=None) == 6 and call(qo=q) == 6 and call(lo=c.lengths, to=c.tokens) == 6
+        assert call(counts=c.lengths) == 6 and call(coords=cnt) == 6
+    ends = {"k": 2 * 2 * 64 * 128 * 2, "v": 2 * 2 * 64 * 128 * 2, "positions": 2 * 2 * 64 * 4, "weights": 2 * 2 * 64 * 4}
+    for name, size in ends.items():
+        at = getattr(c, name)
+        for p in (at, at + size - 16):
+            for arg in ("kn", "vn", "q", "coords", "counts", "qo", "lo", "to"):
+                assert call(**{arg: p}) == ARG, (name, arg)
+    assert call(counts=qo) == ARG and call(counts=qo + 2 * 4 * 3 * 128 * 2 - 4) == ARG and call(counts=to) == ARG
+    assert call(coords=qo) == ARG and call(coords=lo) == ARG and call(coords=c.tokens, to=c.tokens) == ARG
+
+
 def test_attention_refuses():
     L = wb.lib()
     c = _cache()
