@@ -411,7 +411,8 @@ wave_status wave_cache_append(const wave_cache *cache, const void *k_new, const 
  * The prefix is read once for the batch (all B * G queries of a KV head
  * multiply the same rows), the own rows once per KV head.
  *   q             DEVICE [B,Hq,d] dtype, 16-byte aligned
- *   prefix_k, prefix_v  DEVICE [Hkv,P,d] dtype, 16-byte aligned; may be NULL where P = 0
+ *   prefix_k, prefix_v  DEVICE [Hkv,P,d] dtype, dense (the k and v of a cache with B = 1
+ *                 and capacity = P are), 16-byte aligned; may be NULL where P = 0
  *   weights_out   DEVICE [B,Hkv,capacity] fp32 or NULL.  Each own row j of a unit
  *                 gets decay * weights[j] + the sum over the unit's G heads of the
  *                 softmax weight that row j received (the prefix's share counts in

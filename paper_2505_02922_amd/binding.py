@@ -621,7 +621,10 @@ def wave_cache_attention_decode(q: torch.Tensor, cache: Cache, prefix_k: Optiona
                                 lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """q [B, Hq, d] against the prefix [Hkv, P, d] that the batch shares (None: there is none) and each
     sequence's rows, under one softmax.  weights_out (cache.weights: in place) receives decay * weights +
-    what each row got in this step.  Returns (out [B,Hq,d] f32, lse [B,Hq] f32)."""
+    what each row got in this step.  Returns (out [B,Hq,d] f32, lse [B,Hq] f32).
+
+    The prefix is read as it lies only where it is contiguous, as k[0] and v[0] of a one-sequence cache with as much room
+    as the prompt has rows are; any other view (part of a larger buffer) is copied whole by every call."""
     where = "wave_cache_attention_decode"
     shape, dtype, P = q.shape, cache.dtype, 0
     _require(len(shape) == 3 and shape[0] == cache.B and shape[2] == cache.d, 2, where)

@@ -552,6 +552,24 @@ def test_attention_of_scores_that_are_no_numbers(dtype, cap):
     assert _same_bits(w[0, 0, :n], cache.weights[0, 0, :n])        # (decay 1: the old weights and nothing)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_prompt_appended_to_its_own_cache_is_the_prefix(dtype):
+    """A one-sequence cache with as much room as the prompt has rows is the prefix as it lies; part of a larger one (a view that
+    the call copies) gives the same bits."""
+    P, B, Hq, Hkv, d = 203, 3, 8, 2, 64
+    cache, q, _, _ = _inputs(dtype, B, Hq, Hkv, d, 40, [40, 0, 9], 0, 12)
+    k, v = (torch.randn(1, Hkv, P, d, generator=_gen(s)).to(TYPES[dtype]).cuda() for s in (1, 2))
+    rot = wb.wave_rotary_plan(d, 1e4)
+    tight, roomy = wb.alloc_cache(TYPES[dtype], 1, Hkv, d, P), wb.alloc_cache(TYPES[dtype], 1, Hkv, d, P + 50)
+    for prompt in (tight, roomy):
+        wb.wave_cache_append(prompt, k, v, rotary=rot)
+    assert tight.k[0].is_contiguous() and not roomy.k[0, :, :P].is_contiguous()
+    out, lse = wb.wave_cache_attention_decode(q, cache, tight.k[0], tight.v[0])
+    _check_attention(dtype, q, cache, [40, 0, 9], tight.k[0], tight.v[0], 1.0, cache.weights, out, lse, None)
+    o2, l2 = wb.wave_cache_attention_decode(q, cache, roomy.k[0, :, :P], roomy.v[0, :, :P])
+    assert _same_bits(out, o2) and _same_bits(lse, l2)
+
+
 def test_attention_equals_full_attention_decode():
     g = _gen(21)
     K, V = (torch.randn(2, 2, 1000, 128, generator=g).bfloat16().cuda() for _ in range(2))
