@@ -301,8 +301,9 @@ struct State {
 // wave's own place for a step's key rows.  Keys go through it because an operand has sixteen rows side by side, 64 bytes of
 // each in a load: straight from memory every line is asked for twice, and must stay in the caches between.  A load of the
 // values takes whole rows.  1.12 GB of own rows: 235 us with both straight from memory, 222 with the values passing by the
-// caches, 209 us = 5.5 TB/s, what a plain read of 1 GiB reaches, so.  (Values through LDS too: the same alone, but 171
-// instead of 155 us beside a long prefix, which needs LDS itself.)
+// caches, 209 us = 5.5 TB/s, what a plain read of 1 GiB reaches, so.  At d = 64, eight sequences of 3000 .. 65536 rows: 89 us, 92
+// with the values in the caches.  (Values through LDS too: the same alone, but a tenth slower beside a long prefix, which
+// needs LDS itself.)
 // ----------------------------------------------------------------------------
 template <typename T, int D, bool ONCE, typename Leave>
 __device__ __forceinline__ void stream_rows(const char* K, const char* V, int k0, int stride, int end, float scale,
@@ -509,7 +510,10 @@ __device__ __forceinline__ void own_rows(const AttendArgs& a, int block, JoinSha
 }
 
 // Prefix with the own rows' stream: one workgroup per (KV head, range of prefix rows, tile of 16 of the B * G query rows).
-// Up to 16 query rows, and fp32, whose products take eight times as long, so that sharing rows in LDS has nothing to gain.
+// Up to 16 query rows, a matter of memory (eight KV heads, 65536 rows for 16 query rows each: 45 us and 5 for the join, 5.5 TB/s),
+// and fp32: its products bind it from about 64 query rows on (32768 rows, eight KV heads: 47 us for 16, 85 for 32, 192 .. 231 for
+// 128: at best 91 TFLOP/s of the 134 that a large fp32 product reaches), so rows shared in LDS could only help between, where
+// the second tile's rows come from the caches.
 template <typename T, int D>
 __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, JoinShared& js, const Areas areas) {
   typedef Step<T, D> S;
@@ -534,11 +538,12 @@ __device__ __forceinline__ void prefix_rows(const AttendArgs& a, int block, Join
 // are on their way.  The values' operand comes transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of sixteen
 // channels, and each gets the four values of its channel; a read takes two neighbouring chunks of eight rows).
 // The scores of the next step are formed beside the softmax of this one, so that matrix and vector work of a wave do not
-// wait for each other.  Measured (64K rows, 448 query rows per KV head, 62 GFLOP): 144 us.  The
-// card lowers its clock to 1.7 .. 1.8 GHz under this mixture (2.5 GHz in the own rows; products of random numbers alone: 2.0
-// PFLOP/s instead of 2.4), and the time follows the work itself: sixteen products fewer a step 23 us, no loads into LDS 14 us, no
-// exponentials 7 us, no LDS reads of the keys or of the values 4 us each, while other orders of the same instructions, a third
-// fewer vector instructions, or two workgroups a CU instead of one change nothing.
+// wait for each other.  Measured (64K rows, 448 query rows on each of four KV heads, 60 GFLOP): 153 us back to back.  The card
+// lowers its clock to 1.7 .. 1.8 GHz under this mixture (2.5 GHz in the own rows; products of random numbers alone: 2.0
+// PFLOP/s instead of 2.4), and the time follows the work itself: of 144 us on a cooler card, sixteen products fewer a step are 23, no
+// loads into LDS 14, no exponentials 7, no LDS reads of the keys or of the values 4 each, while other orders of the same
+// instructions, a third fewer vector instructions, or two workgroups a CU instead of one change nothing.  (448 columns are three and
+// a half tiles of 128: two of the last tile's waves have none and only fetch, an eighth of the waves in all.)
 template <int D>
 struct SharedStep {
   static constexpr int ROWS = 32, ROW = D * 2, CHUNKS = ROW / 16, HALF = ROWS * ROW, BYTES = 2 * HALF;  // keys, then values
@@ -685,9 +690,8 @@ __device__ __forceinline__ void prefix_shared(const AttendArgs& a, int block, ch
 // ----------------------------------------------------------------------------
 // Prefix and own rows in one launch: one is bound by the matrix units as soon as it has many query rows, the other by
 // memory.  256 workgroups of the one (all, if there are fewer) and as many of the other alternate, so that a CU has one of
-// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows: 144 us, 121
-// and 67 alone.  Measured when this took 174 us: all of the prefix first 180 us; mixed in proportion, which
-// leaves single prefix workgroups for the end, 206.)
+// each; what is left of the longer kind follows.  (64K prefix rows for 448 query rows per KV head with 160K own rows: 174 us, 153
+// and 59 alone.  All of the prefix first 180 us; mixed in proportion, which leaves single prefix workgroups for the end, 206.)
 // Tiles of one prefix range are a multiple of 8 workgroups apart, on one XCD, wherever Hkv * splits is one.
 // ----------------------------------------------------------------------------
 struct Role {
@@ -1043,18 +1047,18 @@ struct PrefixCut {
 };
 static PrefixCut prefix_cut(const wave_cache& c, int M, int mtile) {
   const int mtiles = (M + mtile - 1) / mtile;
-  // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 52 us
-  // instead of 57 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory (100K rows, 64 query
-  // rows: 95 us instead of 110).  No more than 256 ranges, each of which every head's joining reads (one KV head, 65536 rows:
+  // One workgroup a CU where it is bound by the matrix units (its partial results cost more than a second one gains: 60 us
+  // instead of 68 for 32K rows, 128 query rows and 500 own rows), two where it is bound by memory (100K rows, 64 query
+  // rows: 88 us instead of 93).  No more than 256 ranges, each of which every head's joining reads (one KV head, 65536 rows:
   // 28 us with 512, 20).
   const int aim = mtile == 128 && c.d == 128 ? 256 : 512;
   const int even = aim / (c.Hkv * mtiles) > 1 ? aim / (c.Hkv * mtiles) : 1;
   return PrefixCut{mtiles, even < 256 ? even : 256};
 }
-// Pieces of own rows aimed at, as many as are resident: two a CU, four at d = 64 (or half of them, see find_piece).  Four beside
-// a prefix that its products bind: short ones fill the gaps (64K prefix rows for 448 query rows and 160K own rows: 158 us with
-// two or three, 155 with four or six; 32K for 128 and 16K: 56 with up to four, 57 with six; 50K for 192 at d = 64 and 80K: 70
-// and 76).
+// Pieces of own rows aimed at, as many as are resident: two a CU, four at d = 64 (or half of them, see find_piece).  Four, and never
+// half of them, beside a prefix that its products bind: there many own rows gain, and few lose less (32K prefix rows for 128 query
+// rows on eight KV heads with 100K own rows: 108 us, without this rule 117; with 16K 60 and 59; 64K for 448 on four with 160K: 161 and
+// 159; d = 64, 50K for 192 and 80K: 42 both ways).
 static bool binds(const wave_cache& c, int M, const PrefixCut& cut, long long splits) {
   return M > 16 && c.Hkv * splits * cut.mtiles >= 128;
 }
@@ -1079,9 +1083,10 @@ CacheAttendGeom cache_attend_geometry(const wave_cache& c, int Hq, int P, bool a
   g.one_launch = steps <= 1 || (steps <= 2 && (c.B * c.Hkv <= 256 || c.B > 512));
   const int M = c.B * G;
   // Two tiles of columns a wave share its reads of keys and values, and double what a workgroup has to do.  That pays where there
-  // is work for most CUs at the smallest ranges (d = 128: 64 sequences behind 500 rows 16.6 us, with one tile 14.4; behind 8000
-  // 34.8 and 35.7); at d = 64, where a wave has half as much to read, only far beyond (64 x 7 query rows behind 8000 rows 28 us,
-  // 24; 200 x 4 behind 16000 87 and 95).
+  // is work for most CUs at the smallest ranges (d = 128, 448 query rows on four KV heads: behind 500 rows 16.9 us, with one tile
+  // 14.0; behind 2000 19.6 and 23.8; behind 8000 32 both ways); at d = 64, where a wave has half as much to read, not before that
+  // grows far beyond, and then hardly (448 behind 8000 rows 24.0 us, 21.5; 800 behind 16000 45.4 and 43.3; 128 on eight KV heads behind
+  // 64K 56.8 and 57.2).
   const long long tiles128 = (long long)c.Hkv * ((M + 127) / 128) * (((long long)P + 127) / 128);
   const bool wide = M > 64 && tiles128 >= (c.d == 128 ? 192 : 4096);
   const int narrow = M <= 16 || c.dtype == WAVE_F32 ? 16 : 64, widest = narrow == 64 && M > 64 ? 128 : narrow;
