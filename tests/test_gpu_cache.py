@@ -248,6 +248,23 @@ def test_append_with_its_own_numbers_as_coordinates(name, Hq, Hkv):
         assert _same_bits(t, b.t[key]), key
 
 
+def test_append_of_more_workgroups_than_a_launch_row():
+    """Two million sequences with 129 tokens each, three workgroups a sequence, of which the first two tokens fit (33 GiB of new
+    rows; keys and values are the same array)."""
+    B, n, d = (1 << 21) - 1, 129, 64
+    row = torch.randn(B, 1, 1, d, device="cuda", dtype=torch.bfloat16)
+    new = row.expand(B, 1, n, d).contiguous()
+    cache = wb.alloc_cache(torch.bfloat16, B, 1, d, 2)
+    cache.tokens.copy_(torch.randint(0, 1 << 20, (B,), device="cuda", dtype=torch.int32))
+    first = cache.tokens.clone()
+    r = wb.wave_rotary_plan(d, 1e4)
+    assert wb.wave_cache_append(cache, new, new, rotary=r) is None
+    at = torch.stack([first, first + 1], 1)[None]
+    want = wb.wave_rotary_apply(row.expand(B, 1, 2, d).contiguous(), at.contiguous(), r)
+    assert _same_bits(cache.k, want) and _same_bits(cache.v, new[:, :, :2])
+    assert bool((cache.lengths == 2).all()) and torch.equal(cache.tokens, first + 2) and torch.equal(cache.positions[:, 0], at[0])
+
+
 # --------------------------------------------------------------------------- attention
 def _check_attention(dtype, q, cache, lengths, pk, pv, decay, old, out, lse, w, tag=""):
     B, Hq, d = q.shape
