@@ -53,7 +53,7 @@ def listed():
         dict(_LLAMA, name="attend_bf16_64k_b8", op="attend", B=8, page=64, short=3001, long=65536, shared=0),
         # A beam search's step: eight beams of one short sequence.
         dict(_TINY, name="reorder_f32_beams_b8", op="reorder", B=8, to=8, page=32, short=200, long=200, shared=6),
-        # A large batch of samples of 64 prompts; some leave, some are forked.
+        # A large batch of samples that begin alike; some leave, some are forked.
         dict(_LLAMA, name="reorder_bf16_8k_b256", op="reorder", B=256, to=256, page=128, short=700, long=8191, shared=4),
     ]
 
