@@ -354,6 +354,37 @@ wave_status wave_rotary_plan(wave_rotary *rotary, int rot_dim, double base, cons
 wave_status wave_rotary_apply(const void *x, const int32_t *coords, const wave_rotary *rotary, int dtype,
                               int B, int H, int N, int d, void *y, void *hip_stream);
 
+/* Rows of several heads where they lie: element c of the row of sequence b, head h and token n is
+ * data[b * stride_b + h * stride_h + n * stride_n + c], so a fused projection's output is read without a
+ * copy.  Strides are in elements, none negative (0 repeats a row), each a multiple of 16 bytes;
+ * data is 16-byte aligned. */
+typedef struct {
+  const void *data;         /* DEVICE dtype                                            */
+  int64_t stride_b, stride_h, stride_n;
+} wave_rows;
+
+/* Norms of queries and keys for each head: row x becomes x_c * weight_c / sqrt(mean(x^2) + eps), the mean over all d
+ * channels, before it is turned. */
+typedef struct {
+  const void *q_weight, *k_weight; /* DEVICE [d] dtype, 16-byte aligned; NULL: those rows are not normed */
+  float eps;                       /* 0 or more, finite                                */
+} wave_head_norm;
+
+/* Norms and rotary positions of queries and keys in one pass.
+ *   q, k       rows [B,Hq,N] and [B,Hkv,N]; either may be NULL (its heads and output are then not looked at)
+ *   norm       HOST, or NULL: nothing is normed
+ *   rotary     HOST, or NULL: nothing is turned; coords must then be NULL, and norm must not
+ *   coords     DEVICE [n_axes,B,N] int32
+ *   q_out, k_out  DEVICE [B,Hq,N,d] and [B,Hkv,N,d] dtype, dense, 16-byte aligned; each may be its own input
+ *              where that is dense, and must not overlap anything else that the call reads or writes
+ * Sums of squares, norms, sines and products are fp32 (angles as in wave_rotary_apply) and each
+ * result is rounded once to dtype: a row whose squares add up to 2^128 and more has norm infinity.
+ * Sizes as in wave_rotary_apply, with H = Hq + Hkv. */
+wave_status wave_norm_rotary_apply(const wave_rows *q, int Hq, const wave_rows *k, int Hkv,
+                                   const wave_head_norm *norm, const wave_rotary *rotary,
+                                   const int32_t *coords, int dtype, int B, int N, int d, void *q_out,
+                                   void *k_out, void *hip_stream);
+
 /* One cache of raw key and value rows per (sequence, KV head).  Plain data, all
  * arrays caller-owned; a field that a call does not need may be NULL.  Rows of
  * sequence b are the first lengths[b] of each of its units, in no order that
@@ -460,6 +491,103 @@ wave_status wave_cache_attention_decode(const void *q, int Hq, const wave_cache 
 size_t wave_cache_evict_workspace(const wave_cache *from, int n_keep);
 wave_status wave_cache_evict(const wave_cache *from, const wave_cache *to, int n_keep, int n_sink,
                              int n_local, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * The paged cache: keys and values in 8 bits, in pages that sequences share.
+ * A page holds `page` tokens of every KV head.  New rows wait in the sequence's
+ * tail, in dtype; as soon as a page's last row is there the page is rounded to 8
+ * bits, once, with one scale for each head, and never changes again: what a page holds does
+ * not depend on how its tokens came in, the newest rows are exact, and sequences that begin
+ * alike share pages.
+ *   scale = max |x| / 127 over the page's rows of a head, as they are in dtype;
+ *   code  = x * (127 / max |x|) to the nearest whole number, ties to even (fp32)
+ * and a row reads as code * scale.  A head's part of a page whose largest value is below 2^-100 reads as zeros
+ * (scale 0); one that holds an infinity or no number reads as no numbers throughout.
+ *
+ * Plain data, all arrays caller-owned.  A sequence of L tokens has L / page pages, the first entries of its row of
+ * the table, and L % page rows in its tail; what lies behind either is never read.
+ * references counts the sequences that hold a page; one with 0 (or less) is free, so an empty
+ * cache is lengths and references of 0.  A caller who keeps a page (a prompt that comes back) adds 1 of its own.
+ * A sequence is not cut short by setting its length back: the rows of a complete page are no longer in the tail.
+ * The library reads lengths and table on the device: a length outside 0 ..
+ * max_pages * page + page - 1 and an entry outside 0 .. n_pages - 1 count as the nearest inside.
+ * Every call returns WAVE_ERR_SHAPE for a page other than 32, 64 or 128, B * Hkv of 2^21 and more,
+ * n_pages above 2^28, or max_pages * page above 2^30.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype;            /* wave_dtype of queries, new rows and tails               */
+  int32_t B, Hkv, d;
+  int32_t page;             /* tokens of a page: 32, 64 or 128                         */
+  int32_t n_pages;          /* pages of the pool                                       */
+  int32_t max_pages;        /* entries of a sequence's row of the table                */
+  int8_t *k_codes, *v_codes;  /* DEVICE [n_pages,Hkv,page,d], 16-byte aligned          */
+  float *k_scales, *v_scales; /* DEVICE [n_pages,Hkv]                                  */
+  void *k_tail, *v_tail;    /* DEVICE [B,Hkv,page,d] dtype, 16-byte aligned            */
+  int32_t *table;           /* DEVICE [B,max_pages] pages of each sequence             */
+  int32_t *lengths;         /* DEVICE [B] tokens                                       */
+  int32_t *references;      /* DEVICE [n_pages]                                        */
+} wave_pages;
+
+/* Appends n_new tokens (1 for a decode step, any number for a prompt) to every sequence: keys and queries are
+ * normed and turned as by wave_norm_rotary_apply, rows are rounded to dtype, and every page that becomes complete takes a
+ * free page of the pool: the lowest ones, in the order of the sequences and of each sequence's tokens.
+ *   from          the cache (every array is needed)
+ *   to            what it becomes: k_tail, v_tail, table, lengths and references are all from's own (in
+ *                 place) or all other arrays, and from is then still what it was, so an append of drafted tokens
+ *                 is taken back by going on with from.  (Then only one of the two may go on: both count the same
+ *                 pages as free.)  Codes and scales are from's own, and so are all sizes.  What lies behind a
+ *                 sequence's pages and rows in to's arrays is left as it is
+ *   k_new, v_new  rows [B,Hkv,n_new]
+ *   q             rows [B,Hq,n_new] or NULL (then Hq and q_out are not looked at); only normed and turned.
+ *                 q_out DEVICE [B,Hq,n_new,d] dtype, may be q where that is dense.  NULL where there is neither a
+ *                 rotary plan nor norm->q_weight
+ *   counts        DEVICE [B] int32 or NULL: only the first counts[b] of the n_new tokens exist (a value
+ *                 outside 0 .. n_new counts as the nearer); nothing of the others is written, their rows
+ *                 of q_out included
+ *   norm, rotary  HOST, or NULL
+ *   coords        DEVICE [n_axes,B,n_new] int32, or NULL: lengths[b] + t on every axis
+ *   workspace     DEVICE, 256-byte aligned, >= wave_pages_append_workspace(from)
+ * Tokens that do not fit, in the table's row or because no page is free for them, are left out (their rows of q_out are
+ * written): a sequence then ends one row before the page that it did not get, and lengths
+ * says how many there are.  What the call writes must not overlap what it reads or writes otherwise.
+ * WAVE_ERR_SHAPE: n_new above 2^30, B * n_new of 2^31 and more, B * Hq of 2^24 and more. */
+size_t wave_pages_append_workspace(const wave_pages *from);
+wave_status wave_pages_append(const wave_pages *from, const wave_pages *to, const wave_rows *k_new,
+                              const wave_rows *v_new, const wave_rows *q, int Hq, int n_new,
+                              const int32_t *counts, const wave_head_norm *norm, const wave_rotary *rotary,
+                              const int32_t *coords, void *q_out, void *workspace, size_t workspace_bytes,
+                              void *hip_stream);
+
+/* Rows back in dtype (an index is built from raw rows): row t of the outputs is row first[b] + t of sequence b, pages'
+ * rows rounded once; rows that the sequence has not are left as they are.
+ *   first         DEVICE [B] int32, or NULL: 0
+ *   k_out, v_out  DEVICE [B,Hkv,n,d] dtype, 16-byte aligned; one may be NULL
+ * (references is not needed.)  WAVE_ERR_SHAPE: n above 2^30, or B * Hkv * n of 2^34 and more. */
+wave_status wave_pages_read(const wave_pages *pages, const int32_t *first, int n, void *k_out, void *v_out,
+                            void *hip_stream);
+
+/* Exact attention of one token per sequence over the rows that the cache holds: o = softmax(q K_b^T / sqrt(d)) V_b.
+ *   q             DEVICE [B,Hq,d] dtype, 16-byte aligned
+ *   out           DEVICE [B,Hq,d] fp32;  lse DEVICE [B,Hq] fp32 (natural log)
+ *   workspace     DEVICE, 256-byte aligned, >= wave_pages_attention_workspace(...)
+ * A sequence without rows has out = 0 and lse = -infinity.  Scores are exact products of queries and codes, summed in fp32,
+ * times the page's scale; the softmax and all sums are fp32, and a softmax weight meets the values' codes as three bf16
+ * numbers that hold all its bits.  (references is not needed.)
+ * WAVE_ERR_SHAPE: Hq / Hkv not a whole number in 1 .. 8, or B * Hq of 2^24 and more. */
+size_t wave_pages_attention_workspace(const wave_pages *pages, int Hq);
+wave_status wave_pages_attention_decode(const void *q, int Hq, const wave_pages *pages, float *out, float *lse,
+                                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Sequences copied, forked and freed: sequence b of `to` becomes what sequence parent[b] of `from` was, an empty one where
+ * parent[b] is outside 0 .. from->B - 1.  Pages are shared, so only tables and tails are copied; references changes by
+ * what `to` holds of each page less what `from` held.
+ *   parent        DEVICE [to->B] int32
+ *   to            k_tail, v_tail, table, lengths and references are all other arrays (B may then be
+ *                 another; from is still what it was, but only one of the two may go on), or all from's
+ *                 own: then a sequence can only stay, parent[b] = b, or leave, any other number.
+ *                 Codes and scales are from's own (the call does not touch them) */
+wave_status wave_pages_reorder(const wave_pages *from, const wave_pages *to, const int32_t *parent,
+                               void *hip_stream);
 
 /* Test hook, host only: the k_s distinct seed-token indices (relative to the
  * segment start) with which segment s of unit (b, h) starts k-means: the first

@@ -29,7 +29,9 @@ EXPORTS = ("wave_index_plan", "wave_index_build", "wave_index_append_plan", "wav
            "wave_full_attention_workspace", "wave_full_attention_decode", "wave_init_indices",
            "wave_rotary_plan", "wave_rotary_apply", "wave_cache_append",
            "wave_cache_attention_workspace", "wave_cache_attention_decode",
-           "wave_cache_evict_workspace", "wave_cache_evict",
+           "wave_cache_evict_workspace", "wave_cache_evict", "wave_norm_rotary_apply",
+           "wave_pages_append_workspace", "wave_pages_append", "wave_pages_read",
+           "wave_pages_attention_workspace", "wave_pages_attention_decode", "wave_pages_reorder",
            "wave_kmeans_assign_step", "wave_calibration_copy", "wave_calibration_read",
            "wave_profile_enable", "wave_profile_read", "wave_status_string")
 
@@ -67,6 +69,24 @@ class wave_cache(ctypes.Structure):
                 ("d", ctypes.c_int32), ("capacity", ctypes.c_int32),
                 ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("weights", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("tokens", ctypes.c_void_p)]
+
+
+class wave_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64)]
+
+
+class wave_head_norm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+class wave_pages(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("page", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("k_tail", ctypes.c_void_p), ("v_tail", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("references", ctypes.c_void_p)]
 
 
 class WaveError(RuntimeError):
@@ -118,6 +138,15 @@ def lib() -> ctypes.CDLL:
         L.wave_cache_evict_workspace.argtypes = [ctypes.POINTER(wave_cache), i32]
         L.wave_cache_evict.argtypes = [ctypes.POINTER(wave_cache), ctypes.POINTER(wave_cache), i32, i32, i32,
                                        vp, sz, vp]
+        rows, pages = ctypes.POINTER(wave_rows), ctypes.POINTER(wave_pages)
+        norm, rotary = ctypes.POINTER(wave_head_norm), ctypes.POINTER(wave_rotary)
+        L.wave_norm_rotary_apply.argtypes = [rows, i32, rows, i32, norm, rotary, vp, i32, i32, i32, i32, vp, vp, vp]
+        L.wave_pages_append_workspace.argtypes = [pages]
+        L.wave_pages_append.argtypes = [pages, pages, rows, rows, rows, i32, i32, vp, norm, rotary, vp, vp, vp, sz, vp]
+        L.wave_pages_read.argtypes = [pages, vp, i32, vp, vp, vp]
+        L.wave_pages_attention_workspace.argtypes = [pages, i32]
+        L.wave_pages_attention_decode.argtypes = [vp, i32, pages, vp, vp, vp, sz, vp]
+        L.wave_pages_reorder.argtypes = [pages, pages, vp, vp]
         L.wave_init_indices.argtypes = [u64, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int32)]
         L.wave_kmeans_assign_step.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp]
         L.wave_calibration_copy.argtypes = [vp, vp, sz, i32, vp]
@@ -135,6 +164,8 @@ def lib() -> ctypes.CDLL:
         L.wave_attention_decode_budget_workspace.restype = sz
         L.wave_cache_attention_workspace.restype = sz
         L.wave_cache_evict_workspace.restype = sz
+        L.wave_pages_append_workspace.restype = sz
+        L.wave_pages_attention_workspace.restype = sz
         _lib = L
     return _lib
 
@@ -667,6 +698,253 @@ def wave_cache_evict(cache: Cache, n_keep: int, n_sink: int, n_local: int, to: O
     _require(to.index == cache.index, 1, where)
     _together(where, cache.index, ws)
     _enqueue(where, cache.index, cache.ref, to.ref, n_keep, n_sink, n_local, ws.data_ptr(), ws.nbytes)
+    return to
+
+
+def _rows(t: torch.Tensor, to_keep: List[torch.Tensor]) -> wave_rows:
+    """t [B, H, N, d] as it lies where the library can read it so (rows of neighbouring channels, on 16 bytes), otherwise a
+    copy of it."""
+    shape, strides, unit = t.shape, t.stride(), 16 // t.element_size()
+    if strides[3] != 1 or t.data_ptr() % 16 or any([strides[i] % unit and shape[i] > 1 for i in (0, 1, 2)]):
+        t = t.contiguous()
+        strides = t.stride()
+    to_keep.append(t)
+    return wave_rows(t.data_ptr(), *[strides[i] if shape[i] > 1 else 0 for i in (0, 1, 2)])
+
+
+def _head_norm(where: str, dtype: torch.dtype, d: int, q_weight: Optional[torch.Tensor],
+               k_weight: Optional[torch.Tensor], eps: float, to_keep: List[torch.Tensor]) -> Optional[wave_head_norm]:
+    if q_weight is None and k_weight is None:
+        return None
+    at = []
+    for w in (q_weight, k_weight):
+        if w is not None:
+            if w.dtype != dtype:
+                raise WaveError(3, where)
+            if w.shape != (d,):
+                raise WaveError(2, where)
+            w = w.contiguous()
+            if w.data_ptr() % 16:
+                w = w.clone()
+            to_keep.append(w)
+        at.append(_address(w))
+    return wave_head_norm(*at, eps)
+
+
+def wave_norm_rotary_apply(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor] = None,
+                           k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                           coords: Optional[torch.Tensor] = None, rotary: Optional[wave_rotary] = None,
+                           q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """q [B, Hq, N, d] and k [B, Hkv, N, d] (one may be None), f32 or bf16 and of any strides (views of a fused projection
+    are read where they lie): every row normed by its weight [d] (None: not normed), x * weight / sqrt(mean(x^2) + eps),
+    then turned by coords [n_axes, B, N] int32.  Returns (q, k) so, dense, in q_out and k_out where they are given (a dense
+    input itself: in place)."""
+    where = "wave_norm_rotary_apply"
+    given = [t for t in (q, k) if t is not None]
+    _require(bool(given) and all([t.dim() == 4 for t in given]), 2, where)
+    B, _, N, d = given[0].shape
+    dtype, index = given[0].dtype, given[0].get_device()
+    _require(all([t.shape[0] == B and t.shape[2] == N and t.shape[3] == d for t in given]), 2, where)
+    _require(all([t.dtype == dtype for t in given]), 3, where)
+    keep: List[torch.Tensor] = []
+    if coords is not None:
+        _require(rotary is not None, 1, where)
+        _require(coords.dtype == torch.int32, 3, where)
+        _require(coords.shape == (rotary.n_axes, B, N), 2, where)
+        coords = coords.contiguous()
+    norm = _head_norm(where, dtype, d, q_weight, k_weight, eps, keep)
+    outs, rows = [], []
+    for t, out in ((q, q_out), (k, k_out)):
+        if t is None:
+            outs.append(None)
+            rows.append(None)
+            continue
+        outs.append(torch.empty_like(t, memory_format=torch.contiguous_format) if out is None else _as_is(where, out, dtype, t.shape))
+        rows.append(_rows(t, keep))
+    _together(where, index, q, k, q_weight, k_weight, coords, *outs)
+    if B and N and all([t.shape[1] for t in given]):
+        _enqueue(where, index, rows[0], 0 if q is None else q.shape[1], rows[1], 0 if k is None else k.shape[1], norm, rotary,
+                 _address(coords), _dtype_code(dtype), B, N, d, _address(outs[0]), _address(outs[1]))
+    return outs[0], outs[1]
+
+
+PAGE_POOL = ("k_codes", "v_codes", "k_scales", "v_scales")
+PAGE_STATE = ("k_tail", "v_tail", "table", "lengths", "references")
+
+
+class Pages:
+    """A wave_pages struct plus the torch tensors that own its arrays: the pool's k_codes and v_codes [n_pages, Hkv, page, d]
+    int8, k_scales and v_scales [n_pages, Hkv]; the sequences' k_tail and v_tail [B, Hkv, page, d], table [B, max_pages],
+    lengths [B] and references [n_pages]."""
+
+    def __init__(self, c: wave_pages, tensors: Dict[str, torch.Tensor], dtype: torch.dtype):
+        self.c = c
+        self.t = tensors
+        self.dtype = dtype
+        self.B, self.Hkv, self.d, self.page = c.B, c.Hkv, c.d, c.page
+        self.n_pages, self.max_pages = c.n_pages, c.max_pages
+        self.ref = ctypes.byref(c)
+        self.index = tensors["k_codes"].get_device()
+
+    def __getattr__(self, name):
+        t = self.__dict__.get("t", {})
+        if name in t:
+            return t[name]
+        raise AttributeError(name)
+
+
+def pages_from_tensors(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                       k_tail: torch.Tensor, v_tail: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                       references: torch.Tensor) -> Pages:
+    """A paged cache over tensors that the caller holds; they are taken as they are (contiguous, one GPU)."""
+    where = "pages_from_tensors"
+    _require(k_codes.dim() == 4 and k_tail.dim() == 4 and table.dim() == 2, 2, where)
+    n_pages, Hkv, page, d = k_codes.shape
+    B, max_pages = table.shape
+    for t, dt, shape in ((k_codes, torch.int8, (n_pages, Hkv, page, d)), (v_codes, torch.int8, (n_pages, Hkv, page, d)),
+                         (k_scales, torch.float32, (n_pages, Hkv)), (v_scales, torch.float32, (n_pages, Hkv)),
+                         (k_tail, k_tail.dtype, (B, Hkv, page, d)), (v_tail, k_tail.dtype, (B, Hkv, page, d)),
+                         (table, torch.int32, (B, max_pages)), (lengths, torch.int32, (B,)), (references, torch.int32, (n_pages,))):
+        _as_is(where, t, dt, shape)
+        _require(t.device == k_codes.device, 1, where)
+    tensors = dict(zip(PAGE_POOL + PAGE_STATE, (k_codes, v_codes, k_scales, v_scales, k_tail, v_tail, table, lengths, references)))
+    c = wave_pages()
+    c.dtype, c.B, c.Hkv, c.d, c.page, c.n_pages, c.max_pages = _dtype_code(k_tail.dtype), B, Hkv, d, page, n_pages, max_pages
+    for name, t in tensors.items():
+        setattr(c, name, _ptr(t))
+    return Pages(c, tensors, k_tail.dtype)
+
+
+def alloc_pages(dtype: torch.dtype, B: int, Hkv: int, d: int, page: int, n_pages: int, max_pages: int, device="cuda",
+                pool: Optional[Pages] = None) -> Pages:
+    """An empty paged cache; with `pool` another state over that cache's pages (for what wave_pages_append and
+    wave_pages_reorder leave beside it)."""
+    new = dict(device=torch.empty(0, device=device).device)
+    if pool is None:
+        held = [torch.zeros(n_pages, Hkv, page, d, dtype=torch.int8, **new) for _ in range(2)] + \
+               [torch.zeros(n_pages, Hkv, **new) for _ in range(2)]
+    else:
+        held = [pool.t[name] for name in PAGE_POOL]
+    return pages_from_tensors(*held, torch.empty(B, Hkv, page, d, dtype=dtype, **new), torch.empty(B, Hkv, page, d, dtype=dtype, **new),
+                              torch.full((B, max_pages), -1, dtype=torch.int32, **new), torch.zeros(B, dtype=torch.int32, **new),
+                              torch.zeros(n_pages, dtype=torch.int32, **new))
+
+
+def wave_pages_append_workspace(pages: Pages) -> int:
+    return int(lib().wave_pages_append_workspace(pages.ref))
+
+
+def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                      q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                      coords: Optional[torch.Tensor] = None, rotary: Optional[wave_rotary] = None,
+                      counts: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, to: Optional[Pages] = None,
+                      ws: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """k, v [B, Hkv, n, d] and q [B, Hq, n, d] of n new tokens per sequence (counts [B] int32: of its first counts[b]), of any
+    strides.  Norms and turns q and k as wave_norm_rotary_apply (coords None: the tokens' numbers) and puts k and v behind
+    each sequence's rows, in place or into the state `to`; a page that becomes complete is held in 8 bits.  Returns q normed
+    and turned (q_out, which may be q where that is dense)."""
+    where = "wave_pages_append"
+    to = pages if to is None else to
+    B, d, dtype, shape = pages.B, pages.d, pages.dtype, k.shape
+    if len(shape) != 4 or shape[0] != B or shape[1] != pages.Hkv or shape[3] != d or v.shape != shape:
+        raise WaveError(2, where)
+    if k.dtype != dtype or v.dtype != dtype:
+        raise WaveError(3, where)
+    n, Hq = shape[2], 0
+    keep: List[torch.Tensor] = []
+    rows_q = None
+    if q is not None:
+        heads = q.shape
+        if len(heads) != 4 or heads[0] != B or heads[2] != n or heads[3] != d:
+            raise WaveError(2, where)
+        if q.dtype != dtype:
+            raise WaveError(3, where)
+        Hq = heads[1]
+        if q_out is None:
+            new = torch.empty_like if counts is None else torch.zeros_like
+            q_out = new(q, memory_format=torch.contiguous_format)
+        else:
+            _as_is(where, q_out, dtype, heads)
+        rows_q = _rows(q, keep)
+    else:
+        q_out = None
+    if coords is not None:
+        if coords.dtype != torch.int32:
+            raise WaveError(3, where)
+        if rotary is None:
+            raise WaveError(1, where)
+        if coords.shape != (rotary.n_axes, B, n):
+            raise WaveError(2, where)
+        coords = coords.contiguous()
+    if counts is not None:
+        if counts.dtype != torch.int32:
+            raise WaveError(3, where)
+        if counts.shape != (B,):
+            raise WaveError(2, where)
+        counts = counts.contiguous()
+    norm = _head_norm(where, dtype, d, q_weight, k_weight, eps, keep)
+    if ws is None:
+        ws = workspace(wave_pages_append_workspace(pages), pages.t["k_codes"].device)
+    _require(to.index == pages.index, 1, where)
+    _together(where, pages.index, k, v, q, q_out, q_weight, k_weight, coords, counts, ws)
+    _enqueue(where, pages.index, pages.ref, to.ref, _rows(k, keep), _rows(v, keep), rows_q, Hq, n, _address(counts), norm, rotary,
+             _address(coords), _address(q_out), ws.data_ptr(), ws.nbytes)
+    return q_out
+
+
+def wave_pages_read(pages: Pages, n: int, first: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                    v_out: Optional[torch.Tensor] = None):
+    """Rows first[b] .. first[b] + n - 1 (first [B] int32, None: from 0 on) of every sequence in the storage type: (k, v), each
+    [B, Hkv, n, d].  Rows that a sequence has not stay as they are in k_out and v_out, and are 0 where those are not given."""
+    where = "wave_pages_read"
+    shape = (pages.B, pages.Hkv, n, pages.d)
+    _require(n >= 0, 1, where)
+    if first is not None:
+        _require(first.dtype == torch.int32, 3, where)
+        _require(first.shape == (pages.B,), 2, where)
+        first = first.contiguous()
+    outs = [torch.zeros(shape, dtype=pages.dtype, device=pages.t["k_codes"].device) if t is None else
+            _as_is(where, t, pages.dtype, shape) for t in (k_out, v_out)]
+    _together(where, pages.index, first, *outs)
+    if n:
+        _enqueue(where, pages.index, pages.ref, _address(first), n, outs[0].data_ptr(), outs[1].data_ptr())
+    return outs[0], outs[1]
+
+
+def wave_pages_attention_workspace(pages: Pages, Hq: int) -> int:
+    return int(lib().wave_pages_attention_workspace(pages.ref, Hq))
+
+
+def wave_pages_attention_decode(q: torch.Tensor, pages: Pages, out: Optional[torch.Tensor] = None,
+                                lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """q [B, Hq, d] against each sequence's rows.  Returns (out [B,Hq,d] f32, lse [B,Hq] f32)."""
+    where = "wave_pages_attention_decode"
+    shape = q.shape
+    _require(len(shape) == 3 and shape[0] == pages.B and shape[2] == pages.d, 2, where)
+    _require(q.dtype == pages.dtype, 3, where)
+    out = torch.empty_like(q, dtype=torch.float32, memory_format=torch.contiguous_format) if out is None else \
+        _as_is(where, out, torch.float32, shape)
+    lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if lse is None else \
+        _as_is(where, lse, torch.float32, shape[:2])
+    if ws is None:
+        ws = workspace(wave_pages_attention_workspace(pages, shape[1]), pages.t["k_codes"].device)
+    _together(where, pages.index, q, out, lse, ws)
+    q = q.contiguous()
+    _enqueue(where, pages.index, q.data_ptr(), shape[1], pages.ref, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.nbytes)
+    return out, lse
+
+
+def wave_pages_reorder(pages: Pages, parent: torch.Tensor, to: Optional[Pages] = None) -> Pages:
+    """Sequence b of `to` becomes what sequence parent[b] of `pages` was (parent [to.B] int32; one outside: an empty one), with
+    the pages shared.  Without `to`, in place: a sequence stays (parent[b] = b) or leaves.  Returns the state that holds them."""
+    where = "wave_pages_reorder"
+    to = pages if to is None else to
+    _require(parent.dtype == torch.int32, 3, where)
+    _require(parent.shape == (to.B,), 2, where)
+    _require(to.index == pages.index, 1, where)
+    _together(where, pages.index, parent)
+    parent = parent.contiguous()
+    _enqueue(where, pages.index, pages.ref, to.ref, parent.data_ptr())
     return to
 
 

@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libwave.so")
 SOURCES = ["wave_api.hip", "wave_decode.hip", "wave_build.hip", "wave_append.hip",
-           "wave_cache.hip", "wave_cache_attention.hip"]
+           "wave_cache.hip", "wave_cache_attention.hip", "wave_pages.hip", "wave_pages_attention.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc", "-Wall",
          "-Wno-unused-function",
          # packed fp32 instructions are kept out of the generated code

@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 
 #include "wave_common.h"
@@ -722,6 +723,269 @@ wave_status wave_cache_evict(const wave_cache* from, const wave_cache* to, int n
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need)
     return WAVE_ERR_WORKSPACE;
   return launch_cache_evict(*from, *to, n_keep, n_sink, n_local, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+// ----------------------------------------------------------------------------
+// Norms with rotary positions, and the paged cache
+// ----------------------------------------------------------------------------
+// What a call reads or writes.  Nothing that it writes may overlap anything else of these; a pair that may be the same array
+// is left to the caller of clash().
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+static bool clash(std::initializer_list<Span> writes, std::initializer_list<Span> reads) {
+  for (const Span* w = writes.begin(); w != writes.end(); ++w) {
+    for (const Span* o = w + 1; o != writes.end(); ++o)
+      if (overlaps(w->at, w->bytes, o->at, o->bytes)) return true;
+    for (const Span& r : reads)
+      if (overlaps(w->at, w->bytes, r.at, r.bytes)) return true;
+  }
+  return false;
+}
+
+// Strided rows [B, H, N]: what they span, and whether they lie as a dense array does.
+static wave_status check_rows(const wave_rows& r, int dtype, int B, int H, int N, int d, Span* span, HeadRows* out) {
+  const int64_t es = (int64_t)elem_bytes(dtype), unit = 16 / es, most = int64_t(1) << 60;
+  if (!r.data || !aligned16(r.data)) return WAVE_ERR_ARG;
+  const int64_t strides[3] = {r.stride_b, r.stride_h, r.stride_n}, counts[3] = {B, H, N};
+  double last = d;  // (only to find spans that no memory has)
+  int64_t end = d;
+  for (int i = 0; i < 3; ++i) {
+    if (strides[i] < 0 || strides[i] % unit) return WAVE_ERR_ARG;
+    last += (double)strides[i] * (double)(counts[i] - 1);
+    if (last > (double)most / es) return WAVE_ERR_SHAPE;
+    end += strides[i] * (counts[i] - 1);
+  }
+  *span = Span{r.data, (size_t)(end * es)};
+  *out = HeadRows{static_cast<const char*>(r.data), r.stride_b * es, r.stride_h * es, r.stride_n * es};
+  return WAVE_OK;
+}
+static bool dense_rows(const wave_rows& r, int B, int H, int N, int d) {
+  return (N == 1 || r.stride_n == d) && (H == 1 || r.stride_h == (int64_t)N * d) && (B == 1 || r.stride_b == (int64_t)H * N * d);
+}
+static wave_status check_norm(const wave_head_norm* n, NormArgs* a) {
+  if (!n) return WAVE_OK;
+  if (!(n->eps >= 0.f) || !(n->eps < HUGE_VALF) || !aligned16(n->q_weight) || !aligned16(n->k_weight)) return WAVE_ERR_ARG;
+  a->q_weight = static_cast<const char*>(n->q_weight);
+  a->k_weight = static_cast<const char*>(n->k_weight);
+  a->eps = n->eps;
+  return WAVE_OK;
+}
+
+wave_status wave_norm_rotary_apply(const wave_rows* q, int Hq, const wave_rows* k, int Hkv, const wave_head_norm* norm,
+                                   const wave_rotary* rotary, const int32_t* coords, int dtype, int B, int N, int d,
+                                   void* q_out, void* k_out, void* hip_stream) {
+  if (dtype != WAVE_F32 && dtype != WAVE_BF16) return WAVE_ERR_DTYPE;
+  if ((!q && !k) || B < 1 || N < 1 || (q && Hq < 1) || (k && Hkv < 1)) return WAVE_ERR_ARG;
+  if (rotary ? !coords : (coords || !norm)) return WAVE_ERR_ARG;
+  if (d != 64 && d != 128) return WAVE_ERR_SHAPE;
+  NormArgs a{};
+  wave_status st = check_norm(norm, &a);
+  if (st != WAVE_OK) return st;
+  RotaryArgs rot{};
+  if (rotary) {
+    st = check_rotary(rotary, d, &rot);
+    if (st != WAVE_OK) return st;
+  }
+  a.Hq = q ? Hq : 0;
+  a.Hk = k ? Hkv : 0;
+  const long long heads = (long long)a.Hq + a.Hk;
+  if (B * heads >= (1ll << 31) || (long long)B * N >= (1ll << 31) || heads > (1 << 30) || N > (1 << 30)) return WAVE_ERR_SHAPE;
+  const size_t row = (size_t)B * N * d * elem_bytes(dtype);
+  Span qs{}, ks{};
+  const Span qo{q ? q_out : nullptr, row * a.Hq}, ko{k ? k_out : nullptr, row * a.Hk};
+  if (q) {
+    st = check_rows(*q, dtype, B, Hq, N, d, &qs, &a.q);
+    if (st != WAVE_OK) return st;
+    if (!q_out || !aligned16(q_out)) return WAVE_ERR_ARG;
+  }
+  if (k) {
+    st = check_rows(*k, dtype, B, Hkv, N, d, &ks, &a.k);
+    if (st != WAVE_OK) return st;
+    if (!k_out || !aligned16(k_out)) return WAVE_ERR_ARG;
+  }
+  const bool q_same = q && q_out == q->data && dense_rows(*q, B, Hq, N, d);
+  const bool k_same = k && k_out == k->data && dense_rows(*k, B, Hkv, N, d);
+  const size_t wb = (size_t)d * elem_bytes(dtype);
+  const Span weights[2] = {{a.q_weight, wb}, {a.k_weight, wb}};
+  const Span at{coords, rotary ? sizeof(int32_t) * (size_t)rotary->n_axes * B * N : 0};
+  const std::initializer_list<Span> writes = {qo, ko};
+  const std::initializer_list<Span> reads = {q_same ? Span{} : qs, k_same ? Span{} : ks, weights[0], weights[1], at};
+  if (clash(writes, reads)) return WAVE_ERR_ARG;
+  a.q_out = static_cast<char*>(q_out);
+  a.k_out = static_cast<char*>(k_out);
+  a.coords = coords;
+  a.B = B;
+  a.N = N;
+  a.turns = rotary != nullptr;
+  return launch_norm_rotary(a, rot, dtype, d, static_cast<hipStream_t>(hip_stream));
+}
+
+static wave_status check_pages(const wave_pages* p) {
+  if (!p) return WAVE_ERR_ARG;
+  if (p->dtype != WAVE_F32 && p->dtype != WAVE_BF16) return WAVE_ERR_DTYPE;
+  if (p->B < 1 || p->Hkv < 1 || p->n_pages < 1 || p->max_pages < 1) return WAVE_ERR_ARG;
+  if ((p->d != 64 && p->d != 128) || (p->page != 32 && p->page != 64 && p->page != 128)) return WAVE_ERR_SHAPE;
+  if ((long long)p->B * p->Hkv * 8 >= kMaxGrid || p->n_pages > (1 << 28) || (long long)p->max_pages * p->page > (1 << 30))
+    return WAVE_ERR_SHAPE;
+  return WAVE_OK;
+}
+static wave_status check_pages_buffers(const wave_pages& p, bool counted) {
+  if (!p.k_codes || !p.v_codes || !p.k_scales || !p.v_scales || !p.k_tail || !p.v_tail || !p.table || !p.lengths ||
+      (counted && !p.references))
+    return WAVE_ERR_ARG;
+  if (!aligned16(p.k_codes) || !aligned16(p.v_codes) || !aligned16(p.k_tail) || !aligned16(p.v_tail)) return WAVE_ERR_ARG;
+  return WAVE_OK;
+}
+struct PagesBytes {
+  size_t codes, scales, tail, table, lengths, references;
+  explicit PagesBytes(const wave_pages& p)
+      : codes((size_t)p.n_pages * p.Hkv * p.page * p.d), scales(sizeof(float) * (size_t)p.n_pages * p.Hkv),
+        tail((size_t)p.B * p.Hkv * p.page * p.d * elem_bytes(p.dtype)), table(sizeof(int32_t) * (size_t)p.B * p.max_pages),
+        lengths(sizeof(int32_t) * (size_t)p.B), references(sizeof(int32_t) * (size_t)p.n_pages) {}
+};
+// Two states of one pool: *apart says whether `to` has its own arrays.  B may differ where that is allowed.
+static wave_status check_states(const wave_pages* from, const wave_pages* to, bool any_B, bool* apart) {
+  for (const wave_pages* p : {from, to}) {
+    wave_status st = check_pages(p);
+    if (st != WAVE_OK) return st;
+    st = check_pages_buffers(*p, true);
+    if (st != WAVE_OK) return st;
+  }
+  if (to->dtype != from->dtype || to->Hkv != from->Hkv || to->d != from->d || to->page != from->page ||
+      to->n_pages != from->n_pages || to->max_pages != from->max_pages)
+    return WAVE_ERR_SHAPE;
+  if (to->k_codes != from->k_codes || to->v_codes != from->v_codes || to->k_scales != from->k_scales || to->v_scales != from->v_scales)
+    return WAVE_ERR_ARG;
+  const int same = (to->k_tail == from->k_tail) + (to->v_tail == from->v_tail) + (to->table == from->table) +
+                   (to->lengths == from->lengths) + (to->references == from->references);
+  if (same != 0 && same != 5) return WAVE_ERR_ARG;
+  *apart = same == 0;
+  if (to->B != from->B && !(any_B && *apart)) return WAVE_ERR_SHAPE;
+  return WAVE_OK;
+}
+
+size_t wave_pages_append_workspace(const wave_pages* from) {
+  return check_pages(from) == WAVE_OK ? pages_append_workspace(*from) : 0;
+}
+
+wave_status wave_pages_append(const wave_pages* from, const wave_pages* to, const wave_rows* k_new, const wave_rows* v_new,
+                              const wave_rows* q, int Hq, int n_new, const int32_t* counts, const wave_head_norm* norm,
+                              const wave_rotary* rotary, const int32_t* coords, void* q_out, void* workspace,
+                              size_t workspace_bytes, void* hip_stream) {
+  bool apart;
+  wave_status st = check_states(from, to, false, &apart);
+  if (st != WAVE_OK) return st;
+  const wave_pages& p = *from;
+  if (!k_new || !v_new || n_new < 1 || (q && Hq < 1) || (coords && !rotary)) return WAVE_ERR_ARG;
+  if (n_new > (1 << 30) || (long long)p.B * n_new >= (1ll << 31) || (q && (long long)p.B * Hq >= kMaxGrid)) return WAVE_ERR_SHAPE;
+  PagesAppendArgs a{};
+  NormArgs& r = a.rows;
+  st = check_norm(norm, &r);
+  if (st != WAVE_OK) return st;
+  if (q && !rotary && !r.q_weight) return WAVE_ERR_ARG;
+  RotaryArgs rot{};
+  if (rotary) {
+    st = check_rotary(rotary, p.d, &rot);
+    if (st != WAVE_OK) return st;
+  }
+  Span ks{}, vs{}, qs{};
+  st = check_rows(*k_new, p.dtype, p.B, p.Hkv, n_new, p.d, &ks, &a.k_new);
+  if (st == WAVE_OK) st = check_rows(*v_new, p.dtype, p.B, p.Hkv, n_new, p.d, &vs, &a.v_new);
+  if (st == WAVE_OK && q) st = check_rows(*q, p.dtype, p.B, Hq, n_new, p.d, &qs, &r.q);
+  if (st != WAVE_OK) return st;
+  if (q && (!q_out || !aligned16(q_out))) return WAVE_ERR_ARG;
+  if (q && q_out == q->data && dense_rows(*q, p.B, Hq, n_new, p.d)) qs = Span{};
+  const size_t es = elem_bytes(p.dtype), wb = (size_t)p.d * es;
+  const PagesBytes x(p);
+  const std::initializer_list<Span> writes = {{to->k_tail, x.tail}, {to->v_tail, x.tail}, {to->table, x.table}, {to->lengths, x.lengths},
+                           {to->references, x.references}, {to->k_codes, x.codes}, {to->v_codes, x.codes}, {to->k_scales, x.scales},
+                           {to->v_scales, x.scales}, {q ? q_out : nullptr, q ? (size_t)p.B * Hq * n_new * wb : 0},
+                           {workspace, pages_append_workspace(p)}};
+  const Span none{};
+  const std::initializer_list<Span> reads = {ks, vs, qs, {counts, x.lengths}, {coords, rotary ? sizeof(int32_t) * (size_t)rotary->n_axes * p.B * n_new : 0},
+                          {r.q_weight, wb}, {r.k_weight, wb}, apart ? Span{p.k_tail, x.tail} : none, apart ? Span{p.v_tail, x.tail} : none,
+                          apart ? Span{p.table, x.table} : none, apart ? Span{p.lengths, x.lengths} : none,
+                          apart ? Span{p.references, x.references} : none};
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < pages_append_workspace(p))
+    return WAVE_ERR_WORKSPACE;
+  if (clash(writes, reads)) return WAVE_ERR_ARG;
+  r.coords = coords;
+  r.q_out = static_cast<char*>(q_out);
+  r.B = p.B;
+  r.Hq = q ? Hq : 0;
+  r.N = n_new;
+  r.turns = rotary != nullptr;
+  a.counts = counts;
+  a.n = n_new;
+  a.apart = apart;
+  return launch_pages_append(*from, *to, a, rot, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+wave_status wave_pages_read(const wave_pages* pages, const int32_t* first, int n, void* k_out, void* v_out, void* hip_stream) {
+  wave_status st = check_pages(pages);
+  if (st != WAVE_OK) return st;
+  st = check_pages_buffers(*pages, false);
+  if (st != WAVE_OK) return st;
+  const wave_pages& p = *pages;
+  if (n < 1 || (!k_out && !v_out) || !aligned16(k_out) || !aligned16(v_out)) return WAVE_ERR_ARG;
+  if (n > (1 << 30) || (double)p.B * p.Hkv * n >= (double)(1ll << 34)) return WAVE_ERR_SHAPE;
+  const PagesBytes x(p);
+  const size_t bytes = (size_t)p.B * p.Hkv * n * p.d * elem_bytes(p.dtype);
+  const std::initializer_list<Span> writes = {{k_out, bytes}, {v_out, bytes}};
+  const std::initializer_list<Span> reads = {{p.k_codes, x.codes}, {p.v_codes, x.codes}, {p.k_scales, x.scales}, {p.v_scales, x.scales}, {p.k_tail, x.tail},
+                         {p.v_tail, x.tail}, {p.table, x.table}, {p.lengths, x.lengths}, {first, x.lengths}};
+  if (clash(writes, reads)) return WAVE_ERR_ARG;
+  return launch_pages_read(p, first, n, k_out, v_out, static_cast<hipStream_t>(hip_stream));
+}
+
+static wave_status check_pages_attention(const wave_pages* p, int Hq) {
+  const wave_status st = check_pages(p);
+  if (st != WAVE_OK) return st;
+  if (Hq < p->Hkv || Hq % p->Hkv != 0 || Hq / p->Hkv > 8 || (long long)p->B * Hq >= kMaxGrid) return WAVE_ERR_SHAPE;
+  return WAVE_OK;
+}
+
+size_t wave_pages_attention_workspace(const wave_pages* pages, int Hq) {
+  return check_pages_attention(pages, Hq) == WAVE_OK ? pages_attend_geometry(*pages, Hq).total : 0;
+}
+
+wave_status wave_pages_attention_decode(const void* q, int Hq, const wave_pages* pages, float* out, float* lse, void* workspace,
+                                        size_t workspace_bytes, void* hip_stream) {
+  wave_status st = check_pages_attention(pages, Hq);
+  if (st != WAVE_OK) return st;
+  st = check_pages_buffers(*pages, false);
+  if (st != WAVE_OK) return st;
+  const wave_pages& p = *pages;
+  if (!q || !aligned16(q) || !out || !lse || (reinterpret_cast<uintptr_t>(out) & 3u) || (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return WAVE_ERR_ARG;
+  const size_t need = pages_attend_geometry(p, Hq).total;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need) return WAVE_ERR_WORKSPACE;
+  const PagesBytes x(p);
+  const size_t heads = (size_t)p.B * Hq;
+  const std::initializer_list<Span> writes = {{out, heads * p.d * sizeof(float)}, {lse, heads * sizeof(float)}, {workspace, need}};
+  const std::initializer_list<Span> reads = {{q, heads * p.d * elem_bytes(p.dtype)}, {p.k_codes, x.codes}, {p.v_codes, x.codes}, {p.k_scales, x.scales},
+                         {p.v_scales, x.scales}, {p.k_tail, x.tail}, {p.v_tail, x.tail}, {p.table, x.table}, {p.lengths, x.lengths}};
+  if (clash(writes, reads)) return WAVE_ERR_ARG;
+  return launch_pages_attend(q, Hq, p, out, lse, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+wave_status wave_pages_reorder(const wave_pages* from, const wave_pages* to, const int32_t* parent, void* hip_stream) {
+  bool apart;
+  const wave_status st = check_states(from, to, true, &apart);
+  if (st != WAVE_OK) return st;
+  if (!parent) return WAVE_ERR_ARG;
+  const PagesBytes x(*from), y(*to);
+  const Span none{};
+  const std::initializer_list<Span> writes = {{to->k_tail, y.tail}, {to->v_tail, y.tail}, {to->table, y.table}, {to->lengths, y.lengths},
+                          {to->references, y.references}};
+  const std::initializer_list<Span> reads = {{parent, y.lengths}, {from->k_codes, x.codes}, {from->v_codes, x.codes}, {from->k_scales, x.scales},
+                          {from->v_scales, x.scales}, apart ? Span{from->k_tail, x.tail} : none, apart ? Span{from->v_tail, x.tail} : none,
+                          apart ? Span{from->table, x.table} : none, apart ? Span{from->lengths, x.lengths} : none,
+                          apart ? Span{from->references, x.references} : none};
+  if (clash(writes, reads)) return WAVE_ERR_ARG;
+  return launch_pages_reorder(*from, *to, parent, static_cast<hipStream_t>(hip_stream));
 }
 
 wave_status wave_init_indices(uint64_t seed, int b, int h, int s, int L_s, int k_s, int32_t* out) {

@@ -397,6 +397,41 @@ CacheEvictGeom cache_evict_geometry(const wave_cache& from, int n_keep);
 wave_status launch_cache_evict(const wave_cache& from, const wave_cache& to, int n_keep, int n_sink, int n_local,
                                void* ws, hipStream_t st);
 
+// Norms with rotary positions, and the paged cache (wave_pages.hip, wave_pages_attention.hip).
+struct HeadRows {
+  const char* data;
+  long long b, h, n;  // strides in bytes
+};
+struct NormArgs {
+  HeadRows q, k;
+  char *q_out, *k_out;              // dense
+  const char *q_weight, *k_weight;  // NULL: not normed
+  const int32_t* coords;            // [n_axes][B][N]
+  int B, Hq, Hk, N;                 // (a tensor that is not there has no heads)
+  float eps;
+  bool turns;
+};
+wave_status launch_norm_rotary(const NormArgs& a, const RotaryArgs& rot, int dtype, int d, hipStream_t st);
+struct PagesAppendArgs {
+  NormArgs rows;               // q alone, and coords, k_weight and eps for the keys
+  HeadRows k_new, v_new;
+  const int32_t* counts;
+  int n;
+  bool apart;                  // `to` has arrays of its own
+};
+size_t pages_append_workspace(const wave_pages& p);
+wave_status launch_pages_append(const wave_pages& from, const wave_pages& to, PagesAppendArgs a, const RotaryArgs& rot,
+                                void* ws, hipStream_t st);
+wave_status launch_pages_read(const wave_pages& p, const int32_t* first, int n, void* k_out, void* v_out, hipStream_t st);
+wave_status launch_pages_reorder(const wave_pages& from, const wave_pages& to, const int32_t* parent, hipStream_t st);
+struct PagesAttendGeom {
+  bool one_launch;           // short caches: one workgroup per unit, nothing in the workspace
+  int target, few, pieces;   // pieces of rows per KV head: aimed at, aimed at where they are short, room for
+  size_t off_info, off_ml, off_acc, total;
+};
+PagesAttendGeom pages_attend_geometry(const wave_pages& p, int Hq);
+wave_status launch_pages_attend(const void* q, int Hq, const wave_pages& p, float* out, float* lse, void* ws, hipStream_t st);
+
 // splitmix64-keyed Fisher-Yates seed points, shared by the host hook and the device kernel.
 __host__ __device__ inline uint64_t splitmix64_next(uint64_t& state) {
   state += 0x9E3779B97F4A7C15ull;

@@ -1,0 +1,701 @@
+// Norms with rotary positions, and the rows of the paged cache: appending new tokens, reading rows back, sharing pages.
+#include "wave_rotary.h"
+
+namespace wave {
+
+namespace {
+
+// ----------------------------------------------------------------------------
+// Norms with rotary positions.  The lanes of a row (the items of a turn) add up its squares with DPP; a thread keeps the
+// sines of its item of one token and goes through the token's heads with them.  Every fused multiply-add is written out:
+// a row has the same bits whichever kernel, and whichever form of it, norms and turns it.
+// ----------------------------------------------------------------------------
+template <int LANES>
+__device__ __forceinline__ float item_sum(float x) {
+  static_assert(LANES == 4 || LANES == 8 || LANES == 16, "lanes of a row");
+  x += dpp<DPP_XOR1>(x);
+  x += dpp<DPP_XOR2>(x);
+  if (LANES >= 8) x += dpp<DPP_HALF_MIRROR>(x);
+  if (LANES >= 16) x += dpp<DPP_MIRROR>(x);
+  return x;
+}
+
+template <typename T, int D>
+struct NormTurn : Turn<T, D> {
+  typedef Turn<T, D> Base;
+  static constexpr int EPC = Base::EPC, ITEMS = Base::ITEMS;
+  __device__ __forceinline__ void place(const RotaryArgs& r, bool rotates, int item) {
+    if (rotates) {
+      Base::place(r, item);
+    } else {
+      this->turns = false;
+      this->one = 2 * item;
+      this->two = 2 * item + 1;
+    }
+  }
+  // (as in the base, the circles coming off exactly)
+  template <typename F>
+  __device__ __forceinline__ void angles(const RotaryArgs& r, int item, F&& position) {
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) {
+      this->c[e] = 1.f;
+      this->s[e] = 0.f;
+      if (this->turns) {
+        const int i = item * EPC + e;
+        const double at = (double)position(r.axis[i]), per = r.turns[i];
+        const double part = fma(at, per, -rint(at * per));
+        sincospif((float)(part + part), &this->s[e], &this->c[e]);
+      }
+    }
+  }
+  __device__ __forceinline__ void pair(float& x, float& y, int e) const {
+    const float c = this->c[e], s = this->s[e], u = fmaf(x, c, -(y * s));
+    y = fmaf(x, s, y * c);
+    x = u;
+  }
+  __device__ __forceinline__ void turn(const RotaryArgs& r, float (&x)[EPC], float (&y)[EPC]) const {
+    if (r.pairing == WAVE_ROTARY_HALVES) {
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) pair(x[e], y[e], e);
+    } else {  // pairs of the first and of the second chunk
+#pragma unroll
+      for (int e = 0; e < EPC; e += 2) {
+        pair(x[e], x[e + 1], e / 2);
+        pair(y[e], y[e + 1], EPC / 2 + e / 2);
+      }
+    }
+  }
+  struct Weight {
+    uint4 a, b;
+    bool any;
+  };
+  __device__ __forceinline__ Weight weight(const char* w) const {
+    Weight r;
+    r.any = w != nullptr;
+    if (r.any) {
+      r.a = load16(w + this->one * 16);
+      r.b = load16(w + this->two * 16);
+    }
+    return r;
+  }
+  // All lanes of the row together.  x * (w / norm) in fp32, then the turn, then one rounding.
+  __device__ __forceinline__ void apply(const RotaryArgs& r, const Weight& w, float eps, uint4& a, uint4& b) const {
+    if (!w.any && !this->turns) return;
+    float x[EPC], y[EPC];
+    unpack<T>(a, x);
+    unpack<T>(b, y);
+    if (w.any) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) sum = fmaf(y[e], y[e], fmaf(x[e], x[e], sum));
+      const float f = rsqrtf(fmaf(item_sum<ITEMS>(sum), 1.f / D, eps));
+      float u[EPC], v[EPC];
+      unpack<T>(w.a, u);
+      unpack<T>(w.b, v);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        x[e] = x[e] * f * u[e];
+        y[e] = y[e] * f * v[e];
+      }
+    }
+    if (this->turns) turn(r, x, y);
+    a = pack<T>(x);
+    b = pack<T>(y);
+  }
+};
+
+__device__ __forceinline__ const char* row_of(const HeadRows& r, int b, int h, int n) {
+  return r.data + (b * r.b + h * r.h + n * r.n);
+}
+
+// The heads of a token are its q and then its k heads.  count: tokens that there are; position(axis, n).
+template <typename T, int D, typename Position>
+__device__ __forceinline__ void norm_heads(const NormArgs& a, const RotaryArgs& rot, const TurnShape& sh, int b, int tile, int group,
+                                           int count, Position&& position) {
+  typedef NormTurn<T, D> Tu;
+  constexpr size_t ROW = D * sizeof(T);
+  const int item = threadIdx.x % Tu::ITEMS, lane = (threadIdx.x / Tu::ITEMS) & ((1 << sh.lane_shift) - 1);
+  const int n = tile * sh.tokens + (int)(threadIdx.x / Tu::ITEMS >> sh.lane_shift);
+  if (n >= count) return;
+  Tu t;
+  t.place(rot, a.turns, item);
+  const int slots = a.Hq + a.Hk, step = sh.head_groups << sh.lane_shift;
+  uint4 u[TURN_BATCH], v[TURN_BATCH];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < TURN_BATCH; ++i) {
+      const int h = min(h0 + i * step, slots - 1);
+      const char* row = h < a.Hq ? row_of(a.q, b, h, n) : row_of(a.k, b, h - a.Hq, n);
+      u[i] = load16(row + t.one * 16);
+      v[i] = load16(row + t.two * 16);
+    }
+  };
+  // the first rows are on their way while the sines are formed
+  int h0 = (group << sh.lane_shift) + lane;
+  load(h0);
+  const typename Tu::Weight wq = t.weight(a.q_weight), wk = t.weight(a.k_weight);
+  if (a.turns) t.angles(rot, item, [&](int axis) { return position(axis, n); });
+  for (; h0 < slots;) {
+#pragma unroll
+    for (int i = 0; i < TURN_BATCH; ++i) {
+      const int h = h0 + i * step;
+      if (h < slots) {
+        const bool is_q = h < a.Hq;
+        typename Tu::Weight w = wk;
+        if (is_q) w = wq;
+        t.apply(rot, w, a.eps, u[i], v[i]);
+        char* row = is_q ? a.q_out + (((size_t)b * a.Hq + h) * a.N + n) * ROW : a.k_out + (((size_t)b * a.Hk + h - a.Hq) * a.N + n) * ROW;
+        store16(row + t.one * 16, u[i]);
+        store16(row + t.two * 16, v[i]);
+      }
+    }
+    h0 += TURN_BATCH * step;
+    if (h0 < slots) load(h0);
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void norm_rotary_kernel(const NormArgs a, const RotaryArgs rot, TurnShape sh, int tiles) {
+  const unsigned block = workgroup_number();
+  const int group = block % sh.head_groups, bt = block / sh.head_groups;
+  const int b = bt / tiles, tile = bt % tiles;
+  if (b >= a.B) return;
+  norm_heads<T, D>(a, rot, sh, b, tile, group, a.N,
+                   [&](int axis, int n) { return a.coords[((size_t)axis * a.B + b) * a.N + n]; });
+}
+
+template <typename T, int D>
+wave_status norm_rotary_td(const NormArgs& a, const RotaryArgs& rot, hipStream_t st) {
+  constexpr int ITEMS = Turn<T, D>::ITEMS;
+  const TurnShape sh = turn_shape<ITEMS>(a.N, a.B, a.Hq + a.Hk);
+  const int tiles = (a.N + sh.tokens - 1) / sh.tokens;
+  WAVE_LAUNCH("norm_rotary", (norm_rotary_kernel<T, D>), grid_rows((long long)a.B * tiles * sh.head_groups), 256, 0, st, a, rot, sh,
+              tiles);
+  return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
+}
+
+// ----------------------------------------------------------------------------
+// The paged cache
+// ----------------------------------------------------------------------------
+__host__ __device__ inline int page_shift(int page) { return page == 32 ? 5 : page == 64 ? 6 : 7; }
+__host__ __device__ inline int pages_room(const wave_pages& p) { return p.max_pages * p.page + p.page - 1; }
+__device__ __forceinline__ int pages_length(const wave_pages& p, int b) { return min(max(p.lengths[b], 0), pages_room(p)); }
+__device__ __forceinline__ int page_entry(const wave_pages& p, int b, int i) {
+  return min(max(p.table[(size_t)b * p.max_pages + i], 0), p.n_pages - 1);
+}
+
+// Append, first launch: one workgroup finds how many tokens of each sequence fit and which pages they take.  A sequence's
+// share depends on what those before it take, and the free pages are found by going through references in ascending order,
+// so the pages are the same in every run.  It is a chain of a few loads and scans behind barriers; its time is theirs.
+struct PagesPlan {
+  int4* sequence;   // [B] rows before, rows after, its first one among the taken pages, tokens given
+  int32_t* taken;   // [n_pages] the taken pages in ascending order
+  int32_t* last;    // [1] the last one (-1: none)
+};
+PagesPlan pages_plan(const wave_pages& p, void* ws) {
+  char* w = static_cast<char*>(ws);
+  PagesPlan r;
+  r.last = reinterpret_cast<int32_t*>(w);
+  r.sequence = reinterpret_cast<int4*>(w + 256);
+  r.taken = reinterpret_cast<int32_t*>(w + 256 + align_up(sizeof(int4) * (size_t)p.B));
+  return r;
+}
+
+constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64, PLAN_PER = 16, PLAN_ROUND = PLAN_PER * PLAN_THREADS;
+constexpr int PLAN_MANY = (1 << 30) - 1;  // sums stop here: more pages than there can be
+__device__ __forceinline__ int sum_to_many(int a, int b) { return min(a + b, PLAN_MANY); }
+
+__global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pages from, const wave_pages to, const int32_t* counts, int n,
+                                                                 const PagesPlan plan, bool apart) {
+  __shared__ int part[PLAN_WAVES], place[PLAN_PER * PLAN_WAVES + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, shift = page_shift(from.page);
+  // the first round's references are on their way while the lengths are looked at
+  int ref[PLAN_PER];
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < PLAN_PER; ++i) ref[i] = from.references[min(r0 + i * PLAN_THREADS + tid, from.n_pages - 1)];
+  };
+  load(0);
+  int wanted = 0;  // pages wanted by the sequences so far
+  for (int b0 = 0; b0 < from.B; b0 += PLAN_THREADS) {
+    const int b = b0 + tid;
+    int length = 0, count = 0, need = 0;
+    if (b < from.B) {
+      length = pages_length(from, b);
+      count = counts ? min(max(counts[b], 0), n) : n;
+      const int fit = min(count, pages_room(from) - length);
+      need = ((length + fit) >> shift) - (length >> shift);
+    }
+    const int incl = wave_scan(need, 0, sum_to_many);
+    if (lane == 63) part[wave] = incl;
+    __syncthreads();
+    int before = wanted;
+#pragma unroll
+    for (int w = 0; w < PLAN_WAVES; ++w) {
+      if (w == wave) before = wanted;
+      wanted = sum_to_many(wanted, part[w]);
+    }
+    // (where the sums stop, there is no page anyway)
+    const int below = __shfl_up(incl, 1);
+    if (b < from.B) plan.sequence[b] = make_int4(length, need, sum_to_many(before, lane ? below : 0), count);
+    __syncthreads();
+  }
+  int found = 0;
+  if (tid == 0) plan.last[0] = -1;
+  for (int r0 = 0; r0 < from.n_pages && found < wanted; r0 += PLAN_ROUND) {
+    uint64_t free[PLAN_PER];
+#pragma unroll
+    for (int i = 0; i < PLAN_PER; ++i) {
+      free[i] = __ballot(ref[i] <= 0 && r0 + i * PLAN_THREADS + tid < from.n_pages);
+      if (lane == 0) place[i * PLAN_WAVES + wave] = __popcll(free[i]);
+    }
+    __syncthreads();
+    if (r0 + PLAN_ROUND < from.n_pages) load(r0 + PLAN_ROUND);
+    if (wave == 0) {  // the sums before each of the 256 counts
+      int c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = place[lane * 4 + i];
+        sum += c[i];
+      }
+      const int incl = wave_incl_scan(sum);
+      int at = incl - sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        place[lane * 4 + i] = at;
+        at += c[i];
+      }
+      if (lane == 63) place[PLAN_PER * PLAN_WAVES] = incl;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PLAN_PER; ++i) {
+      const int rank = found + place[i * PLAN_WAVES + wave] + __popcll(free[i] & ((1ull << lane) - 1));
+      if ((free[i] >> lane & 1) && rank < wanted) {
+        const int page = r0 + i * PLAN_THREADS + tid;
+        plan.taken[rank] = page;
+        if (!apart) to.references[page] = 1;
+        if (rank == wanted - 1) plan.last[0] = page;
+      }
+    }
+    found += place[PLAN_PER * PLAN_WAVES];
+    __syncthreads();
+  }
+  if (found < wanted && tid == 0) plan.last[0] = from.n_pages;  // every free page is taken
+  for (int b = tid; b < from.B; b += PLAN_THREADS) {
+    int4 s = plan.sequence[b];
+    const int whole = s.x >> shift, got = min(max(found - s.z, 0), s.y);
+    int end = s.x + min(s.w, pages_room(from) - s.x);
+    if (got < s.y) end = ((whole + got + 1) << shift) - 1;
+    s.y = end;
+    plan.sequence[b] = s;
+    to.lengths[b] = end;
+  }
+}
+
+// Append, second launch.
+//   pages  a workgroup has some heads' keys or values of one page of a sequence: rows that were in the tail, new rows, or both.
+//          If the page is complete they are rounded to 8 bits (a thread keeps its 16 channels of every row between the maximum and
+//          the codes), otherwise they are the new tail.
+//   q      as in norm_rotary_kernel
+//   lists  table and references of a state with arrays of its own
+struct AppendGrid {
+  unsigned page_blocks, q_blocks;  // the others are lists
+  int units, head_groups;          // pages that a sequence's new tokens may touch; workgroups that share a page's heads
+  TurnShape sh;
+  int tiles;
+};
+
+// code of x in a page whose values are x / inv
+__device__ __forceinline__ int code_of(float x, float inv) {
+  const float r = fminf(fmaxf(rintf(x * inv), -127.f), 127.f);  // (x * inv may be 127 and a little)
+  return (int)r;
+}
+
+template <typename T, int D, int PAGE>
+struct PageRows {
+  typedef NormTurn<T, D> Tu;
+  static constexpr int EPC = Tu::EPC, ITEMS = Tu::ITEMS, SIDE = 256 / ITEMS;  // rows side by side
+  static constexpr int PASSES = PAGE > SIDE ? PAGE / SIDE : 1;
+  static constexpr size_t ROW = D * sizeof(T);
+
+  // One page of sequence b, heads first .. in steps of `step`.  alone: the workgroup writes the tail that it has read from.
+  static __device__ __forceinline__ void run(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
+                                             const PagesPlan& plan, const int4 s, int b, int u, bool keys, int first, int step,
+                                             uint32_t (*top)[4]) {
+    const int tid = threadIdx.x, item = tid % ITEMS, row0 = tid / ITEMS;
+    const int whole = s.x / PAGE, start = (whole + u) * PAGE, end = s.y;
+    const bool complete = start + PAGE <= end, turns = keys && a.rows.turns;
+    const char* tail = static_cast<const char*>(keys ? from.k_tail : from.v_tail);
+    char* to_tail = static_cast<char*>(keys ? to.k_tail : to.v_tail);
+    const HeadRows& rows = keys ? a.k_new : a.v_new;
+    Tu t[PASSES];
+    uint4 x[PASSES], y[PASSES];
+    auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int r = row0 + i * SIDE, at = start + r;
+        if (r < PAGE && at < end) {
+          const char* p = at < s.x ? tail + (((size_t)b * from.Hkv + h) * PAGE + r) * ROW : row_of(rows, b, h, at - s.x);
+          x[i] = load16(p + t[i].one * 16);
+          y[i] = load16(p + t[i].two * 16);
+        } else {
+          x[i] = y[i] = make_uint4(0, 0, 0, 0);
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) t[i].place(rot, turns, item);
+    load(first);
+    typename Tu::Weight w = t[0].weight(keys ? a.rows.k_weight : nullptr);
+    if (turns) {
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int at = start + row0 + i * SIDE, n = at - s.x;
+        if (n >= 0 && at < end)
+          t[i].angles(rot, item, [&](int axis) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : at; });
+      }
+    }
+    const int page = complete ? plan.taken[s.z + u] : 0;
+    if (complete && keys && first == 0 && tid == 0) to.table[(size_t)b * to.max_pages + whole + u] = page;
+    int turn = 0;
+    for (int h = first; h < from.Hkv; h += step, turn ^= 1) {
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int at = start + row0 + i * SIDE;
+        if (at >= s.x && at < end) t[i].apply(rot, w, a.rows.eps, x[i], y[i]);
+      }
+      if (!complete) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+          const int r = row0 + i * SIDE, at = start + r;
+          if (r < PAGE && at < end && (a.apart || at >= s.x)) {
+            char* p = to_tail + (((size_t)b * from.Hkv + h) * PAGE + r) * ROW;
+            store16(p + t[i].one * 16, x[i]);
+            store16(p + t[i].two * 16, y[i]);
+          }
+        }
+        if (h + step < from.Hkv) load(h + step);
+        continue;
+      }
+      // magnitudes order like integers, what is no number above infinity
+      uint32_t most = 0;
+      float f[2 * EPC];
+      auto values = [&](int i) {
+        float lo[EPC], hi[EPC];
+        unpack<T>(x[i], lo);
+        unpack<T>(y[i], hi);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          f[e] = lo[e];
+          f[EPC + e] = hi[e];
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        values(i);
+#pragma unroll
+        for (int e = 0; e < 2 * EPC; ++e) most = max(most, __float_as_uint(f[e]) & 0x7fffffffu);
+      }
+      most = wave_max_u(most);
+      if ((tid & 63) == 0) top[turn][tid >> 6] = most;
+      __syncthreads();
+      most = max(max(top[turn][0], top[turn][1]), max(top[turn][2], top[turn][3]));
+      // (below 2^-100, where 127 / max may be infinite, the page counts as zeros)
+      const bool number = most < 0x7f800000u, some = most >= 0x0d800000u;
+      const float inv = number && some ? 127.f / __uint_as_float(most) : 0.f;
+      const float scale = !number ? __uint_as_float(0x7fc00000u) : some ? __uint_as_float(most) / 127.f : 0.f;
+      const size_t unit = (size_t)page * from.Hkv + h;
+      if (tid == 0) (keys ? to.k_scales : to.v_scales)[unit] = scale;
+      int8_t* codes = (keys ? to.k_codes : to.v_codes) + unit * PAGE * D;
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int r = row0 + i * SIDE;
+        values(i);
+        uint32_t word[EPC / 2];  // both chunks' codes, four a word
+#pragma unroll
+        for (int j = 0; j < EPC / 2; ++j) {
+          uint32_t o = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o |= (uint32_t)((inv == 0.f ? 0 : code_of(f[j * 4 + e], inv)) & 0xff) << (8 * e);
+          word[j] = o;
+        }
+        if (r < PAGE) {
+          int8_t* p = codes + (size_t)r * D;
+          if constexpr (EPC == 8) {
+            *reinterpret_cast<uint2*>(p + t[i].one * 8) = make_uint2(word[0], word[1]);
+            *reinterpret_cast<uint2*>(p + t[i].two * 8) = make_uint2(word[2], word[3]);
+          } else {
+            *reinterpret_cast<uint32_t*>(p + t[i].one * 4) = word[0];
+            *reinterpret_cast<uint32_t*>(p + t[i].two * 4) = word[1];
+          }
+        }
+      }
+      if (h + step < from.Hkv) load(h + step);
+    }
+  }
+};
+
+template <typename T, int D, int PAGE>
+__global__ __launch_bounds__(256) void pages_append_kernel(const wave_pages from, const wave_pages to, const PagesAppendArgs a,
+                                                           const RotaryArgs rot, const PagesPlan plan, const AppendGrid grid) {
+  typedef PageRows<T, D, PAGE> Rows;
+  __shared__ uint32_t top[2][4];
+  unsigned block = workgroup_number();
+  if (block < grid.page_blocks) {
+    const int group = block % grid.head_groups, keys = (block / grid.head_groups) & 1;
+    const unsigned bu = block / grid.head_groups / 2;
+    const int u = bu % grid.units, b = bu / grid.units;
+    const int4 s = plan.sequence[b];
+    const int whole = s.x / PAGE, rest = s.y / PAGE - whole;  // the unit whose rows are the tail
+    // In place the rows that page 0 takes from the tail are where the new tail goes: the same workgroup does both.
+    const bool both = !a.apart && rest > 0 && s.x % PAGE != 0 && s.y % PAGE != 0;
+    if (u > rest || (u == rest && (both || s.y % PAGE == 0))) return;
+    Rows::run(from, to, a, rot, plan, s, b, u, keys, group, grid.head_groups, top);
+    if (u == 0 && both) {
+      __syncthreads();  // everything that was in the tail has been read, and the maxima too
+      Rows::run(from, to, a, rot, plan, s, b, rest, keys, group, grid.head_groups, top);
+    }
+    return;
+  }
+  block -= grid.page_blocks;
+  if (block < grid.q_blocks) {
+    const int group = block % grid.sh.head_groups, bt = block / grid.sh.head_groups;
+    const int b = bt / grid.tiles, tile = bt % grid.tiles;
+    const int4 s = plan.sequence[b];
+    norm_heads<T, D>(a.rows, rot, grid.sh, b, tile, group, s.w, [&](int axis, int n) {
+      return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : s.x + n;
+    });
+    return;
+  }
+  block -= grid.q_blocks;
+  if (!a.apart) return;
+  // one workgroup a sequence for the tables, the others for references
+  if (block < (unsigned)from.B) {
+    const int whole = plan.sequence[block].x / PAGE;
+    const size_t at = (size_t)block * from.max_pages;
+    for (int i = threadIdx.x; i < whole; i += 256) to.table[at + i] = from.table[at + i];
+    return;
+  }
+  const int last = plan.last[0];
+  const long long i = (long long)(block - from.B) * 256 + threadIdx.x;
+  if (i < from.n_pages) {
+    const int r = from.references[i];
+    to.references[i] = r <= 0 && i <= last ? 1 : r;
+  }
+}
+
+template <typename T, int D, int PAGE>
+wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
+                             const PagesPlan& plan, hipStream_t st) {
+  WAVE_LAUNCH("pages_plan", pages_plan_kernel, 1, PLAN_THREADS, 0, st, from, to, a.counts, a.n, plan, a.apart);
+  AppendGrid g{};
+  g.units = a.n == 1 ? 1 : (int)(((long long)PAGE - 2 + a.n) / PAGE) + 1;
+  // A page's heads are split while the launch leaves most CUs without work; together they share the sines.
+  g.head_groups = 1;
+  while ((long long)from.B * g.units * 2 * g.head_groups < 1024 && g.head_groups < from.Hkv) g.head_groups *= 2;
+  if (g.head_groups > from.Hkv) g.head_groups = from.Hkv;
+  long long blocks = (long long)from.B * g.units * 2 * g.head_groups;
+  g.page_blocks = (unsigned)blocks;
+  if (a.rows.Hq > 0) {
+    g.sh = turn_shape<Turn<T, D>::ITEMS>(a.n, from.B, a.rows.Hq);
+    g.tiles = (a.n + g.sh.tokens - 1) / g.sh.tokens;
+    g.q_blocks = (unsigned)((long long)from.B * g.tiles * g.sh.head_groups);
+    blocks += g.q_blocks;
+  }
+  if (a.apart) blocks += from.B + ((long long)from.n_pages + 255) / 256;
+  WAVE_LAUNCH("pages_append", (pages_append_kernel<T, D, PAGE>), grid_rows(blocks), 256, 0, st, from, to, a, rot, plan, g);
+  return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
+}
+template <typename T, int D>
+wave_status pages_append_td(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
+                            const PagesPlan& plan, hipStream_t st) {
+  return from.page == 32   ? pages_append_tdp<T, D, 32>(from, to, a, rot, plan, st)
+         : from.page == 64 ? pages_append_tdp<T, D, 64>(from, to, a, rot, plan, st)
+                           : pages_append_tdp<T, D, 128>(from, to, a, rot, plan, st);
+}
+
+// ----------------------------------------------------------------------------
+// Reading back.  A thread has 16 codes of a row; READ_ROWS rows of a workgroup's tile are in flight in each thread.
+// ----------------------------------------------------------------------------
+struct ReadArgs {
+  const int32_t* first;
+  char *k_out, *v_out;
+  int n, tiles;
+};
+constexpr int READ_ROWS = 4;
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void pages_read_kernel(const wave_pages p, const ReadArgs a, int sides) {
+  constexpr int LANES = D / 16, SIDE = 256 / LANES, TILE = SIDE * READ_ROWS;
+  constexpr size_t ROW = D * sizeof(T);
+  unsigned block = workgroup_number();
+  const bool keys = sides == 2 ? (block & 1) == 0 : a.k_out != nullptr;
+  block /= sides;
+  const int tile = block % a.tiles;
+  const unsigned unit = block / a.tiles;
+  if (unit >= (unsigned)(p.B * p.Hkv)) return;
+  const int b = unit / p.Hkv, h = unit % p.Hkv, shift = page_shift(p.page);
+  const int length = pages_length(p, b), whole = length >> shift << shift;
+  const long long first = a.first ? a.first[b] : 0;
+  const int lane = threadIdx.x % LANES;
+  const int8_t* codes = keys ? p.k_codes : p.v_codes;
+  const float* scales = keys ? p.k_scales : p.v_scales;
+  const char* tail = static_cast<const char*>(keys ? p.k_tail : p.v_tail);
+  char* out = keys ? a.k_out : a.v_out;
+  const int t0 = tile * TILE + threadIdx.x / LANES;
+  if (first + (long long)tile * TILE >= length) return;
+  int page[READ_ROWS];
+  float scale[READ_ROWS];
+  uint4 c[READ_ROWS];
+#pragma unroll
+  for (int i = 0; i < READ_ROWS; ++i) {
+    const long long at = first + t0 + i * SIDE;
+    page[i] = at >= 0 && at < whole ? page_entry(p, b, (int)at >> shift) : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < READ_ROWS; ++i) {
+    const long long at = first + t0 + i * SIDE;
+    const size_t row = ((size_t)page[i] * p.Hkv + h);
+    scale[i] = scales[row];
+    c[i] = load16(codes + ((row << shift) + ((int)at & (p.page - 1))) * D + lane * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < READ_ROWS; ++i) {
+    const int t = t0 + i * SIDE;
+    const long long at = first + t;
+    if (t >= a.n || at < 0 || at >= length) continue;
+    char* to = out + ((size_t)unit * a.n + t) * ROW + lane * 16 * sizeof(T);
+    constexpr int CHUNKS = (int)sizeof(T), EPC = Elem<T>::EPC;  // of 16 bytes
+    if (at >= whole) {
+      const char* from = tail + ((size_t)unit * p.page + (at - whole)) * ROW + lane * 16 * sizeof(T);
+#pragma unroll
+      for (int j = 0; j < CHUNKS; ++j) store16(to + j * 16, load16(from + j * 16));
+      continue;
+    }
+    const uint32_t word[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+      float f[EPC];
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) f[e] = (float)(int8_t)(word[(j * EPC + e) / 4] >> (8 * ((j * EPC + e) & 3))) * scale[i];
+      store16(to + j * 16, pack<T>(f));
+    }
+  }
+}
+
+template <typename T, int D>
+wave_status pages_read_td(const wave_pages& p, ReadArgs a, hipStream_t st) {
+  constexpr int TILE = 256 / (D / 16) * READ_ROWS;
+  a.tiles = (a.n + TILE - 1) / TILE;
+  const int sides = (a.k_out ? 1 : 0) + (a.v_out ? 1 : 0);
+  WAVE_LAUNCH("pages_read", (pages_read_kernel<T, D>), grid_rows((long long)p.B * p.Hkv * a.tiles * sides), 256, 0, st, p, a, sides);
+  return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
+}
+
+// ----------------------------------------------------------------------------
+// Reordering.  References change by atomic additions of whole numbers, whose order does not show.
+// ----------------------------------------------------------------------------
+__device__ __forceinline__ int parent_of(const wave_pages& from, const int32_t* parent, int b) {
+  const int p = parent[b];
+  return p >= 0 && p < from.B ? p : -1;
+}
+
+// to's own arrays: tails, tables and lengths from the parents', references as they were
+__global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, int row_bytes,
+                                                         unsigned tail_blocks) {
+  unsigned block = workgroup_number();
+  if (block < tail_blocks) {  // a head's keys or values of a sequence's tail
+    const bool keys = (block & 1) == 0;
+    const unsigned unit = block / 2;
+    const int b = unit / from.Hkv, h = unit % from.Hkv;
+    if (b >= to.B) return;
+    const int s = parent_of(from, parent, b);
+    if (s < 0) return;
+    const int chunks = (pages_length(from, s) & (from.page - 1)) * (row_bytes / 16);
+    const char* x = static_cast<const char*>(keys ? from.k_tail : from.v_tail) + ((size_t)s * from.Hkv + h) * from.page * row_bytes;
+    char* y = static_cast<char*>(keys ? to.k_tail : to.v_tail) + (size_t)unit * to.page * row_bytes;
+    for (int i = threadIdx.x; i < chunks; i += 256) store16(y + (size_t)i * 16, load16(x + (size_t)i * 16));
+    return;
+  }
+  block -= tail_blocks;
+  if (block < (unsigned)to.B) {
+    const int b = block, s = parent_of(from, parent, b);
+    const int length = s < 0 ? 0 : pages_length(from, s), whole = length >> page_shift(from.page);
+    for (int i = threadIdx.x; i < whole; i += 256) to.table[(size_t)b * to.max_pages + i] = from.table[(size_t)s * from.max_pages + i];
+    if (threadIdx.x == 0) to.lengths[b] = length;
+    return;
+  }
+  block -= to.B;
+  const long long i = (long long)block * 256 + threadIdx.x;
+  if (i < from.n_pages) to.references[i] = from.references[i];
+}
+
+// One workgroup for each sequence of `to` (what it holds) and of `from` (what it held).  One that stays where it is changes
+// nothing.  In place: those that leave.
+__global__ __launch_bounds__(256) void pages_count_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, bool apart) {
+  int b = workgroup_number();
+  const int shift = page_shift(from.page);
+  if (!apart) {
+    if (b >= from.B || parent[b] == b) return;
+    const int whole = pages_length(from, b) >> shift;
+    __syncthreads();
+    if (threadIdx.x == 0) to.lengths[b] = 0;
+    for (int i = threadIdx.x; i < whole; i += 256) atomicSub(&to.references[page_entry(from, b, i)], 1);
+    return;
+  }
+  if (b < to.B) {
+    const int s = parent_of(from, parent, b);
+    if (s < 0 || s == b) return;
+    const int whole = pages_length(from, s) >> shift;
+    for (int i = threadIdx.x; i < whole; i += 256) atomicAdd(&to.references[page_entry(from, s, i)], 1);
+    return;
+  }
+  b -= to.B;
+  if (b >= from.B || (b < to.B && parent[b] == b)) return;
+  const int whole = pages_length(from, b) >> shift;
+  for (int i = threadIdx.x; i < whole; i += 256) atomicSub(&to.references[page_entry(from, b, i)], 1);
+}
+
+}  // namespace
+
+wave_status launch_norm_rotary(const NormArgs& a, const RotaryArgs& rot, int dtype, int d, hipStream_t st) {
+  if (dtype == WAVE_BF16) return d == 128 ? norm_rotary_td<bf16_t, 128>(a, rot, st) : norm_rotary_td<bf16_t, 64>(a, rot, st);
+  return d == 128 ? norm_rotary_td<float, 128>(a, rot, st) : norm_rotary_td<float, 64>(a, rot, st);
+}
+
+size_t pages_append_workspace(const wave_pages& p) {
+  return align_up(256 + align_up(sizeof(int4) * (size_t)p.B) + sizeof(int32_t) * (size_t)p.n_pages);
+}
+
+wave_status launch_pages_append(const wave_pages& from, const wave_pages& to, PagesAppendArgs a, const RotaryArgs& rot,
+                                void* ws, hipStream_t st) {
+  const PagesPlan plan = pages_plan(from, ws);
+  if (from.dtype == WAVE_BF16)
+    return from.d == 128 ? pages_append_td<bf16_t, 128>(from, to, a, rot, plan, st) : pages_append_td<bf16_t, 64>(from, to, a, rot, plan, st);
+  return from.d == 128 ? pages_append_td<float, 128>(from, to, a, rot, plan, st) : pages_append_td<float, 64>(from, to, a, rot, plan, st);
+}
+
+wave_status launch_pages_read(const wave_pages& p, const int32_t* first, int n, void* k_out, void* v_out, hipStream_t st) {
+  ReadArgs a{};
+  a.first = first;
+  a.n = n;
+  a.k_out = static_cast<char*>(k_out);
+  a.v_out = static_cast<char*>(v_out);
+  if (p.dtype == WAVE_BF16) return p.d == 128 ? pages_read_td<bf16_t, 128>(p, a, st) : pages_read_td<bf16_t, 64>(p, a, st);
+  return p.d == 128 ? pages_read_td<float, 128>(p, a, st) : pages_read_td<float, 64>(p, a, st);
+}
+
+wave_status launch_pages_reorder(const wave_pages& from, const wave_pages& to, const int32_t* parent, hipStream_t st) {
+  const bool apart = to.lengths != from.lengths;
+  if (apart) {
+    const long long tails = (long long)to.B * to.Hkv * 2;
+    const int row = from.d * (from.dtype == WAVE_BF16 ? 2 : 4);
+    WAVE_LAUNCH("pages_copy", pages_copy_kernel, grid_rows(tails + to.B + ((long long)from.n_pages + 255) / 256), 256, 0, st, from, to,
+                parent, row, (unsigned)tails);
+  }
+  WAVE_LAUNCH("pages_count", pages_count_kernel, grid_rows(apart ? (long long)to.B + from.B : from.B), 256, 0, st, from, to, parent, apart);
+  return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
+}
+
+}  // namespace wave

@@ -1,0 +1,851 @@
+"""Norms with rotary positions and the paged 8-bit cache on the GPU against the plain statement, through the C ABI.
+
+Tolerances count roundings (u = 2^-24 for fp32, half a step):
+  norm     the squares' sum, at most 16 in a row in each lane and then four times two partial sums, all positive: 1 + 1 + 16 + 4 u, of which
+           the root halves the relative error: 11 u; the mean, eps and the root's own last place 3 u; two products 2 u: 16 u of a value,
+           so of a pair's length; then the turn's 8 u of it, and half a step of the type
+  pages    rows as they are in the type go to 8 bits by a formula in fp32 whose every operation rounds to nearest: equal
+  read     code * scale rounded to fp32, then to the type: equal
+  scores   a sum of d products (3 d for an fp32 query, three bf16 numbers) in fp32 and three roundings of the scale: (3 d + 6) u of the
+           sum of the products' magnitudes (delta)
+  output   of a row's weight: 2 delta + 8 u, with the values' scale one more; n u for the sums of n terms, 16 u for the joining; and,
+           as the errors of different rows have no sign in common, 1e-5 of the norm
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as co
+from oracle import pages_oracle as po
+from paper_2505_02922_amd import binding as wb
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+OWN = wb.PAGE_STATE
+
+
+def _gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def _same_bits(a, b):
+    v = {1: torch.int8, 2: torch.int16, 4: torch.int32}[a.element_size()]
+    return a.shape == b.shape and torch.equal(a.contiguous().view(v), b.contiguous().view(v))
+
+
+# --------------------------------------------------------------------------- norms with rotary positions
+def _expected(x, weight, eps, coords, plan, pairing, base):
+    """x [B, H, N, d] double -> the rows normed and turned, and the length of every channel's pair, in numpy."""
+    y = x if weight is None else x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * weight
+    size = np.abs(y)
+    if plan is None:
+        return y, size
+    rot, sections, order = plan
+    axis, freq = co.pair_plan(rot, base, sections, order)
+    z = y.copy()
+    for i, (a, f) in enumerate(zip(axis, freq)):
+        p, q = (i, i + rot // 2) if pairing == co.HALVES else (2 * i, 2 * i + 1)
+        angle = coords[a].astype(np.float64)[:, None] * f
+        c, s = np.cos(angle), np.sin(angle)
+        z[..., p], z[..., q] = y[..., p] * c - y[..., q] * s, y[..., p] * s + y[..., q] * c
+        size[..., p] = size[..., q] = np.hypot(y[..., p], y[..., q])
+    return z, size
+
+
+def _near(got, x, weight, eps, coords, plan, pairing, base, dtype, tag):
+    want, size = _expected(x.double().numpy(), None if weight is None else weight.double().numpy(), eps,
+                           None if coords is None else coords.numpy(), plan, pairing, base)
+    far = 0.0 if coords is None else float(np.abs(coords.numpy().astype(np.float64)).max()) * 2.0 ** -51
+    bar = (24 * U + far) * size * (1 + HALF_STEP[dtype]) + HALF_STEP[dtype] * np.abs(want) + 1e-38
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert np.all(err <= bar), (tag, float((err - bar).max()))
+
+
+PLANS = [(128, 128, [64], 0, 0), (128, 128, [16, 24, 24], 1, 0), (128, 64, [16, 16], 2, 1), (64, 64, [32], 0, 1), (64, 48, [8, 9, 7], 0, 0),
+         (64, 16, [1, 2, 3, 2], 1, 1)]
+
+
+def test_vectorised_form_is_the_plain_one():
+    rng = np.random.default_rng(1)
+    x, w = rng.standard_normal((2, 3, 4, 64)), rng.standard_normal(64)
+    coords = rng.integers(0, 99, (2, 2, 4))
+    y, _ = _expected(x, w, 1e-3, coords, (48, [10, 14], co.TURNS), co.NEIGHBOURS, 1e4)
+    axis, freq = co.pair_plan(48, 1e4, [10, 14], co.TURNS)
+    for b in range(2):
+        for h in range(3):
+            for n in range(4):
+                assert np.allclose(y[b, h, n], po.norm_rotate(x[b, h, n], w, 1e-3, coords[:, b, n], axis, freq, co.NEIGHBOURS))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,rot,sections,order,pairing", PLANS)
+@pytest.mark.parametrize("B,Hq,Hkv,N", [(1, 1, 1, 1), (2, 3, 1, 31), (1, 6, 2, 33), (3, 40, 5, 2), (1, 2, 2, 300), (5, 7, 7, 1)])
+@pytest.mark.parametrize("fused", [False, True])
+def test_norm_rotary(dtype, d, rot, sections, order, pairing, B, Hq, Hkv, N, fused):
+    g, base, eps = _gen(N + Hq), 500000.0, 1e-5
+    if fused:     # views of a projection's output, beside its values
+        x = (3 * torch.randn(B, N, Hq + 2 * Hkv, d, generator=g)).to(TYPES[dtype]).transpose(1, 2)
+        q, k, _ = x.split([Hq, Hkv, Hkv], 1)
+        qc, kc, _ = x.cuda().split([Hq, Hkv, Hkv], 1)
+        assert qc.stride() == q.stride()
+    else:
+        q, k = ((3 * torch.randn(B, h, N, d, generator=g)).to(TYPES[dtype]) for h in (Hq, Hkv))
+        qc, kc = q.cuda(), k.cuda()
+    qw, kw = ((1 + 0.3 * torch.randn(d, generator=g)).to(TYPES[dtype]) for _ in range(2))
+    coords = torch.randint(0, 1 << 20, (len(sections), B, N), generator=g, dtype=torch.int32)
+    coords[0, 0, 0] = -5
+    r, plan = wb.wave_rotary_plan(rot, base, sections, order, pairing), (rot, sections, order)
+    got_q, got_k = wb.wave_norm_rotary_apply(qc, kc, qw.cuda(), kw.cuda(), eps, coords.cuda(), r)
+    _near(got_q, q, qw, eps, coords, plan, pairing, base, dtype, "q")
+    _near(got_k, k, kw, eps, coords, plan, pairing, base, dtype, "k")
+    # one of the two alone, and outputs given
+    out = torch.full_like(got_q, 9.0)
+    alone, none = wb.wave_norm_rotary_apply(qc, None, qw.cuda(), None, eps, coords.cuda(), r, q_out=out)
+    assert alone is out and none is None and _same_bits(out, got_q)
+    assert _same_bits(wb.wave_norm_rotary_apply(None, kc, None, kw.cuda(), eps, coords.cuda(), r)[1], got_k)
+    # turned only; only normed; only the keys normed
+    only_q, only_k = wb.wave_norm_rotary_apply(qc, kc, coords=coords.cuda(), rotary=r)
+    _near(only_q, q, None, eps, coords, plan, pairing, base, dtype, "turned q")
+    _near(only_k, k, None, eps, coords, plan, pairing, base, dtype, "turned k")
+    normed_q, normed_k = wb.wave_norm_rotary_apply(qc, kc, qw.cuda(), kw.cuda(), eps)
+    _near(normed_q, q, qw, eps, None, None, 0, base, dtype, "normed q")
+    _near(normed_k, k, kw, eps, None, None, 0, base, dtype, "normed k")
+    mixed_q, mixed_k = wb.wave_norm_rotary_apply(qc, kc, None, kw.cuda(), eps, coords.cuda(), r)
+    assert _same_bits(mixed_q, only_q) and _same_bits(mixed_k, got_k)
+    if not fused:   # in place
+        wb.wave_norm_rotary_apply(qc, kc, qw.cuda(), kw.cuda(), eps, coords.cuda(), r, q_out=qc, k_out=kc)
+        assert _same_bits(qc, got_q) and _same_bits(kc, got_k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_rotary_layouts(dtype):
+    """Rows that repeat (stride 0), that begin off 16 bytes or have odd strides (copied by the binding), no rows at all."""
+    g = _gen(3)
+    r = wb.wave_rotary_plan(64, 1e4)
+    w = torch.ones(64, dtype=TYPES[dtype], device="cuda")
+    coords = torch.arange(5, dtype=torch.int32, device="cuda").expand(1, 3, 5).contiguous()
+    one = torch.randn(1, 2, 1, 64, generator=g).to(TYPES[dtype]).cuda()
+    want = wb.wave_norm_rotary_apply(one.expand(3, 2, 5, 64).contiguous(), None, w, coords=coords, rotary=r)[0]
+    assert _same_bits(wb.wave_norm_rotary_apply(one.expand(3, 2, 5, 64), None, w, coords=coords, rotary=r)[0], want)
+    x = torch.randn(3, 2, 5, 200, generator=g).to(TYPES[dtype]).cuda()
+    for part in (x[..., 1:65], x[..., 3:131:2], x[..., 8:72], x.transpose(1, 2)[..., 1:65].transpose(1, 2), x[..., 1:65].flip(1)):
+        want = wb.wave_norm_rotary_apply(part.contiguous(), None, w, coords=coords, rotary=r)[0]
+        assert _same_bits(wb.wave_norm_rotary_apply(part, None, w, coords=coords, rotary=r)[0], want)
+    odd = torch.ones(65, dtype=TYPES[dtype], device="cuda")[1:]
+    assert _same_bits(wb.wave_norm_rotary_apply(part, None, odd, coords=coords, rotary=r)[0], want)
+    empty = torch.empty(0, 2, 5, 64, dtype=TYPES[dtype], device="cuda")
+    assert wb.wave_norm_rotary_apply(empty, None, w)[0].shape == empty.shape
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_extreme_rows(dtype):
+    """Rows of zeros, of tiny and of large values, with an infinity, with no number; far positions."""
+    x = torch.zeros(1, 7, 2, 128)
+    x[0, 1] = 1e-15
+    x[0, 2] = 1e17            # squares add up to less than 2^128
+    x[0, 3, :, 5] = math.inf
+    x[0, 4, :, 7] = math.nan
+    x[0, 5] = torch.randn(2, 128, generator=_gen(4))
+    x[0, 6, :, 0] = -1e18
+    x = x.to(TYPES[dtype])
+    w = torch.ones(128, dtype=TYPES[dtype])
+    coords = torch.tensor([[[2 ** 31 - 1, -2 ** 31]]], dtype=torch.int32)
+    r = wb.wave_rotary_plan(32, 1e4)
+    for eps in (1e-6, 0.0):
+        got = wb.wave_norm_rotary_apply(x.cuda(), None, w.cuda(), None, eps, coords.cuda(), r)[0].cpu()
+        fine = [1, 2, 5, 6] if eps == 0 else [0, 1, 2, 5, 6]
+        _near(got[:, fine], x[:, fine], w, eps, coords, (32, [16], 0), 0, 1e4, dtype, "extreme")
+        assert bool(torch.isnan(got[0, 4]).all())
+        assert bool(torch.isnan(got[0, 3, :, 5]).all()) and not bool(got[0, 3, :, 32:].any())    # x / infinity, the infinity itself no number
+        if eps == 0:
+            assert bool(torch.isnan(got[0, 0]).all())                                              # zero by zero
+
+
+@pytest.mark.parametrize("N", [1, 2])
+def test_norm_rotary_of_more_workgroups_than_a_launch_row(N):
+    B = (1 << 24) + 3
+    x = torch.randn(B, 1, N, 64, device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(64, device="cuda", dtype=torch.bfloat16)
+    coords = torch.randint(0, 1 << 20, (1, B, N), device="cuda", dtype=torch.int32)
+    r = wb.wave_rotary_plan(48, 1e4, None, 0, 1)
+    want = wb.wave_norm_rotary_apply(x.view(1, 1, B * N, 64), None, w, coords=coords.view(1, 1, B * N), rotary=r)[0]
+    got = wb.wave_norm_rotary_apply(x, None, w, coords=coords, rotary=r)[0]
+    assert _same_bits(got.view(-1), want.view(-1))
+
+
+# --------------------------------------------------------------------------- append, read
+def _state(pages):
+    return {n: t.clone() for n, t in pages.t.items()}
+
+
+def _check_state(pages, plain, tag=""):
+    """Lists, tails and pages of a state against the plain one's."""
+    B, T = pages.B, pages.page
+    assert pages.lengths.tolist() == [plain.length(b) for b in range(B)], tag
+    assert pages.references.tolist() == plain.references, tag
+    t = {n: x.cpu() for n, x in pages.t.items()}
+    for b in range(B):
+        held = plain.pages[b]
+        assert t["table"][b, :len(held)].tolist() == held, (tag, b)
+        for i, name in ((0, "k_tail"), (1, "v_tail")):
+            for r, row in enumerate(plain.tails[b]):
+                assert np.array_equal(t[name][b, :, r].float().numpy(), row[i], equal_nan=True), (tag, b, name, r)
+        for page in held:
+            kc, vc, ks, vs = plain.pool[page][0], plain.pool[page][1], plain.pool[page][2], plain.pool[page][3]
+            for name, want in (("k_codes", kc), ("v_codes", vc), ("k_scales", ks), ("v_scales", vs)):
+                assert np.array_equal(t[name][page].numpy(), want, equal_nan=name.endswith("scales")), (tag, b, page, name)
+
+
+def _check_read(pages, plain, n, first, tag=""):
+    shape = (pages.B, pages.Hkv, n, pages.d)
+    outs = [torch.full(shape, 5.0, dtype=pages.dtype, device="cuda") for _ in range(2)]
+    at = None if first is None else torch.tensor(first, dtype=torch.int32, device="cuda")
+    got = wb.wave_pages_read(pages, n, first=at, k_out=outs[0], v_out=outs[1])
+    assert got[0] is outs[0] and got[1] is outs[1]
+    got = [x.cpu() for x in got]
+    for b in range(pages.B):
+        length, f = plain.length(b), 0 if first is None else first[b]
+        for h in range(pages.Hkv):
+            rows = plain.rows(b, h)
+            for x, want in zip(got, rows):
+                for t in range(n):
+                    if 0 <= f + t < length:
+                        assert _same_bits(x[b, h, t], torch.from_numpy(want[f + t]).float().to(pages.dtype)), (tag, b, h, t)
+                    else:
+                        assert bool((x[b, h, t] == 5.0).all()), (tag, b, h, t)
+
+
+def _as_rows(x):
+    return x.float().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,page", [(64, 32), (64, 64), (64, 128), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("apart", [False, True])
+def test_append_rows_as_they_are(dtype, d, page, apart):
+    """Appends of one row to more than two pages, ragged, in place and into a state beside: lists, tails, codes and scales as
+    in the plain statement, everything else as it was."""
+    B, Hkv, n_pages, max_pages, g = 4, 3, 23, 6, _gen(d + page)
+    plain = po.Paged(B, page, n_pages, max_pages)
+    pages = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, n_pages, max_pages)
+    for n in ("k_tail", "v_tail", "k_scales", "v_scales"):
+        pages.t[n].fill_(math.nan)
+    other = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, n_pages, max_pages, pool=pages)
+    other.references.fill_(7)
+    steps = [(1, None), (page - 2, None), (1, [1, 0, 1, 5]), (1, None), (2 * page + 3, [page, 2 * page + 3, 0, page + 1]), (page, None), (1, None),
+             (3 * page, [-1, 4, page - 3, 3 * page])]
+    for i, (n, counts) in enumerate(steps):
+        k, v = ((torch.randn(B, Hkv, n, d, generator=g) * (1 + 50 * (torch.rand(B, Hkv, n, 1, generator=g) < 0.02))).to(TYPES[dtype]) for _ in range(2))
+        c = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+        before = _state(pages)
+        plain.append(_as_rows(k), _as_rows(v), counts)
+        if apart:
+            wb.wave_pages_append(pages, k.cuda(), v.cuda(), counts=c, to=other)
+            for name in OWN:
+                assert _same_bits(pages.t[name], before[name]), (i, name)
+            pages, other = other, pages
+        else:
+            wb.wave_pages_append(pages, k.cuda(), v.cuda(), counts=c)
+            for b in range(B):
+                held, rest = len(plain.pages[b]), len(plain.tails[b])
+                assert _same_bits(pages.table[b, held:], before["table"][b, held:]), i
+        _check_state(pages, plain, i)
+        free = [p for p in range(n_pages) if plain.references[p] <= 0]
+        assert _same_bits(pages.k_codes[free], before["k_codes"][free]) and _same_bits(pages.v_scales[free], before["v_scales"][free]), i
+    most = max(plain.length(b) for b in range(B))
+    _check_read(pages, plain, most + 3, None)
+    _check_read(pages, plain, page + 1, [-3, 5, most - 1, 2 ** 31 - 1])
+    _check_read(pages, plain, 1, [0, page - 1, page, page * 2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tail_behind_its_rows_is_left(dtype):
+    B, Hkv, d, page = 2, 1, 64, 32
+    pages = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, 4, 2)
+    to = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, 4, 2, pool=pages)
+    for s in (pages, to):
+        s.k_tail.fill_(3.0), s.v_tail.fill_(4.0), s.table.fill_(77)
+    x = torch.randn(B, Hkv, 40, d, generator=_gen(2)).to(TYPES[dtype]).cuda()
+    wb.wave_pages_append(pages, x, x, to=to, counts=torch.tensor([40, 3], dtype=torch.int32, device="cuda"))
+    for name, fill in (("k_tail", 3.0), ("v_tail", 4.0)):
+        t = to.t[name]
+        assert _same_bits(t[0, :, :8], x[0, :, 32:]) and _same_bits(t[1, :, :3], x[1, :, :3])
+        assert bool((t[0, :, 8:] == fill).all()) and bool((t[1, :, 3:] == fill).all())
+    assert to.table.tolist() == [[0, 77], [77, 77]] and to.lengths.tolist() == [40, 3] and to.references.tolist() == [1, 0, 0, 0]
+    assert pages.lengths.tolist() == [0, 0] and pages.references.tolist() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,rot,sections,order,pairing", [PLANS[1], PLANS[2], PLANS[4]])
+@pytest.mark.parametrize("B,Hq,Hkv,n,page,normed,fused", [(1, 4, 1, 1, 32, True, False), (5, 14, 2, 1, 64, False, True), (2, 6, 6, 37, 32, True, True),
+                                                           (3, 8, 2, 150, 64, True, False), (2, 0, 2, 200, 128, True, True), (33, 8, 8, 2, 32, False, False)])
+def test_append_normed_and_turned(dtype, d, rot, sections, order, pairing, B, Hq, Hkv, n, page, normed, fused):
+    """Queries, and keys before they are held, are those of wave_norm_rotary_apply."""
+    g = _gen(n)
+    pages = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, 16 * B, 16)
+    plain = po.Paged(B, page, 16 * B, 16)
+    r = wb.wave_rotary_plan(rot, 1e6, sections, order, pairing)
+    qw, kw = ((1 + 0.2 * torch.randn(d, generator=g)).to(TYPES[dtype]).cuda() if normed else None for _ in range(2))
+    for step in range(3 if n > 1 else 40):
+        x = torch.randn(B, n, Hq + 2 * Hkv, d, generator=g).to(TYPES[dtype]).cuda().transpose(1, 2)
+        q, k, v = (t if fused else t.contiguous() for t in x.split([Hq, Hkv, Hkv], 1))
+        coords = torch.randint(0, 5000, (len(sections), B, n), generator=g, dtype=torch.int32).cuda()
+        counts = None if step != 1 else torch.randint(0, n + 1, (B,), generator=g, dtype=torch.int32).cuda()
+        if step == 2:     # text: the tokens' own numbers
+            coords = (pages.lengths[:, None] + torch.arange(n, device="cuda")).expand(len(sections), B, n).to(torch.int32).contiguous()
+        want_q, want_k = wb.wave_norm_rotary_apply(q if Hq else None, k, qw if Hq else None, kw, 1e-6, coords, r)
+        q_out = torch.full((B, Hq, n, d), 7.0, dtype=TYPES[dtype], device="cuda") if Hq else None
+        got = wb.wave_pages_append(pages, k, v, q=q if Hq else None, q_weight=qw if Hq else None, k_weight=kw, coords=None if step == 2 else coords,
+                                   rotary=r, counts=counts, q_out=q_out)
+        assert got is q_out
+        given = [n] * B if counts is None else counts.tolist()
+        for b in range(B if Hq else 0):
+            assert _same_bits(got[b, :, :given[b]], want_q[b, :, :given[b]]) and bool((got[b, :, given[b]:] == 7.0).all())
+        plain.append(_as_rows(want_k), _as_rows(v), given)
+        if step in (0, 1, 2, 31, 39):
+            _check_state(pages, plain, step)
+
+
+def test_append_normed_without_positions():
+    g = _gen(5)
+    q, k, v = (torch.randn(2, h, 40, 64, generator=g).bfloat16().cuda() for h in (4, 2, 2))
+    w = (1 + 0.2 * torch.randn(64, generator=g)).bfloat16().cuda()
+    pages, plain = wb.alloc_pages(torch.bfloat16, 2, 2, 64, 32, 8, 4), po.Paged(2, 32, 8, 4)
+    want_q, want_k = wb.wave_norm_rotary_apply(q, k, w, w)
+    assert _same_bits(wb.wave_pages_append(pages, k, v, q=q, q_weight=w, k_weight=w), want_q)
+    plain.append(_as_rows(want_k), _as_rows(v))
+    _check_state(pages, plain)
+    assert wb.wave_pages_append(pages, k, v, q=q, q_weight=w, q_out=q) is q and _same_bits(q, want_q)     # in place
+    plain.append(_as_rows(k), _as_rows(v))
+    _check_state(pages, plain)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pages_of_extreme_values(dtype):
+    """Zeros, values near the type's ends, infinities and no numbers: a page's head each."""
+    B, Hkv, d, page = 1, 8, 64, 32
+    g = _gen(6)
+    x = torch.randn(B, Hkv, page, d, generator=g)
+    x[0, 0] = 0.0
+    x[0, 1] *= 2.0 ** -103     # the largest below 2^-100
+    x[0, 2] = x[0, 2].clamp(-3, 3) * 1e38
+    x[0, 3, 5, 9] = math.inf
+    x[0, 4, 31, 63] = math.nan
+    x[0, 5, 0, 0] = -math.inf
+    x[0, 6] *= 2.0 ** -99
+    x[0, 7, 3, 3] = 1e30       # all others round to zero
+    x = x.to(TYPES[dtype])
+    pages, plain = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, 2, 2), po.Paged(B, page, 2, 2)
+    wb.wave_pages_append(pages, x.cuda(), -x.cuda())
+    plain.append(_as_rows(x), _as_rows(-x))
+    _check_state(pages, plain)
+    k, v = wb.wave_pages_read(pages, page)
+    assert bool(torch.isnan(k[0, 3:6]).all()) and bool(torch.isnan(v[0, 3:6]).all()) and not bool(k[0, :2].any())
+    assert bool(torch.isfinite(k[0, [0, 1, 2, 6, 7]]).all())
+
+
+def test_append_in_any_pieces_gives_the_same_rows():
+    B, Hkv, d, page, n = 3, 2, 128, 64, 333
+    g = _gen(7)
+    q, k, v = (torch.randn(B, h, n, d, generator=g).bfloat16().cuda() for h in (4, Hkv, Hkv))
+    w = torch.ones(d, device="cuda", dtype=torch.bfloat16)
+    r = wb.wave_rotary_plan(128, 1e4)
+    read, queries = [], []
+    for cuts in ((0, n), (0, 1, 64, 65, 200, n), tuple(range(0, n + 1, 3)), (0, 63, 64, 128, 129, n)):
+        pages = wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, 20, 6)
+        qs = [wb.wave_pages_append(pages, k[:, :, a:b], v[:, :, a:b], q=q[:, :, a:b], q_weight=w, k_weight=w, rotary=r) for a, b in zip(cuts, cuts[1:])]
+        read.append(wb.wave_pages_read(pages, n))
+        queries.append(torch.cat(qs, 2))
+        assert pages.lengths.tolist() == [n] * B and sorted(pages.table[:, :5].flatten().tolist()) == list(range(15))
+    for (a, b), c in zip(read, queries):
+        assert _same_bits(a, read[0][0]) and _same_bits(b, read[0][1]) and _same_bits(c, queries[0])
+
+
+@pytest.mark.parametrize("n_pages,B", [(1, 1), (63, 7), (1000, 300), (16384, 40), (16385, 9), (50000, 2100)])
+def test_free_pages_of_pools_of_every_size(n_pages, B):
+    """Few and many pages and sequences, most pages taken; those that are wanted are found or run out in order."""
+    g = _gen(n_pages)
+    page, n = 32, 70
+    references = (torch.rand(n_pages, generator=g) < 0.9).to(torch.int32) * 3
+    references[:5] = -1                                       # counts as free
+    pages = wb.alloc_pages(torch.float32, B, 1, 64, page, n_pages, 2)
+    pages.references.copy_(references)
+    x = torch.randn(B, 1, n, 64, generator=g)
+    counts = torch.randint(0, n + 1, (B,), generator=g, dtype=torch.int32)
+    wb.wave_pages_append(pages, x.cuda(), x.cuda(), counts=counts.cuda())
+    free = [p for p in range(n_pages) if references[p] <= 0]
+    refs, lengths, table = references.clone(), [], pages.table.tolist()
+    for b in range(B):
+        need = int(counts[b]) // page
+        mine, free = free[:need], free[need:]
+        refs[mine] = 1
+        lengths.append(int(counts[b]) if len(mine) == need else (len(mine) + 1) * page - 1)
+        assert table[b][:len(mine)] == mine, b
+    assert pages.lengths.tolist() == lengths and torch.equal(pages.references.cpu(), refs)
+    k, _ = wb.wave_pages_read(pages, n)
+    for b in (0, B // 2, B - 1):
+        held = x[b, 0, :lengths[b]]
+        whole = lengths[b] // page * page
+        assert torch.equal(k[b, 0, whole:lengths[b]].cpu(), held[whole:])
+        for p in range(0, whole, page):
+            codes, scale = po.page_codes(held[p:p + page].numpy())
+            assert np.array_equal(k[b, 0, p:p + page].cpu().numpy(), codes.astype(np.float32) * scale)
+
+
+def test_many_sequences_and_more_workgroups_than_a_launch_row():
+    """Two million sequences; the rows of every one of them are its own."""
+    B, d, page = (1 << 21) - 1, 64, 32
+    pages = wb.alloc_pages(torch.bfloat16, B, 1, d, page, 100, 1)
+    pages.lengths[::2] = 5
+    x = torch.randn(1, 1, 2, d, generator=_gen(8)).bfloat16().cuda()
+    k = x.expand(B, 1, 2, d)
+    wb.wave_pages_append(pages, k, k)
+    assert bool((pages.lengths[::2] == 7).all()) and bool((pages.lengths[1::2] == 2).all())
+    assert bool((pages.k_tail[::2, 0, 5:7] == x[0]).all()) and bool((pages.v_tail[1::2, 0, :2] == x[0]).all())
+    got, _ = wb.wave_pages_read(pages, 2, first=torch.where(torch.arange(B, device="cuda") % 2 == 0, 5, 0).to(torch.int32))
+    assert bool((got == x).all())
+    parent = torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    parent[-1] = B - 1
+    wb.wave_pages_reorder(pages, parent)
+    assert int(pages.lengths.sum()) == int(pages.lengths[-1]) == 7
+
+
+def test_lengths_and_entries_outside_count_as_the_nearest():
+    B, Hkv, d, page, most = 4, 2, 64, 32, 2
+    g = _gen(9)
+    pages = wb.alloc_pages(torch.float32, B, Hkv, d, page, 3, most)
+    x = torch.randn(B, Hkv, 40, d, generator=g).cuda()
+    wb.wave_pages_append(pages, x[:, :, :32], x[:, :, :32], counts=torch.tensor([32, 32, 32, 0], dtype=torch.int32, device="cuda"))
+    room = most * page + page - 1
+    pages.table.copy_(torch.tensor([[2, 0], [-5, 99], [1, 2], [7, 7]], dtype=torch.int32))
+    near = wb.alloc_pages(torch.float32, B, Hkv, d, page, 3, most, pool=pages)
+    near.table.copy_(torch.tensor([[2, 0], [0, 2], [1, 2], [2, 2]], dtype=torch.int32))
+    pages.lengths.copy_(torch.tensor([-7, room + 50, 70, -2 ** 31], dtype=torch.int32))
+    near.lengths.copy_(torch.tensor([0, room, 70, 0], dtype=torch.int32))
+    for s in (pages, near):
+        s.k_tail.copy_(x[:, :, :32]), s.v_tail.copy_(x[:, :, :32]), s.references.fill_(5)
+    q = torch.randn(B, 4, d, generator=g).cuda()
+    for a, b in zip(wb.wave_pages_attention_decode(q, pages) + wb.wave_pages_read(pages, 99),
+                    wb.wave_pages_attention_decode(q, near) + wb.wave_pages_read(near, 99)):
+        assert _same_bits(a, b)
+    parent = torch.tensor([1, 1, 3, 0], dtype=torch.int32, device="cuda")
+    after = []
+    for s in (pages, near):
+        to = wb.alloc_pages(torch.float32, B, Hkv, d, page, 3, most, pool=pages)
+        wb.wave_pages_reorder(s, parent, to)
+        after.append(to)
+    assert after[0].lengths.tolist() == after[1].lengths.tolist() == [room, room, 0, 0] and torch.equal(after[0].references, after[1].references)
+    wb.wave_pages_append(pages, x[:, :, :5], x[:, :, :5]), wb.wave_pages_append(near, x[:, :, :5], x[:, :, :5])
+    assert pages.lengths.tolist() == near.lengths.tolist() == [5, room, 75, 5]
+
+
+# --------------------------------------------------------------------------- attention
+def _check_attention(q, pages, lengths, out, lse, tag=""):
+    """Against fp64 over the codes, scales and tails that the cache holds, on the GPU."""
+    B, Hq, d = q.shape
+    Hkv, T = pages.Hkv, pages.page
+    G = Hq // Hkv
+    err2 = ref2 = 0.0
+    for b in range(B):
+        n = min(max(lengths[b], 0), pages.max_pages * T + T - 1)
+        at = pages.table[b, :n // T].long()
+        for h in range(Hkv):
+            rows = [torch.cat([(pages.t[c][at, h].double() * pages.t[s][at, h].double()[:, None, None]).reshape(-1, d), pages.t[t][b, h, :n % T].double()])
+                    for c, s, t in (("k_codes", "k_scales", "k_tail"), ("v_codes", "v_scales", "v_tail"))]
+            heads = slice(h * G, (h + 1) * G)
+            go, gl = out[b, heads].double(), lse[b, heads].double()
+            if n == 0:
+                assert not bool(go.any()) and bool((gl == -math.inf).all()), (tag, b, h)
+                continue
+            K, V = rows
+            qq = q[b, heads].double()
+            z = qq @ K.T / math.sqrt(d)
+            total = torch.logsumexp(z, -1)
+            p = torch.exp(z - total[:, None])
+            o = p @ V
+            delta = (3 * d + 6) * U * (qq.abs() @ K.abs().T) / math.sqrt(d)
+            mean = (p * 2 * delta).sum(-1, keepdim=True)
+            bar = (p * (2 * delta + (n + 24) * U)) @ V.abs() + o.abs() * (mean + 8 * U)
+            worst = ((go - o).abs() - bar).max()
+            assert float(worst) <= 1e-30, (tag, b, h, float((go - o).abs().max()))
+            bar = (p * delta).sum(-1) + (n + 16) * U + 4 * U * total.abs()
+            assert bool(((gl - total).abs() <= bar).all()), (tag, b, h, gl, total)
+            err2 += float(((go - o) ** 2).sum())
+            ref2 += float((p ** 2 @ V ** 2).sum())
+    assert err2 <= (1e-5 ** 2) * max(ref2, 1e-30) or ref2 == 0, (tag, math.sqrt(err2 / ref2))
+
+
+def _filled(dtype, B, Hkv, d, page, lengths, seed, max_pages=None, keys=1.0):
+    """A cache whose pages lie anywhere in the pool; what is not in use holds no numbers."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    most = max_pages or max(1, max(lengths) // page)
+    room = most * page + page - 1
+    inside = [min(max(n, 0), room) for n in lengths]
+    whole = sum(n // page for n in inside)
+    pool = whole + 3
+    pages = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, pool, most)
+    order = torch.randperm(pool, generator=g, device="cuda")
+    pages.k_codes.copy_(torch.randint(-127, 128, pages.k_codes.shape, generator=g, device="cuda", dtype=torch.int8))
+    pages.v_codes.copy_(torch.randint(-127, 128, pages.v_codes.shape, generator=g, device="cuda", dtype=torch.int8))
+    for name, size in (("k_scales", keys / 127), ("v_scales", 4 / 127)):
+        pages.t[name].copy_(size * (0.3 + torch.rand(pool, Hkv, generator=g, device="cuda")))
+        pages.t[name][order[whole:]] = math.nan
+    pages.k_tail.normal_(generator=g), pages.v_tail.normal_(generator=g)
+    pages.table.fill_(-1)
+    pages.references[order[:whole]] = 1
+    at = 0
+    for b, n in enumerate(inside):
+        pages.table[b, :n // page] = order[at:at + n // page].to(torch.int32)
+        at += n // page
+        pages.k_tail[b, :, n % page:], pages.v_tail[b, :, n % page:] = math.nan, math.nan
+    pages.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+    return pages
+
+
+def _query(dtype, B, Hq, d, seed, peak=1.0):
+    return (peak * torch.randn(B, Hq, d, generator=_gen(seed))).to(TYPES[dtype]).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [32, 64, 128])
+@pytest.mark.parametrize("B,Hq,Hkv,lengths,room", [
+    (1, 1, 1, [1], None), (1, 8, 1, [33], None), (2, 6, 2, [0, 129], None), (3, 7, 1, [128, 1, 130], None), (5, 10, 2, [0, 70, 31, 32, 64], 40),
+    (2, 24, 3, [1500, 7], None), (2, 2, 2, [-4, 99999], 3), (17, 16, 4, list(range(25, 42)), None), (4, 8, 2, [4000, 3999, 4096, 2017], 200),
+    (3, 5, 5, [255, 256, 257], 2)])
+def test_attention(dtype, d, page, B, Hq, Hkv, lengths, room):
+    pages = _filled(dtype, B, Hkv, d, page, lengths, B + page, room)
+    q = _query(dtype, B, Hq, d, B)
+    before = _state(pages)
+    out, lse = wb.wave_pages_attention_decode(q, pages)
+    _check_attention(q, pages, lengths, out, lse)
+    for name in before:
+        assert _same_bits(before[name], pages.t[name]), name
+    o2, l2 = torch.empty(B * Hq * d + 1, device="cuda")[1:].view(B, Hq, d), torch.empty(B * Hq + 1, device="cuda")[1:].view(B, Hq)
+    wb.wave_pages_attention_decode(q, pages, out=o2, lse=l2)          # (they need only lie on floats)
+    assert _same_bits(o2, out) and _same_bits(l2, lse)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("room", [None, 100])
+def test_attention_heads(dtype, G, room):
+    lengths = [300, 64, 0, 95, 511]
+    pages = _filled(dtype, 5, 3, 64, 32, lengths, G, room)
+    q = _query(dtype, 5, 3 * G, 64, G, 2.0)
+    _check_attention(q, pages, lengths, *wb.wave_pages_attention_decode(q, pages))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,Hq,Hkv,d,page,lengths", [
+    (1, 64, 64, 64, 32, [70001]),           # pieces of more steps than a wave looks up pages for at once
+    (1, 64, 64, 64, 128, [131100]), (1, 2, 1, 128, 64, [200000]), (70, 8, 2, 64, 64, [100 + 53 * b for b in range(70)]),
+    (3, 8, 8, 128, 64, [30000, 1, 64]), (300, 2, 1, 64, 32, [b % 50 for b in range(300)])])
+def test_attention_long_and_many(dtype, B, Hq, Hkv, d, page, lengths):
+    pages = _filled(dtype, B, Hkv, d, page, lengths, 3, 4 + max(lengths) // page)
+    q = _query(dtype, B, Hq, d, 4, 1.5)
+    _check_attention(q, pages, lengths, *wb.wave_pages_attention_decode(q, pages))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("room", [2, 60])
+def test_attention_extreme_scores(dtype, room):
+    """Scores of hundreds, growing row by row and falling; pages of scale 0 (all scores alike)."""
+    d, page, lengths = 64, 32, [80, 64, 95, 40]
+    pages = _filled(dtype, 4, 1, d, page, lengths, 5, room)
+    for b in range(4):
+        for i in range(lengths[b] // page):
+            p = int(pages.table[b, i])
+            ramp = torch.arange(page, device="cuda") * (1 if b % 2 else -1) + (i if b % 2 else -i)
+            pages.k_codes[p, 0] = ramp[:, None].clamp(-127, 127).to(torch.int8)
+            pages.k_scales[p, 0] = 0.0 if b == 2 else 1.0 + i
+    q = torch.full((4, 3, d), 0.5).to(TYPES[dtype]).cuda()
+    q[:, 1], q[:, 2] = -3.0, 40.0
+    _check_attention(q, pages, lengths, *wb.wave_pages_attention_decode(q, pages))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("room", [3, 60])
+def test_attention_of_pages_that_hold_no_numbers(dtype, room):
+    """They show in the heads that read them and in no others."""
+    d, page, lengths = 64, 32, [97, 97, 97]
+    pages = _filled(dtype, 3, 2, d, page, lengths, 6, room)
+    pages.k_scales[int(pages.table[0, 1]), 0] = math.nan
+    pages.v_scales[int(pages.table[1, 2]), 1] = math.nan
+    pages.v_tail[2, 0, 0, 9] = math.inf
+    q = _query(dtype, 3, 4, d, 6)
+    out, lse = wb.wave_pages_attention_decode(q, pages)
+    assert bool(torch.isnan(out[0, :2]).all()) and bool(torch.isnan(lse[0, :2]).all()) and bool(torch.isfinite(out[0, 2:]).all())
+    assert bool(torch.isnan(out[1, 2:]).all()) and bool(torch.isfinite(out[1, :2]).all()) and bool(torch.isfinite(lse[1:]).all())
+    bad = ~torch.isfinite(out[2])
+    assert bool(bad[:2, 9].all()) and int(bad.sum()) == 2
+
+
+def test_attention_weights_keep_their_bits():
+    """One heavy row among light ones: what a weight loses shows in channels where only light rows have values."""
+    d, page, n = 64, 32, 128
+    pages = _filled("bf16", 1, 1, d, page, [n], 7, 60)
+    pages.k_codes.zero_(), pages.v_codes.zero_()
+    heavy, light = int(pages.table[0, 0]), int(pages.table[0, 2])
+    pages.k_codes[heavy, 0, 3, :] = 127
+    pages.v_codes[heavy, 0, 3, 0], pages.v_codes[light, 0, :, 1] = 127, 127
+    q = torch.full((1, 1, d), 0.25).bfloat16().cuda()
+    out, lse = wb.wave_pages_attention_decode(q, pages)
+    z = torch.zeros(n, dtype=torch.float64)
+    z[3] = 0.25 * 64 * 127 * float(pages.k_scales[heavy, 0]) / 8
+    p = torch.softmax(z, 0)
+    want = torch.zeros(d, dtype=torch.float64)
+    want[0], want[1] = p[3] * 127 * float(pages.v_scales[heavy, 0]), 32 * p[64] * 127 * float(pages.v_scales[light, 0])
+    # the score's roundings, (3 d + 6) u of it twice; 32 + 16 for the sums
+    bar = want * (2 * (3 * d + 6) * U * float(z[3]) + 48 * U) + 1e-30
+    assert bool(((out[0, 0].double().cpu() - want).abs() <= bar).all()), (out[0, 0, :2], want[:2])
+
+
+def test_attention_over_raw_rows_is_the_plain_caches():
+    """While no page is complete nothing is rounded: the plain cache's attention over the same rows."""
+    B, Hq, Hkv, d, n = 3, 8, 2, 128, 127
+    g = _gen(10)
+    q, k, v = (torch.randn(B, h, m, d, generator=g).bfloat16().cuda() for h, m in ((Hq, 1), (Hkv, n), (Hkv, n)))
+    counts = torch.tensor([n, 1, 60], dtype=torch.int32, device="cuda")
+    pages, cache = wb.alloc_pages(torch.bfloat16, B, Hkv, d, 128, 4, 1), wb.alloc_cache(torch.bfloat16, B, Hkv, d, n)
+    wb.wave_pages_append(pages, k, v, counts=counts), wb.wave_cache_append(cache, k, v, counts=counts)
+    a, b = wb.wave_pages_attention_decode(q[:, :, 0], pages), wb.wave_cache_attention_decode(q[:, :, 0], cache)
+    _check_attention(q[:, :, 0], pages, counts.tolist(), *a)
+    for x, y in zip(a, b):
+        assert float((x - y).abs().max()) <= 1e-5 * float(y.abs().max())    # (the same products, sums in another order: 127 of them, 2^-24 each)
+
+
+# --------------------------------------------------------------------------- reorder
+def test_reorder_copies_forks_and_frees():
+    dtype, B, Hkv, d, page, n_pages, most = "bf16", 5, 2, 64, 32, 60, 6
+    g = _gen(11)
+    rng = np.random.default_rng(11)
+    pages, plain = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, n_pages, most), po.Paged(B, page, n_pages, most)
+    for step in range(14):
+        n = int(rng.integers(1, 50))
+        k, v = (torch.randn(pages.B, Hkv, n, d, generator=g).to(TYPES[dtype]) for _ in range(2))
+        counts = rng.integers(0, n + 1, pages.B).tolist()
+        wb.wave_pages_append(pages, k.cuda(), v.cuda(), counts=torch.tensor(counts, dtype=torch.int32, device="cuda"))
+        plain.append(_as_rows(k), _as_rows(v), counts)
+        _check_state(pages, plain, ("append", step))
+        before = _state(pages)
+        if step % 3 == 2:     # in place: some leave
+            parent = [b if rng.random() < 0.6 else int(rng.integers(-2, 9)) for b in range(pages.B)]
+            after = wb.wave_pages_reorder(pages, torch.tensor(parent, dtype=torch.int32, device="cuda"))
+            assert after is pages
+            plain = plain.reorder([b if parent[b] == b else -1 for b in range(pages.B)])
+        else:
+            to_B = int(rng.integers(1, 9))
+            parent = rng.integers(-1, pages.B + 1, to_B).tolist()
+            to = wb.alloc_pages(TYPES[dtype], to_B, Hkv, d, page, n_pages, most, pool=pages)
+            to.k_tail.fill_(2.0), to.table.fill_(55), to.references.fill_(99)
+            assert wb.wave_pages_reorder(pages, torch.tensor(parent, dtype=torch.int32, device="cuda"), to) is to
+            for name in before:
+                assert _same_bits(before[name], pages.t[name]), (step, name)
+            plain = plain.reorder(parent)
+            for b in range(to_B):
+                assert bool((to.k_tail[b, :, len(plain.tails[b]):] == 2.0).all()) and bool((to.table[b, len(plain.pages[b]):] == 55).all())
+            pages = to
+        _check_state(pages, plain, ("reorder", step))
+        held = sum(plain.pages, [])
+        assert plain.references == [held.count(p) for p in range(n_pages)]
+
+
+def test_reorder_identity_and_a_callers_own_reference():
+    B, Hkv, d, page = 3, 1, 64, 32
+    x = torch.randn(B, Hkv, 70, d, generator=_gen(12)).cuda()
+    pages = wb.alloc_pages(torch.float32, B, Hkv, d, page, 8, 3)
+    wb.wave_pages_append(pages, x, x)
+    pages.references[:2] += 1                                           # the first prompt stays
+    same = wb.wave_pages_reorder(pages, torch.arange(B, dtype=torch.int32, device="cuda"), wb.alloc_pages(torch.float32, B, Hkv, d, page, 8, 3, pool=pages))
+    assert torch.equal(same.references, pages.references) and torch.equal(same.table[:, :2], pages.table[:, :2])
+    assert _same_bits(same.k_tail[:, :, :6], pages.k_tail[:, :, :6]) and same.lengths.tolist() == [70] * 3
+    wb.wave_pages_reorder(pages, torch.full((B,), -1, dtype=torch.int32, device="cuda"))
+    assert pages.references.tolist() == [1, 1, 0, 0, 0, 0, 0, 0] and pages.lengths.tolist() == [0, 0, 0]
+    wb.wave_pages_append(pages, x, x)
+    assert pages.table[:, :2].tolist() == [[2, 3], [4, 5], [6, 7]]     # not the kept ones
+
+
+# --------------------------------------------------------------------------- together
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_conversation(dtype):
+    """A prompt, its forks decoding token by token with normed and turned queries and keys, drafts taken back, beams reordered,
+    sequences that leave and new ones: every state against the plain statement, every step's attention against fp64."""
+    B, Hq, Hkv, d, page, n_pages, most = 4, 6, 2, 64, 32, 40, 6
+    g = _gen(13)
+    rng = np.random.default_rng(13)
+    r = wb.wave_rotary_plan(64, 1e4, [16, 16], wb.WAVE_ROTARY_TURNS)
+    qw, kw = ((1 + 0.2 * torch.randn(d, generator=g)).to(TYPES[dtype]).cuda() for _ in range(2))
+    new = lambda pool=None: wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, n_pages, most, pool=pool)
+    pages, plain = new(), po.Paged(B, page, n_pages, most)
+    spare = new(pages)
+    ws = wb.workspace(max(wb.wave_pages_append_workspace(pages), wb.wave_pages_attention_workspace(pages, Hq)))
+
+    def tokens(n):
+        x = torch.randn(B, n, Hq + 2 * Hkv, d, generator=g).to(TYPES[dtype]).cuda().transpose(1, 2)
+        return x.split([Hq, Hkv, Hkv], 1)
+
+    def append(state, to, plain, n, counts):
+        q, k, v = tokens(n)
+        at = (state.lengths[:, None] + torch.arange(n, device="cuda")).expand(2, B, n).to(torch.int32).contiguous()
+        _, kt = wb.wave_norm_rotary_apply(None, k, None, kw, 1e-6, at, r)
+        c = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+        qt = wb.wave_pages_append(state, k, v, q=q, q_weight=qw, k_weight=kw, rotary=r, counts=c, to=to, ws=ws)
+        if plain is not None:
+            plain.append(_as_rows(kt), _as_rows(v), counts)
+        return qt
+
+    append(pages, None, plain, 75, [75, 0, 0, 0])
+    pages, spare = wb.wave_pages_reorder(pages, torch.zeros(B, dtype=torch.int32, device="cuda"), spare), pages
+    plain = plain.reorder([0] * B)
+    _check_state(pages, plain, "forked")
+    assert pages.references[:2].tolist() == [B, B]
+    for step in range(50):
+        if step % 9 == 4:      # three drafted tokens, taken back
+            kept = _state(pages)
+            append(pages, spare, None, 3, None)
+            for name in OWN:
+                assert _same_bits(kept[name], pages.t[name]), (step, name)
+        qt = append(pages, None, plain, 1, None)
+        _check_state(pages, plain, step)
+        lengths = [plain.length(b) for b in range(B)]
+        out, lse = wb.wave_pages_attention_decode(qt[:, :, 0], pages, ws=ws)
+        _check_attention(qt[:, :, 0], pages, lengths, out, lse, step)
+        if step % 7 == 6:
+            parent = rng.integers(-1, B, B).tolist()
+            pages, spare = wb.wave_pages_reorder(pages, torch.tensor(parent, dtype=torch.int32, device="cuda"), spare), pages
+            plain = plain.reorder(parent)
+            _check_state(pages, plain, step)
+
+
+def test_an_index_from_pages_and_the_newest_rows_join_by_their_normalisers():
+    """A prompt goes into pages; an index is built from the rows read back, the tokens behind it stay in the plain cache, and the
+    two parts join: full attention over the rows that are held."""
+    B, Hq, Hkv, d, N, new = 1, 4, 2, 64, 1024, 30
+    g = _gen(14)
+    k, v, kn, vn = (torch.randn(B, Hkv, n, d, generator=g).cuda() for n in (N, N, new, new))
+    q = torch.randn(B, Hq, d, generator=g).cuda()
+    pages = wb.alloc_pages(torch.float32, B, Hkv, d, 64, 20, 17)
+    wb.wave_pages_append(pages, k, v)
+    K, V = wb.wave_pages_read(pages, N)
+    ix = wb.wave_index_build(K, V, 4, 64, 512, 32, 3, 0)
+    o1, l1, _ = wb.wave_attention_decode(q, ix, ix.m)
+    o0, l0 = wb.wave_pages_attention_decode(q, pages)
+    assert float((o1 - o0).abs().max()) <= 2e-4 and float((l1 - l0).abs().max()) <= 2e-4     # every cluster retrieved: full attention
+    tail = wb.alloc_cache(torch.float32, B, Hkv, d, new)
+    wb.wave_cache_append(tail, kn, vn)
+    o2, l2 = wb.wave_cache_attention_decode(q, tail)
+    total = torch.logaddexp(l1, l2)
+    joined = o1 * torch.exp(l1 - total)[..., None] + o2 * torch.exp(l2 - total)[..., None]
+    want, lse = wb.wave_full_attention_decode(q, torch.cat([K, kn], 2), torch.cat([V, vn], 2))
+    assert float((joined - want).abs().max()) <= 4e-4 and float((total - lse).abs().max()) <= 4e-4
+
+
+def test_captured_steps_replay():
+    """A captured step (append into the state beside, attention, and back) replayed with work of its own between the replays,
+    against the same steps run eagerly; another captured graph shares the workspace."""
+    dtype, B, Hq, Hkv, d, page = "bf16", 3, 8, 2, 128, 32
+    r = wb.wave_rotary_plan(128, 1e4)
+    g = _gen(15)
+    w = (1 + 0.2 * torch.randn(d, generator=g)).bfloat16().cuda()
+    tokens = [[torch.randn(B, h, 1, d, generator=g).bfloat16().cuda() for h in (Hq, Hkv, Hkv)] for _ in range(9)]
+    lengths = [60, 27, 0]
+    parent = torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda")
+
+    def make():
+        a = _filled(dtype, B, Hkv, d, page, lengths, 8, 20)
+        b = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, a.n_pages, 20, pool=a)
+        ws = wb.workspace(max(wb.wave_pages_append_workspace(a), wb.wave_pages_attention_workspace(a, Hq)))
+        bufs = dict(q=tokens[0][0].clone(), k=tokens[0][1].clone(), v=tokens[0][2].clone(), q_out=torch.empty_like(tokens[0][0]),
+                    out=torch.empty(B, Hq, d, device="cuda"), lse=torch.empty(B, Hq, device="cuda"))
+        return a, b, ws, bufs
+
+    def step(a, b, ws, x):
+        wb.wave_pages_append(a, x["k"], x["v"], q=x["q"], q_weight=w, k_weight=w, rotary=r, q_out=x["q_out"], to=b, ws=ws)
+        wb.wave_pages_attention_decode(x["q_out"].view(B, Hq, d), b, out=x["out"], lse=x["lse"], ws=ws)
+        wb.wave_pages_reorder(b, parent, a)
+
+    ae, be, we, xe = make()
+    ag, bg, wg, xg = make()
+    ah, bh, _, xh = make()
+    step(*make())                                      # first launches outside the capture
+    torch.cuda.synchronize()
+    saved = [(_state(a), _state(b)) for a, b in ((ag, bg), (ah, bh))]
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(ag, bg, wg, xg)
+    with torch.cuda.graph(other):
+        step(ah, bh, wg, xh)
+    for (sa, sb), a, b in zip(saved, (ag, ah), (bg, bh)):
+        for n in sa:
+            a.t[n].copy_(sa[n]), b.t[n].copy_(sb[n])
+    for i, (q, k, v) in enumerate(tokens):
+        for x in (xe, xg, xh):
+            x["q"].copy_(q), x["k"].copy_(k), x["v"].copy_(v)
+        step(ae, be, we, xe)
+        torch.cuda.synchronize()
+        graph.replay()
+        other.replay()
+        torch.cuda.synchronize()
+        for x, a in ((xg, ag), (xh, ah)):
+            assert _same_bits(xe["out"], x["out"]) and _same_bits(xe["lse"], x["lse"]) and _same_bits(xe["q_out"], x["q_out"]), i
+            assert torch.equal(ae.lengths, a.lengths) and torch.equal(ae.references, a.references), i
+            for b in range(B):
+                n = int(a.lengths[b])
+                assert torch.equal(ae.table[b, :n // page], a.table[b, :n // page]) and _same_bits(ae.k_tail[b, :, :n % page], a.k_tail[b, :, :n % page]), i
+            assert all(_same_bits(u, t) for u, t in zip(wb.wave_pages_read(ae, 80), wb.wave_pages_read(a, 80))), i
+    assert sorted(ae.lengths.tolist()) == sorted(n + len(tokens) for n in lengths)
+
+
+def test_two_streams_and_repeated_calls_give_the_same_bits():
+    lengths = [700, 31, 0, 64]
+    pages = _filled("bf16", 4, 2, 128, 64, lengths, 16, 30)
+    q = _query("bf16", 4, 14, 128, 16)
+    first = wb.wave_pages_attention_decode(q, pages)
+    x = torch.randn(4, 2, 100, 128, generator=_gen(16)).bfloat16().cuda()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [wb.workspace(wb.wave_pages_attention_workspace(pages, 14)) for _ in streams]
+    outs, reads = [], []
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, w in zip(streams, ws):
+            with torch.cuda.stream(s):
+                outs.append(wb.wave_pages_attention_decode(q, pages, ws=w))
+                own = wb.alloc_pages(torch.bfloat16, 4, 2, 128, 32, 40, 5)
+                wb.wave_pages_append(own, x, x)
+                reads.append(wb.wave_pages_read(own, 100)[0])
+    torch.cuda.synchronize()
+    for out, lse in outs:
+        assert _same_bits(out, first[0]) and _same_bits(lse, first[1])
+    for k in reads:
+        assert _same_bits(k, reads[0])
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GiB, used at its far end."""
+    B, Hkv, d, page, n = 1, 8, 128, 128, 300
+    n_pages = 33000                                    # 4.3e9 bytes of codes
+    pages = wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, n_pages, 4)
+    small = wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, 3, 4)
+    pages.references.fill_(1)
+    pages.references[-3:] = 0
+    g = _gen(17)
+    k, v = (torch.randn(B, Hkv, n, d, generator=g).bfloat16().cuda() for _ in range(2))
+    q = _query("bf16", B, 16, d, 17)
+    got = []
+    for s in (pages, small):
+        wb.wave_pages_append(s, k, v)
+        to = wb.wave_pages_reorder(s, torch.zeros(1, dtype=torch.int32, device="cuda"), wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, s.n_pages, 4, pool=s))
+        got.append(wb.wave_pages_attention_decode(q, to) + wb.wave_pages_read(to, n))
+    assert pages.table[0, :2].tolist() == [n_pages - 3, n_pages - 2] and bool(pages.k_codes[-3].any()) and not bool(pages.k_codes[:100].any())
+    for a, b in zip(*got):
+        assert _same_bits(a, b)
