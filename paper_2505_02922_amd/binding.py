@@ -701,34 +701,30 @@ def wave_cache_evict(cache: Cache, n_keep: int, n_sink: int, n_local: int, to: O
     return to
 
 
-def _rows(t: torch.Tensor, to_keep: List[torch.Tensor]) -> wave_rows:
-    """t [B, H, N, d] as it lies where the library can read it so (rows of neighbouring channels, on 16 bytes), otherwise a
-    copy of it."""
-    shape, strides, unit = t.shape, t.stride(), 16 // t.element_size()
-    if strides[3] != 1 or t.data_ptr() % 16 or any([strides[i] % unit and shape[i] > 1 for i in (0, 1, 2)]):
-        t = t.contiguous()
-        strides = t.stride()
-    to_keep.append(t)
-    return wave_rows(t.data_ptr(), *[strides[i] if shape[i] > 1 else 0 for i in (0, 1, 2)])
+def _rows(t: torch.Tensor, mask: int) -> Tuple[wave_rows, torch.Tensor]:
+    """t [B, H, N, d] as it lies where the library can read it so (rows of neighbouring channels on 16 bytes, which are
+    mask + 1 elements), otherwise a copy of it; and the tensor that has to live until the call is made."""
+    b, h, n, c = t.stride()
+    at = t.data_ptr()
+    if c != 1 or at & 15 or (b | h | n) & mask:
+        B, H, N, _ = t.shape
+        b, h, n = b if B > 1 else 0, h if H > 1 else 0, n if N > 1 else 0
+        if c != 1 or at & 15 or (b | h | n) & mask:
+            t = t.clone(memory_format=torch.contiguous_format)
+            b, h, n, _ = t.stride()
+            at = t.data_ptr()
+    return wave_rows(at, b, h, n), t
 
 
-def _head_norm(where: str, dtype: torch.dtype, d: int, q_weight: Optional[torch.Tensor],
-               k_weight: Optional[torch.Tensor], eps: float, to_keep: List[torch.Tensor]) -> Optional[wave_head_norm]:
-    if q_weight is None and k_weight is None:
+def _weight(where: str, w: Optional[torch.Tensor], dtype: torch.dtype, d: int) -> Optional[torch.Tensor]:
+    """A norm's weight [d], on 16 bytes."""
+    if w is None:
         return None
-    at = []
-    for w in (q_weight, k_weight):
-        if w is not None:
-            if w.dtype != dtype:
-                raise WaveError(3, where)
-            if w.shape != (d,):
-                raise WaveError(2, where)
-            w = w.contiguous()
-            if w.data_ptr() % 16:
-                w = w.clone()
-            to_keep.append(w)
-        at.append(_address(w))
-    return wave_head_norm(*at, eps)
+    if w.dtype != dtype:
+        raise WaveError(3, where)
+    if w.shape != (d,):
+        raise WaveError(2, where)
+    return w if w.is_contiguous() and not w.data_ptr() & 15 else w.clone(memory_format=torch.contiguous_format)
 
 
 def wave_norm_rotary_apply(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor] = None,
@@ -740,32 +736,51 @@ def wave_norm_rotary_apply(q: Optional[torch.Tensor], k: Optional[torch.Tensor],
     then turned by coords [n_axes, B, N] int32.  Returns (q, k) so, dense, in q_out and k_out where they are given (a dense
     input itself: in place)."""
     where = "wave_norm_rotary_apply"
-    given = [t for t in (q, k) if t is not None]
-    _require(bool(given) and all([t.dim() == 4 for t in given]), 2, where)
-    B, _, N, d = given[0].shape
-    dtype, index = given[0].dtype, given[0].get_device()
-    _require(all([t.shape[0] == B and t.shape[2] == N and t.shape[3] == d for t in given]), 2, where)
-    _require(all([t.dtype == dtype for t in given]), 3, where)
-    keep: List[torch.Tensor] = []
+    one = k if q is None else q
+    if one is None or one.dim() != 4:
+        raise WaveError(2, where)
+    B, _, N, d = one.shape
+    dtype = one.dtype
+    code = _dtype_code(dtype)
+    mask = 3 if code == WAVE_F32 else 7
+    Hq = Hkv = 0
+    rows_q = rows_k = None
+    if q is None:
+        q_out = None
+    else:
+        shape = q.shape
+        Hq = shape[1]
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else _as_is(where, q_out, dtype, shape)
+        rows_q, keep_q = _rows(q, mask)
+    if k is None:
+        k_out = None
+    else:
+        shape = k.shape
+        if len(shape) != 4 or shape[0] != B or shape[2] != N or shape[3] != d:
+            raise WaveError(2, where)
+        if k.dtype != dtype:
+            raise WaveError(3, where)
+        Hkv = shape[1]
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else _as_is(where, k_out, dtype, shape)
+        rows_k, keep_k = _rows(k, mask)
     if coords is not None:
-        _require(rotary is not None, 1, where)
-        _require(coords.dtype == torch.int32, 3, where)
-        _require(coords.shape == (rotary.n_axes, B, N), 2, where)
+        if rotary is None:
+            raise WaveError(1, where)
+        if coords.dtype != torch.int32:
+            raise WaveError(3, where)
+        if coords.shape != (rotary.n_axes, B, N):
+            raise WaveError(2, where)
         coords = coords.contiguous()
-    norm = _head_norm(where, dtype, d, q_weight, k_weight, eps, keep)
-    outs, rows = [], []
-    for t, out in ((q, q_out), (k, k_out)):
-        if t is None:
-            outs.append(None)
-            rows.append(None)
-            continue
-        outs.append(torch.empty_like(t, memory_format=torch.contiguous_format) if out is None else _as_is(where, out, dtype, t.shape))
-        rows.append(_rows(t, keep))
-    _together(where, index, q, k, q_weight, k_weight, coords, *outs)
-    if B and N and all([t.shape[1] for t in given]):
-        _enqueue(where, index, rows[0], 0 if q is None else q.shape[1], rows[1], 0 if k is None else k.shape[1], norm, rotary,
-                 _address(coords), _dtype_code(dtype), B, N, d, _address(outs[0]), _address(outs[1]))
-    return outs[0], outs[1]
+    norm = None
+    if q_weight is not None or k_weight is not None:
+        q_weight, k_weight = _weight(where, q_weight, dtype, d), _weight(where, k_weight, dtype, d)
+        norm = wave_head_norm(_address(q_weight), _address(k_weight), eps)
+    index = one.get_device()
+    _together(where, index, q, k, q_weight, k_weight, coords, q_out, k_out)
+    if B and N and (Hq or Hkv):
+        _enqueue(where, index, rows_q if Hq else None, Hq, rows_k if Hkv else None, Hkv, norm, rotary, _address(coords), code, B, N, d, _address(q_out),
+                 _address(k_out))
+    return q_out, k_out
 
 
 PAGE_POOL = ("k_codes", "v_codes", "k_scales", "v_scales")
@@ -850,8 +865,7 @@ def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optiona
         raise WaveError(2, where)
     if k.dtype != dtype or v.dtype != dtype:
         raise WaveError(3, where)
-    n, Hq = shape[2], 0
-    keep: List[torch.Tensor] = []
+    n, Hq, mask = shape[2], 0, 3 if dtype == torch.float32 else 7
     rows_q = None
     if q is not None:
         heads = q.shape
@@ -865,7 +879,7 @@ def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optiona
             q_out = new(q, memory_format=torch.contiguous_format)
         else:
             _as_is(where, q_out, dtype, heads)
-        rows_q = _rows(q, keep)
+        rows_q, keep_q = _rows(q, mask)
     else:
         q_out = None
     if coords is not None:
@@ -882,13 +896,19 @@ def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optiona
         if counts.shape != (B,):
             raise WaveError(2, where)
         counts = counts.contiguous()
-    norm = _head_norm(where, dtype, d, q_weight, k_weight, eps, keep)
+    norm = None
+    if q_weight is not None or k_weight is not None:
+        q_weight, k_weight = _weight(where, q_weight, dtype, d), _weight(where, k_weight, dtype, d)
+        norm = wave_head_norm(_address(q_weight), _address(k_weight), eps)
     if ws is None:
         ws = workspace(wave_pages_append_workspace(pages), pages.t["k_codes"].device)
-    _require(to.index == pages.index, 1, where)
+    if to.index != pages.index:
+        raise WaveError(1, where)
     _together(where, pages.index, k, v, q, q_out, q_weight, k_weight, coords, counts, ws)
-    _enqueue(where, pages.index, pages.ref, to.ref, _rows(k, keep), _rows(v, keep), rows_q, Hq, n, _address(counts), norm, rotary,
-             _address(coords), _address(q_out), ws.data_ptr(), ws.nbytes)
+    rows_k, keep_k = _rows(k, mask)
+    rows_v, keep_v = _rows(v, mask)
+    _enqueue(where, pages.index, pages.ref, to.ref, rows_k, rows_v, rows_q, Hq, n, _address(counts), norm, rotary, _address(coords),
+             _address(q_out), ws.data_ptr(), ws.nbytes)
     return q_out
 
 

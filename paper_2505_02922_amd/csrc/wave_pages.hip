@@ -516,18 +516,19 @@ wave_status pages_append_td(const wave_pages& from, const wave_pages& to, const 
 }
 
 // ----------------------------------------------------------------------------
-// Reading back.  A thread has 16 codes of a row; READ_ROWS rows of a workgroup's tile are in flight in each thread.
+// Reading back.  A wave has 32 rows that begin at a multiple of 32, so they are one page's, or the tail's: its page and scale
+// are the wave's.  A lane turns what it loads into 16 bytes, neighbouring lanes into neighbouring ones.
 // ----------------------------------------------------------------------------
 struct ReadArgs {
   const int32_t* first;
   char *k_out, *v_out;
   int n, tiles;
 };
-constexpr int READ_ROWS = 4;
+constexpr int READ_CHUNK = 32, READ_TILE = 4 * READ_CHUNK;
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void pages_read_kernel(const wave_pages p, const ReadArgs a, int sides) {
-  constexpr int LANES = D / 16, SIDE = 256 / LANES, TILE = SIDE * READ_ROWS;
+  constexpr int EPC = Elem<T>::EPC, LANES = D / EPC, SIDE = 64 / LANES, STEPS = READ_CHUNK / SIDE;
   constexpr size_t ROW = D * sizeof(T);
   unsigned block = workgroup_number();
   const bool keys = sides == 2 ? (block & 1) == 0 : a.k_out != nullptr;
@@ -536,58 +537,49 @@ __global__ __launch_bounds__(256) void pages_read_kernel(const wave_pages p, con
   const unsigned unit = block / a.tiles;
   if (unit >= (unsigned)(p.B * p.Hkv)) return;
   const int b = unit / p.Hkv, h = unit % p.Hkv, shift = page_shift(p.page);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int length = pages_length(p, b), whole = length >> shift << shift;
   const long long first = a.first ? a.first[b] : 0;
-  const int lane = threadIdx.x % LANES;
-  const int8_t* codes = keys ? p.k_codes : p.v_codes;
-  const float* scales = keys ? p.k_scales : p.v_scales;
-  const char* tail = static_cast<const char*>(keys ? p.k_tail : p.v_tail);
-  char* out = keys ? a.k_out : a.v_out;
-  const int t0 = tile * TILE + threadIdx.x / LANES;
-  if (first + (long long)tile * TILE >= length) return;
-  int page[READ_ROWS];
-  float scale[READ_ROWS];
-  uint4 c[READ_ROWS];
+  const long long at = (first >> 5 << 5) + (long long)tile * READ_TILE + wave * READ_CHUNK;  // the wave's first row
+  const long long low = first > 0 ? first : 0, high = min(first + a.n, (long long)length);
+  if (at + READ_CHUNK <= low || at >= high) return;
+  const int c0 = (int)at, sub = lane / LANES, part = lane % LANES;
+  char* out = (keys ? a.k_out : a.v_out) + ((size_t)unit * a.n + sub) * ROW + part * 16 + (at - first) * (long long)ROW;
+  auto inside = [&](int i) { return c0 + i * SIDE + sub >= low && c0 + i * SIDE + sub < high; };
+  if (c0 >= whole) {
+    const char* from = static_cast<const char*>(keys ? p.k_tail : p.v_tail) + ((size_t)unit * p.page + (c0 - whole) + sub) * ROW + part * 16;
+#pragma unroll 4
+    for (int i = 0; i < STEPS; ++i)
+      if (inside(i)) store16(out + (size_t)i * SIDE * ROW, load16(from + (size_t)i * SIDE * ROW));
+    return;
+  }
+  const size_t held = (size_t)page_entry(p, b, c0 >> shift) * p.Hkv + h;
+  const float scale = (keys ? p.k_scales : p.v_scales)[held];
+  const int8_t* from = (keys ? p.k_codes : p.v_codes) + ((held << shift) + (c0 & (p.page - 1)) + sub) * D + part * EPC;
+  uint32_t word[STEPS][EPC / 4];
 #pragma unroll
-  for (int i = 0; i < READ_ROWS; ++i) {
-    const long long at = first + t0 + i * SIDE;
-    page[i] = at >= 0 && at < whole ? page_entry(p, b, (int)at >> shift) : 0;
+  for (int i = 0; i < STEPS; ++i) {
+    if constexpr (EPC == 8) {
+      const uint2 u = load8_stream(from + i * SIDE * D);
+      word[i][0] = u.x;
+      word[i][1] = u.y;
+    } else {
+      word[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(from + i * SIDE * D));
+    }
   }
 #pragma unroll
-  for (int i = 0; i < READ_ROWS; ++i) {
-    const long long at = first + t0 + i * SIDE;
-    const size_t row = ((size_t)page[i] * p.Hkv + h);
-    scale[i] = scales[row];
-    c[i] = load16(codes + ((row << shift) + ((int)at & (p.page - 1))) * D + lane * 16);
-  }
+  for (int i = 0; i < STEPS; ++i) {
+    float f[EPC];
 #pragma unroll
-  for (int i = 0; i < READ_ROWS; ++i) {
-    const int t = t0 + i * SIDE;
-    const long long at = first + t;
-    if (t >= a.n || at < 0 || at >= length) continue;
-    char* to = out + ((size_t)unit * a.n + t) * ROW + lane * 16 * sizeof(T);
-    constexpr int CHUNKS = (int)sizeof(T), EPC = Elem<T>::EPC;  // of 16 bytes
-    if (at >= whole) {
-      const char* from = tail + ((size_t)unit * p.page + (at - whole)) * ROW + lane * 16 * sizeof(T);
-#pragma unroll
-      for (int j = 0; j < CHUNKS; ++j) store16(to + j * 16, load16(from + j * 16));
-      continue;
-    }
-    const uint32_t word[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-#pragma unroll
-    for (int j = 0; j < CHUNKS; ++j) {
-      float f[EPC];
-#pragma unroll
-      for (int e = 0; e < EPC; ++e) f[e] = (float)(int8_t)(word[(j * EPC + e) / 4] >> (8 * ((j * EPC + e) & 3))) * scale[i];
-      store16(to + j * 16, pack<T>(f));
-    }
+    for (int e = 0; e < EPC; ++e) f[e] = (float)(int8_t)(word[i][e / 4] >> (8 * (e & 3))) * scale;
+    if (inside(i)) store16(out + (size_t)i * SIDE * ROW, pack<T>(f));
   }
 }
 
 template <typename T, int D>
 wave_status pages_read_td(const wave_pages& p, ReadArgs a, hipStream_t st) {
-  constexpr int TILE = 256 / (D / 16) * READ_ROWS;
-  a.tiles = (a.n + TILE - 1) / TILE;
+  // (the first chunk begins up to 31 rows before the first row, which is the device's)
+  a.tiles = (int)(((long long)a.n + (a.first ? READ_CHUNK - 1 : 0) + READ_TILE - 1) / READ_TILE);
   const int sides = (a.k_out ? 1 : 0) + (a.v_out ? 1 : 0);
   WAVE_LAUNCH("pages_read", (pages_read_kernel<T, D>), grid_rows((long long)p.B * p.Hkv * a.tiles * sides), 256, 0, st, p, a, sides);
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
@@ -601,60 +593,66 @@ __device__ __forceinline__ int parent_of(const wave_pages& from, const int32_t* 
   return p >= 0 && p < from.B ? p : -1;
 }
 
-// to's own arrays: tails, tables and lengths from the parents', references as they were
-__global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, int row_bytes,
-                                                         unsigned tail_blocks) {
+// to's references as from's: what the next launch adds to
+__global__ __launch_bounds__(256) void pages_references_kernel(const int32_t* from, int32_t* to, int n) {
+  const long long i = (long long)workgroup_number() * 256 + threadIdx.x;
+  if (i < n) to[i] = from[i];
+}
+
+// Into arrays of its own.  The first workgroups change references: one for each sequence of `to`, which leaves table and length
+// too, and one for each of `from`; a sequence that stays where it is changes nothing.  The others copy the tails, a head's keys
+// or values each, and take longer.
+__global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, int row_bytes) {
   unsigned block = workgroup_number();
-  if (block < tail_blocks) {  // a head's keys or values of a sequence's tail
-    const bool keys = (block & 1) == 0;
-    const unsigned unit = block / 2;
-    const int b = unit / from.Hkv, h = unit % from.Hkv;
-    if (b >= to.B) return;
-    const int s = parent_of(from, parent, b);
-    if (s < 0) return;
-    const int chunks = (pages_length(from, s) & (from.page - 1)) * (row_bytes / 16);
-    const char* x = static_cast<const char*>(keys ? from.k_tail : from.v_tail) + ((size_t)s * from.Hkv + h) * from.page * row_bytes;
-    char* y = static_cast<char*>(keys ? to.k_tail : to.v_tail) + (size_t)unit * to.page * row_bytes;
-    for (int i = threadIdx.x; i < chunks; i += 256) store16(y + (size_t)i * 16, load16(x + (size_t)i * 16));
-    return;
-  }
-  block -= tail_blocks;
+  const int shift = page_shift(from.page);
   if (block < (unsigned)to.B) {
     const int b = block, s = parent_of(from, parent, b);
-    const int length = s < 0 ? 0 : pages_length(from, s), whole = length >> page_shift(from.page);
-    for (int i = threadIdx.x; i < whole; i += 256) to.table[(size_t)b * to.max_pages + i] = from.table[(size_t)s * from.max_pages + i];
+    const int length = s < 0 ? 0 : pages_length(from, s), whole = length >> shift;
     if (threadIdx.x == 0) to.lengths[b] = length;
+    for (int i = threadIdx.x; i < whole; i += 256) {
+      const int entry = from.table[(size_t)s * from.max_pages + i];
+      to.table[(size_t)b * to.max_pages + i] = entry;
+      if (s != b) atomicAdd(&to.references[min(max(entry, 0), from.n_pages - 1)], 1);
+    }
     return;
   }
   block -= to.B;
-  const long long i = (long long)block * 256 + threadIdx.x;
-  if (i < from.n_pages) to.references[i] = from.references[i];
-}
-
-// One workgroup for each sequence of `to` (what it holds) and of `from` (what it held).  One that stays where it is changes
-// nothing.  In place: those that leave.
-__global__ __launch_bounds__(256) void pages_count_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, bool apart) {
-  int b = workgroup_number();
-  const int shift = page_shift(from.page);
-  if (!apart) {
-    if (b >= from.B || parent[b] == b) return;
+  if (block < (unsigned)from.B) {
+    const int b = block;
+    if (b < to.B && parent[b] == b) return;
     const int whole = pages_length(from, b) >> shift;
-    __syncthreads();
-    if (threadIdx.x == 0) to.lengths[b] = 0;
     for (int i = threadIdx.x; i < whole; i += 256) atomicSub(&to.references[page_entry(from, b, i)], 1);
     return;
   }
-  if (b < to.B) {
-    const int s = parent_of(from, parent, b);
-    if (s < 0 || s == b) return;
-    const int whole = pages_length(from, s) >> shift;
-    for (int i = threadIdx.x; i < whole; i += 256) atomicAdd(&to.references[page_entry(from, s, i)], 1);
-    return;
+  block -= from.B;
+  const bool keys = (block & 1) == 0;
+  const unsigned unit = block / 2;
+  const int b = unit / from.Hkv, h = unit % from.Hkv;
+  if (b >= to.B) return;
+  const int s = parent_of(from, parent, b);
+  if (s < 0) return;
+  const int chunks = (pages_length(from, s) & (from.page - 1)) * (row_bytes / 16);
+  const char* x = static_cast<const char*>(keys ? from.k_tail : from.v_tail) + ((size_t)s * from.Hkv + h) * from.page * row_bytes;
+  char* y = static_cast<char*>(keys ? to.k_tail : to.v_tail) + (size_t)unit * to.page * row_bytes;
+  constexpr int BATCH = 4;
+  for (int i = threadIdx.x; i < chunks; i += 256 * BATCH) {
+    uint4 u[BATCH];
+#pragma unroll
+    for (int e = 0; e < BATCH; ++e) u[e] = load16(x + (size_t)min(i + e * 256, chunks - 1) * 16);
+#pragma unroll
+    for (int e = 0; e < BATCH; ++e)
+      if (i + e * 256 < chunks) store16(y + (size_t)(i + e * 256) * 16, u[e]);
   }
-  b -= to.B;
-  if (b >= from.B || (b < to.B && parent[b] == b)) return;
-  const int whole = pages_length(from, b) >> shift;
-  for (int i = threadIdx.x; i < whole; i += 256) atomicSub(&to.references[page_entry(from, b, i)], 1);
+}
+
+// In place: those that leave.
+__global__ __launch_bounds__(256) void pages_leave_kernel(const wave_pages p, const int32_t* parent) {
+  const unsigned b = workgroup_number();
+  if (b >= (unsigned)p.B || parent[b] == (int)b) return;
+  const int whole = pages_length(p, b) >> page_shift(p.page);
+  __syncthreads();
+  if (threadIdx.x == 0) p.lengths[b] = 0;
+  for (int i = threadIdx.x; i < whole; i += 256) atomicSub(&p.references[page_entry(p, b, i)], 1);
 }
 
 }  // namespace
@@ -687,14 +685,14 @@ wave_status launch_pages_read(const wave_pages& p, const int32_t* first, int n, 
 }
 
 wave_status launch_pages_reorder(const wave_pages& from, const wave_pages& to, const int32_t* parent, hipStream_t st) {
-  const bool apart = to.lengths != from.lengths;
-  if (apart) {
-    const long long tails = (long long)to.B * to.Hkv * 2;
-    const int row = from.d * (from.dtype == WAVE_BF16 ? 2 : 4);
-    WAVE_LAUNCH("pages_copy", pages_copy_kernel, grid_rows(tails + to.B + ((long long)from.n_pages + 255) / 256), 256, 0, st, from, to,
-                parent, row, (unsigned)tails);
+  if (to.lengths == from.lengths) {
+    WAVE_LAUNCH("pages_leave", pages_leave_kernel, grid_rows(from.B), 256, 0, st, from, parent);
+  } else {
+    WAVE_LAUNCH("pages_references", pages_references_kernel, grid_rows(((long long)from.n_pages + 255) / 256), 256, 0, st,
+                from.references, to.references, from.n_pages);
+    WAVE_LAUNCH("pages_copy", pages_copy_kernel, grid_rows((long long)to.B + from.B + (long long)to.B * to.Hkv * 2), 256, 0, st, from, to,
+                parent, from.d * (from.dtype == WAVE_BF16 ? 2 : 4));
   }
-  WAVE_LAUNCH("pages_count", pages_count_kernel, grid_rows(apart ? (long long)to.B + from.B : from.B), 256, 0, st, from, to, parent, apart);
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }
 
