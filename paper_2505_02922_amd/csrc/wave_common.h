@@ -46,6 +46,10 @@ __device__ __forceinline__ uint2 load8_stream(const void* p) {
   return make_uint2(v.x, v.y);
 }
 __device__ __forceinline__ void store16(void* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
+__device__ __forceinline__ void store16_stream(void* p, uint4 v) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+}
 
 template <typename T>
 __device__ __forceinline__ void unpack(const uint4& v, float (&f)[Elem<T>::EPC]);
@@ -410,6 +414,7 @@ struct NormArgs {
   int B, Hq, Hk, N;                 // (a tensor that is not there has no heads)
   float eps;
   bool turns;
+  bool past;                        // outputs pass by the caches, which could not hold them (set by the launch)
 };
 wave_status launch_norm_rotary(const NormArgs& a, const RotaryArgs& rot, int dtype, int d, hipStream_t st);
 struct PagesAppendArgs {

@@ -108,31 +108,35 @@ __device__ __forceinline__ const char* row_of(const HeadRows& r, int b, int h, i
   return r.data + (b * r.b + h * r.h + n * r.n);
 }
 
-// The heads of a token are its q and then its k heads.  count: tokens that there are; position(axis, n).
-template <typename T, int D, typename Position>
+// Outputs of more than the eight L2s hold (32 MB) pass by the caches, as every input does, which is read once (40 heads of 32762 tokens,
+// 671 MB: 135 us, 144 otherwise; 126 and 135 from dense rows; 5 TB/s, what a copy reaches).
+constexpr size_t PAST_BYTES = size_t(32) << 20;
+
+// The heads of a token are its q and then its k heads.  count(): tokens that there are; position(axis, n).
+template <typename T, int D, typename Count, typename Position>
 __device__ __forceinline__ void norm_heads(const NormArgs& a, const RotaryArgs& rot, const TurnShape& sh, int b, int tile, int group,
-                                           int count, Position&& position) {
+                                           Count&& count, Position&& position) {
   typedef NormTurn<T, D> Tu;
   constexpr size_t ROW = D * sizeof(T);
   const int item = threadIdx.x % Tu::ITEMS, lane = (threadIdx.x / Tu::ITEMS) & ((1 << sh.lane_shift) - 1);
   const int n = tile * sh.tokens + (int)(threadIdx.x / Tu::ITEMS >> sh.lane_shift);
-  if (n >= count) return;
   Tu t;
   t.place(rot, a.turns, item);
-  const int slots = a.Hq + a.Hk, step = sh.head_groups << sh.lane_shift;
+  const int row_n = min(n, a.N - 1), slots = a.Hq + a.Hk, step = sh.head_groups << sh.lane_shift;
   uint4 u[TURN_BATCH], v[TURN_BATCH];
   auto load = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < TURN_BATCH; ++i) {
       const int h = min(h0 + i * step, slots - 1);
-      const char* row = h < a.Hq ? row_of(a.q, b, h, n) : row_of(a.k, b, h - a.Hq, n);
-      u[i] = load16(row + t.one * 16);
-      v[i] = load16(row + t.two * 16);
+      const char* row = h < a.Hq ? row_of(a.q, b, h, row_n) : row_of(a.k, b, h - a.Hq, row_n);
+      u[i] = load16_stream(row + t.one * 16);
+      v[i] = load16_stream(row + t.two * 16);
     }
   };
-  // the first rows are on their way while the sines are formed
+  // the first rows are on their way while the count is read and the sines are formed
   int h0 = (group << sh.lane_shift) + lane;
   load(h0);
+  if (n >= count()) return;
   const typename Tu::Weight wq = t.weight(a.q_weight), wk = t.weight(a.k_weight);
   if (a.turns) t.angles(rot, item, [&](int axis) { return position(axis, n); });
   for (; h0 < slots;) {
@@ -145,8 +149,13 @@ __device__ __forceinline__ void norm_heads(const NormArgs& a, const RotaryArgs& 
         if (is_q) w = wq;
         t.apply(rot, w, a.eps, u[i], v[i]);
         char* row = is_q ? a.q_out + (((size_t)b * a.Hq + h) * a.N + n) * ROW : a.k_out + (((size_t)b * a.Hk + h - a.Hq) * a.N + n) * ROW;
-        store16(row + t.one * 16, u[i]);
-        store16(row + t.two * 16, v[i]);
+        if (a.past) {
+          store16_stream(row + t.one * 16, u[i]);
+          store16_stream(row + t.two * 16, v[i]);
+        } else {
+          store16(row + t.one * 16, u[i]);
+          store16(row + t.two * 16, v[i]);
+        }
       }
     }
     h0 += TURN_BATCH * step;
@@ -160,13 +169,14 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(const NormArgs a, cons
   const int group = block % sh.head_groups, bt = block / sh.head_groups;
   const int b = bt / tiles, tile = bt % tiles;
   if (b >= a.B) return;
-  norm_heads<T, D>(a, rot, sh, b, tile, group, a.N,
+  norm_heads<T, D>(a, rot, sh, b, tile, group, [&]() { return a.N; },
                    [&](int axis, int n) { return a.coords[((size_t)axis * a.B + b) * a.N + n]; });
 }
 
 template <typename T, int D>
-wave_status norm_rotary_td(const NormArgs& a, const RotaryArgs& rot, hipStream_t st) {
+wave_status norm_rotary_td(NormArgs a, const RotaryArgs& rot, hipStream_t st) {
   constexpr int ITEMS = Turn<T, D>::ITEMS;
+  a.past = (size_t)a.B * (a.Hq + a.Hk) * a.N * D * sizeof(T) > PAST_BYTES;
   const TurnShape sh = turn_shape<ITEMS>(a.N, a.B, a.Hq + a.Hk);
   const int tiles = (a.N + sh.tokens - 1) / sh.tokens;
   WAVE_LAUNCH("norm_rotary", (norm_rotary_kernel<T, D>), grid_rows((long long)a.B * tiles * sh.head_groups), 256, 0, st, a, rot, sh,
@@ -318,8 +328,9 @@ struct PageRows {
   static constexpr int EPC = Tu::EPC, ITEMS = Tu::ITEMS, SIDE = 256 / ITEMS;  // rows side by side
   static constexpr int PASSES = PAGE > SIDE ? PAGE / SIDE : 1;
   static constexpr size_t ROW = D * sizeof(T);
+  static constexpr bool AHEAD = PASSES <= 2;  // (more would take too many registers)
 
-  // One page of sequence b, heads first .. in steps of `step`.  alone: the workgroup writes the tail that it has read from.
+  // One page of sequence b, heads first .. in steps of `step`.
   static __device__ __forceinline__ void run(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
                                              const PagesPlan& plan, const int4 s, int b, int u, bool keys, int first, int step,
                                              uint32_t (*top)[4]) {
@@ -330,28 +341,27 @@ struct PageRows {
     char* to_tail = static_cast<char*>(keys ? to.k_tail : to.v_tail);
     const HeadRows& rows = keys ? a.k_new : a.v_new;
     Tu t[PASSES];
-    uint4 x[PASSES], y[PASSES];
-    auto load = [&](int h) {
+    uint4 x[PASSES], y[PASSES];  // this head's rows
+    // A lane's rows; lanes behind the page's last one have that one again.
+    auto row = [&](int i) { return min(row0 + i * SIDE, PAGE - 1); };
+    // (a load under a condition of the lanes would be waited for where it is; rows that are not there load the last one)
+    auto load = [&](int h, uint4 (&u)[PASSES], uint4 (&v)[PASSES]) {
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
-        const int r = row0 + i * SIDE, at = start + r;
-        if (r < PAGE && at < end) {
-          const char* p = at < s.x ? tail + (((size_t)b * from.Hkv + h) * PAGE + r) * ROW : row_of(rows, b, h, at - s.x);
-          x[i] = load16(p + t[i].one * 16);
-          y[i] = load16(p + t[i].two * 16);
-        } else {
-          x[i] = y[i] = make_uint4(0, 0, 0, 0);
-        }
+        const int at = min(start + row(i), end - 1);
+        const char* p = at < s.x ? tail + (((size_t)b * from.Hkv + h) * PAGE + (at - start)) * ROW : row_of(rows, b, h, at - s.x);
+        u[i] = load16_stream(p + t[i].one * 16);
+        v[i] = load16_stream(p + t[i].two * 16);
       }
     };
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) t[i].place(rot, turns, item);
-    load(first);
-    typename Tu::Weight w = t[0].weight(keys ? a.rows.k_weight : nullptr);
+    load(first, x, y);
+    const typename Tu::Weight w = t[0].weight(keys ? a.rows.k_weight : nullptr);
     if (turns) {
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
-        const int at = start + row0 + i * SIDE, n = at - s.x;
+        const int at = start + row(i), n = at - s.x;
         if (n >= 0 && at < end)
           t[i].angles(rot, item, [&](int axis) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : at; });
       }
@@ -360,9 +370,25 @@ struct PageRows {
     if (complete && keys && first == 0 && tid == 0) to.table[(size_t)b * to.max_pages + whole + u] = page;
     int turn = 0;
     for (int h = first; h < from.Hkv; h += step, turn ^= 1) {
+      // the next head's rows are on their way
+      uint4 next_x[PASSES], next_y[PASSES];
+      const bool more = h + step < from.Hkv;
+      if (AHEAD && more) load(h + step, next_x, next_y);
+      auto advance = [&]() {
+        if (!more) return;
+        if (AHEAD) {
+#pragma unroll
+          for (int i = 0; i < PASSES; ++i) {
+            x[i] = next_x[i];
+            y[i] = next_y[i];
+          }
+        } else {
+          load(h + step, x, y);
+        }
+      };
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
-        const int at = start + row0 + i * SIDE;
+        const int at = start + row(i);
         if (at >= s.x && at < end) t[i].apply(rot, w, a.rows.eps, x[i], y[i]);
       }
       if (!complete) {
@@ -375,7 +401,7 @@ struct PageRows {
             store16(p + t[i].two * 16, y[i]);
           }
         }
-        if (h + step < from.Hkv) load(h + step);
+        advance();
         continue;
       }
       // magnitudes order like integers, what is no number above infinity
@@ -431,7 +457,7 @@ struct PageRows {
           }
         }
       }
-      if (h + step < from.Hkv) load(h + step);
+      advance();
     }
   }
 };
@@ -462,10 +488,13 @@ __global__ __launch_bounds__(256) void pages_append_kernel(const wave_pages from
   if (block < grid.q_blocks) {
     const int group = block % grid.sh.head_groups, bt = block / grid.sh.head_groups;
     const int b = bt / grid.tiles, tile = bt % grid.tiles;
-    const int4 s = plan.sequence[b];
-    norm_heads<T, D>(a.rows, rot, grid.sh, b, tile, group, s.w, [&](int axis, int n) {
-      return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : s.x + n;
-    });
+    int4 s;
+    norm_heads<T, D>(a.rows, rot, grid.sh, b, tile, group,
+                     [&]() {
+                       s = plan.sequence[b];
+                       return s.w;
+                     },
+                     [&](int axis, int n) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : s.x + n; });
     return;
   }
   block -= grid.q_blocks;
@@ -486,8 +515,9 @@ __global__ __launch_bounds__(256) void pages_append_kernel(const wave_pages from
 }
 
 template <typename T, int D, int PAGE>
-wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
+wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, PagesAppendArgs a, const RotaryArgs& rot,
                              const PagesPlan& plan, hipStream_t st) {
+  a.rows.past = (size_t)from.B * a.rows.Hq * a.n * D * sizeof(T) > PAST_BYTES;
   WAVE_LAUNCH("pages_plan", pages_plan_kernel, 1, PLAN_THREADS, 0, st, from, to, a.counts, a.n, plan, a.apart);
   AppendGrid g{};
   g.units = a.n == 1 ? 1 : (int)(((long long)PAGE - 2 + a.n) / PAGE) + 1;

@@ -206,8 +206,10 @@ __device__ __forceinline__ void stream_unit(const PagesAttendArgs& p, int b, int
   }
 }
 
+// One workgroup per piece of a sequence and KV head.  As many a CU as there are registers for: at d = 128 in bf16 three (168) leave
+// 66.3 us of 70.7 with two (64 sequences of 700 .. 4351 rows on eight KV heads); fp32's three numbers a query need two's.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void pages_rows_kernel(const PagesAttendArgs p) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : sizeof(T) == 2 ? 3 : 2) void pages_rows_kernel(const PagesAttendArgs p) {
   __shared__ JoinShared js;
   __shared__ __attribute__((aligned(16))) char lds[4][16 * (D + 4) * 4];
   const Areas areas{lds[0], lds[1], lds[2], lds[3]};
@@ -294,9 +296,13 @@ PagesAttendGeom pages_attend_geometry(const wave_pages& p, int Hq) {
   const long long room = (long long)p.max_pages * p.page + p.page - 1;
   const long long steps = (room + SHORT_WAVES * 32 - 1) / (SHORT_WAVES * 32);
   g.one_launch = steps <= 1 || (steps <= 2 && ((long long)p.B * p.Hkv <= 256 || p.B > 512));
-  const int per_cu = 2;
-  g.target = per_cu * 256 / p.Hkv > 1 ? per_cu * 256 / p.Hkv : 1;
-  g.few = g.target / 2;
+  // Two pieces a CU, and one where they are short.  Three for many sequences that can still be cut alike, since each then has few:
+  // 64 sequences of 700 .. 4351 rows on four KV heads that begin with the same 640 38.4 us, with three 34.4; 32 of 2000 .. 8000 on eight
+  // 64.2 and 62.7.  (64 on eight, in proportion, 66.3 and 69.9; 8 of 3001 .. 65536 95 and 97.6; four or six a CU, in turns,
+  // 95 and 102; one of 32000 with one and a half 21.6 for 19.1.)
+  const auto pieces = [&](int per_cu) { return per_cu * 256 / p.Hkv > 1 ? per_cu * 256 / p.Hkv : 1; };
+  g.target = pieces(p.B >= 32 && cuts_fit(p.B, pieces(3)) ? 3 : 2);
+  g.few = pieces(1);
   const long long most = (long long)p.B * ((room + 127) / 128), cut = (long long)g.target + (cuts_fit(p.B, g.target) ? 0 : p.B);
   g.pieces = (int)(cut < most ? cut : most);
   size_t o = 0;
