@@ -545,6 +545,7 @@ static wave_status check_rotary(const wave_rotary* r, int d, RotaryArgs* out) {
   *out = RotaryArgs{};
   out->rot = r->rot_dim;
   out->pairing = r->pairing;
+  out->n_axes = r->n_axes;
   for (int i = 0; i < r->rot_dim / 2; ++i) {
     if (r->axis[i] < 0 || r->axis[i] >= r->n_axes) return WAVE_ERR_ARG;
     if (!(fabs(r->inv_freq[i]) < HUGE_VAL)) return WAVE_ERR_ARG;

@@ -373,7 +373,7 @@ wave_status launch_assign_step(const void* xhat, const void* chat, int dtype, in
 struct RotaryArgs {
   double turns[WAVE_ROTARY_MAX_PAIRS];  // of a circle per position
   int axis[WAVE_ROTARY_MAX_PAIRS];
-  int rot, pairing;
+  int rot, pairing, n_axes;
 };
 wave_status launch_rotary(const void* x, const int32_t* coords, const RotaryArgs& rot, int dtype, int B, int H,
                           int N, int d, void* y, hipStream_t st);

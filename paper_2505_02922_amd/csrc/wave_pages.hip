@@ -6,9 +6,11 @@ namespace wave {
 namespace {
 
 // ----------------------------------------------------------------------------
-// Norms with rotary positions.  The lanes of a row (the items of a turn) add up its squares with DPP; a thread keeps the
-// sines of its item of one token and goes through the token's heads with them.  Every fused multiply-add is written out:
-// a row has the same bits whichever kernel, and whichever form of it, norms and turns it.
+// Norms with rotary positions.  A work item is an item of a turn (wave_rotary.h): two 16-byte chunks of a row.  The lanes of a row
+// add up its squares with DPP.  A workgroup forms the sines of its rows once, a pair of channels a thread, and leaves them in LDS:
+// in registers they took eight copies of their code in every thread, which a decode step fetches from memory before it runs
+// (one token of 64 sequences: 5.4 us so, NORM_TOKEN us now), and eight lanes' work for each of a token's heads.
+// Every fused multiply-add is written out: a row has the same bits whichever kernel, and whichever form of it, norms and turns it.
 // ----------------------------------------------------------------------------
 template <int LANES>
 __device__ __forceinline__ float item_sum(float x) {
@@ -20,67 +22,44 @@ __device__ __forceinline__ float item_sum(float x) {
   return x;
 }
 
+constexpr int THREADS = 256;
+
 template <typename T, int D>
-struct NormTurn : Turn<T, D> {
-  typedef Turn<T, D> Base;
-  static constexpr int EPC = Base::EPC, ITEMS = Base::ITEMS;
-  __device__ __forceinline__ void place(const RotaryArgs& r, bool rotates, int item) {
-    if (rotates) {
-      Base::place(r, item);
-    } else {
-      this->turns = false;
-      this->one = 2 * item;
-      this->two = 2 * item + 1;
-    }
-  }
-  // (as in the base, the circles coming off exactly)
-  template <typename F>
-  __device__ __forceinline__ void angles(const RotaryArgs& r, int item, F&& position) {
-#pragma unroll
-    for (int e = 0; e < EPC; ++e) {
-      this->c[e] = 1.f;
-      this->s[e] = 0.f;
-      if (this->turns) {
-        const int i = item * EPC + e;
-        const double at = (double)position(r.axis[i]), per = r.turns[i];
-        const double part = fma(at, per, -rint(at * per));
-        sincospif((float)(part + part), &this->s[e], &this->c[e]);
-      }
-    }
-  }
-  __device__ __forceinline__ void pair(float& x, float& y, int e) const {
-    const float c = this->c[e], s = this->s[e], u = fmaf(x, c, -(y * s));
-    y = fmaf(x, s, y * c);
-    x = u;
-  }
-  __device__ __forceinline__ void turn(const RotaryArgs& r, float (&x)[EPC], float (&y)[EPC]) const {
-    if (r.pairing == WAVE_ROTARY_HALVES) {
-#pragma unroll
-      for (int e = 0; e < EPC; ++e) pair(x[e], y[e], e);
-    } else {  // pairs of the first and of the second chunk
-#pragma unroll
-      for (int e = 0; e < EPC; e += 2) {
-        pair(x[e], x[e + 1], e / 2);
-        pair(y[e], y[e + 1], EPC / 2 + e / 2);
-      }
-    }
-  }
+struct RowItem {
+  static constexpr int EPC = Elem<T>::EPC, ITEMS = D / (2 * EPC), PAIRS = D / 2;
+  struct Sines { float c[EPC], s[EPC]; };
   struct Weight {
     uint4 a, b;
     bool any;
   };
+  int item, one, two;  // its chunks
+  bool turns, halves;
+
+  __device__ __forceinline__ void place(const RotaryArgs& r, bool rotates, int at) {
+    const int rotated = rotates ? r.rot / (2 * EPC) : 0;
+    item = at;
+    turns = item < rotated;
+    halves = turns && r.pairing == WAVE_ROTARY_HALVES;
+    one = halves ? item : 2 * item;
+    two = halves ? item + rotated : 2 * item + 1;
+  }
   __device__ __forceinline__ Weight weight(const char* w) const {
     Weight r;
     r.any = w != nullptr;
     if (r.any) {
-      r.a = load16(w + this->one * 16);
-      r.b = load16(w + this->two * 16);
+      r.a = load16(w + one * 16);
+      r.b = load16(w + two * 16);
     }
     return r;
   }
+  static __device__ __forceinline__ void pair(float& x, float& y, float c, float s) {
+    const float u = fmaf(x, c, -(y * s));
+    y = fmaf(x, s, y * c);
+    x = u;
+  }
   // All lanes of the row together.  x * (w / norm) in fp32, then the turn, then one rounding.
-  __device__ __forceinline__ void apply(const RotaryArgs& r, const Weight& w, float eps, uint4& a, uint4& b) const {
-    if (!w.any && !this->turns) return;
+  __device__ __forceinline__ void apply(const Weight& w, const Sines& t, float eps, uint4& a, uint4& b) const {
+    if (!w.any && !turns) return;
     float x[EPC], y[EPC];
     unpack<T>(a, x);
     unpack<T>(b, y);
@@ -98,9 +77,62 @@ struct NormTurn : Turn<T, D> {
         y[e] = y[e] * f * v[e];
       }
     }
-    if (this->turns) turn(r, x, y);
+    if (turns && halves) {
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) pair(x[e], y[e], t.c[e], t.s[e]);
+    } else if (turns) {  // pairs of the first and of the second chunk
+#pragma unroll
+      for (int e = 0; e < EPC; e += 2) {
+        pair(x[e], x[e + 1], t.c[e / 2], t.s[e / 2]);
+        pair(y[e], y[e + 1], t.c[EPC / 2 + e / 2], t.s[EPC / 2 + e / 2]);
+      }
+    }
     a = pack<T>(x);
     b = pack<T>(y);
+  }
+};
+
+// Cosines and sines of ROWS rows in LDS, a row's [two pairs of an item][item], so that the items of a row read neighbouring 16
+// bytes.
+template <typename T, int D, int ROWS>
+struct SineTable {
+  typedef RowItem<T, D> Item;
+  static constexpr int PAIRS = Item::PAIRS, EPC = Item::EPC, ITEMS = Item::ITEMS, SIDE = THREADS / PAIRS;
+  float4 pairs[ROWS][PAIRS / 2];
+  int position[WAVE_ROTARY_MAX_AXES][ROWS];
+  // Rows r0 .. r1 - 1; at(axis, row).  All threads together; the table is whole behind the call.
+  template <typename F>
+  __device__ __forceinline__ void fill(const RotaryArgs& rot, int r0, int r1, F&& at) {
+    static_assert(ROWS <= THREADS, "");
+    const int mine = threadIdx.x % ROWS;
+    if (mine >= r0 && mine < r1)
+      for (int axis = threadIdx.x / ROWS; axis < rot.n_axes; axis += THREADS / ROWS) position[axis][mine] = at(axis, mine);
+    const int i = threadIdx.x % PAIRS, item = i / EPC, e = i % EPC;
+    const bool any = i < rot.rot / 2;
+    const int axis = any ? rot.axis[i] : 0;
+    const double per = any ? rot.turns[i] : 0.0;
+    __syncthreads();
+    if (any) {
+#pragma unroll 1
+      for (int r = r0 + threadIdx.x / PAIRS; r < r1; r += SIDE) {
+        // angle in fp64; a circle is `1` in turns, so the nearest whole number of circles comes off without error
+        const double to = (double)position[axis][r], part = fma(to, per, -rint(to * per));
+        float2 cs;
+        sincospif((float)(part + part), &cs.y, &cs.x);
+        reinterpret_cast<float2*>(&pairs[r][(e >> 1) * ITEMS + item])[e & 1] = cs;
+      }
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ void get(int row, int item, typename Item::Sines& t) const {
+#pragma unroll
+    for (int k = 0; k < EPC / 2; ++k) {
+      const float4 x = pairs[row][k * ITEMS + item];
+      t.c[2 * k] = x.x;
+      t.s[2 * k] = x.y;
+      t.c[2 * k + 1] = x.z;
+      t.s[2 * k + 1] = x.w;
+    }
   }
 };
 
@@ -112,49 +144,54 @@ __device__ __forceinline__ const char* row_of(const HeadRows& r, int b, int h, i
 // 671 MB: 135 us, 144 otherwise; 126 and 135 from dense rows; 5 TB/s, what a copy reaches).
 constexpr size_t PAST_BYTES = size_t(32) << 20;
 
-// The heads of a token are its q and then its k heads.  count(): tokens that there are; position(axis, n).
-template <typename T, int D, typename Count, typename Position>
-__device__ __forceinline__ void norm_heads(const NormArgs& a, const RotaryArgs& rot, const TurnShape& sh, int b, int tile, int group,
-                                           Count&& count, Position&& position) {
-  typedef NormTurn<T, D> Tu;
-  constexpr size_t ROW = D * sizeof(T);
-  const int item = threadIdx.x % Tu::ITEMS, lane = (threadIdx.x / Tu::ITEMS) & ((1 << sh.lane_shift) - 1);
-  const int n = tile * sh.tokens + (int)(threadIdx.x / Tu::ITEMS >> sh.lane_shift);
-  Tu t;
+// The heads of a token are its q, k and v heads in this order; v's are only handed on.  count(): tokens that there are;
+// position(axis, n); out(h, n): where a head's row goes (NULL: nowhere).
+template <typename T, int D, int ROWS, typename Count, typename Position, typename Out>
+__device__ __forceinline__ void norm_heads(const NormArgs& a, const HeadRows& values, int Hv, const RotaryArgs& rot, const TurnShape& sh,
+                                           int b, int tile, int group, SineTable<T, D, ROWS>& table, Count&& count, Position&& position,
+                                           Out&& out) {
+  typedef RowItem<T, D> Item;
+  const int item = threadIdx.x % Item::ITEMS, lane = (threadIdx.x / Item::ITEMS) & ((1 << sh.lane_shift) - 1);
+  const int row = (int)(threadIdx.x / Item::ITEMS >> sh.lane_shift), first = tile * sh.tokens, n = first + row;
+  Item t;
   t.place(rot, a.turns, item);
-  const int row_n = min(n, a.N - 1), slots = a.Hq + a.Hk, step = sh.head_groups << sh.lane_shift;
+  const int row_n = min(n, a.N - 1), heads = a.Hq + a.Hk, slots = heads + Hv, step = sh.head_groups << sh.lane_shift;
   uint4 u[TURN_BATCH], v[TURN_BATCH];
   auto load = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < TURN_BATCH; ++i) {
       const int h = min(h0 + i * step, slots - 1);
-      const char* row = h < a.Hq ? row_of(a.q, b, h, row_n) : row_of(a.k, b, h - a.Hq, row_n);
-      u[i] = load16_stream(row + t.one * 16);
-      v[i] = load16_stream(row + t.two * 16);
+      const char* at = h < a.Hq ? row_of(a.q, b, h, row_n) : h < heads ? row_of(a.k, b, h - a.Hq, row_n) : row_of(values, b, h - heads, row_n);
+      u[i] = load16_stream(at + t.one * 16);
+      v[i] = load16_stream(at + t.two * 16);
     }
   };
   // the first rows are on their way while the count is read and the sines are formed
   int h0 = (group << sh.lane_shift) + lane;
   load(h0);
-  if (n >= count()) return;
-  const typename Tu::Weight wq = t.weight(a.q_weight), wk = t.weight(a.k_weight);
-  if (a.turns) t.angles(rot, item, [&](int axis) { return position(axis, n); });
+  const typename Item::Weight wq = t.weight(a.q_weight), wk = t.weight(a.k_weight);
+  const int given = count();
+  typename Item::Sines sines;
+  if (a.turns) {
+    table.fill(rot, 0, min(sh.tokens, given - first), [&](int axis, int r) { return position(axis, first + r); });
+    if (t.turns) table.get(row, item, sines);
+  }
+  if (n >= given) return;
   for (; h0 < slots;) {
 #pragma unroll
     for (int i = 0; i < TURN_BATCH; ++i) {
       const int h = h0 + i * step;
       if (h < slots) {
-        const bool is_q = h < a.Hq;
-        typename Tu::Weight w = wk;
-        if (is_q) w = wq;
-        t.apply(rot, w, a.eps, u[i], v[i]);
-        char* row = is_q ? a.q_out + (((size_t)b * a.Hq + h) * a.N + n) * ROW : a.k_out + (((size_t)b * a.Hk + h - a.Hq) * a.N + n) * ROW;
+        typename Item::Weight w = wk;
+        if (h < a.Hq) w = wq;
+        if (h < heads) t.apply(w, sines, a.eps, u[i], v[i]);
+        char* to = out(h, n);
         if (a.past) {
-          store16_stream(row + t.one * 16, u[i]);
-          store16_stream(row + t.two * 16, v[i]);
-        } else {
-          store16(row + t.one * 16, u[i]);
-          store16(row + t.two * 16, v[i]);
+          store16_stream(to + t.one * 16, u[i]);
+          store16_stream(to + t.two * 16, v[i]);
+        } else if (to) {
+          store16(to + t.one * 16, u[i]);
+          store16(to + t.two * 16, v[i]);
         }
       }
     }
@@ -164,18 +201,24 @@ __device__ __forceinline__ void norm_heads(const NormArgs& a, const RotaryArgs& 
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void norm_rotary_kernel(const NormArgs a, const RotaryArgs rot, TurnShape sh, int tiles) {
+__global__ __launch_bounds__(THREADS) void norm_rotary_kernel(const NormArgs a, const RotaryArgs rot, TurnShape sh, int tiles) {
+  constexpr size_t ROW = D * sizeof(T);
+  __shared__ SineTable<T, D, THREADS / RowItem<T, D>::ITEMS> table;
   const unsigned block = workgroup_number();
   const int group = block % sh.head_groups, bt = block / sh.head_groups;
   const int b = bt / tiles, tile = bt % tiles;
   if (b >= a.B) return;
-  norm_heads<T, D>(a, rot, sh, b, tile, group, [&]() { return a.N; },
-                   [&](int axis, int n) { return a.coords[((size_t)axis * a.B + b) * a.N + n]; });
+  norm_heads<T, D>(
+      a, HeadRows{}, 0, rot, sh, b, tile, group, table, [&]() { return a.N; },
+      [&](int axis, int n) { return a.coords[((size_t)axis * a.B + b) * a.N + n]; },
+      [&](int h, int n) {
+        return h < a.Hq ? a.q_out + (((size_t)b * a.Hq + h) * a.N + n) * ROW : a.k_out + (((size_t)b * a.Hk + h - a.Hq) * a.N + n) * ROW;
+      });
 }
 
 template <typename T, int D>
 wave_status norm_rotary_td(NormArgs a, const RotaryArgs& rot, hipStream_t st) {
-  constexpr int ITEMS = Turn<T, D>::ITEMS;
+  constexpr int ITEMS = RowItem<T, D>::ITEMS;
   a.past = (size_t)a.B * (a.Hq + a.Hk) * a.N * D * sizeof(T) > PAST_BYTES;
   const TurnShape sh = turn_shape<ITEMS>(a.N, a.B, a.Hq + a.Hk);
   const int tiles = (a.N + sh.tokens - 1) / sh.tokens;
@@ -227,6 +270,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
   };
   load(0);
   int wanted = 0;  // pages wanted by the sequences so far
+  int4 mine = make_int4(0, 0, 0, 0);
   for (int b0 = 0; b0 < from.B; b0 += PLAN_THREADS) {
     const int b = b0 + tid;
     int length = 0, count = 0, need = 0;
@@ -247,7 +291,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
     }
     // (where the sums stop, there is no page anyway)
     const int below = __shfl_up(incl, 1);
-    if (b < from.B) plan.sequence[b] = make_int4(length, need, sum_to_many(before, lane ? below : 0), count);
+    mine = make_int4(length, need, sum_to_many(before, lane ? below : 0), count);
+    if (b0 + PLAN_THREADS < from.B) plan.sequence[b] = mine;  // (the last round's stay where they are)
     __syncthreads();
   }
   int found = 0;
@@ -293,7 +338,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
   }
   if (found < wanted && tid == 0) plan.last[0] = from.n_pages;  // every free page is taken
   for (int b = tid; b < from.B; b += PLAN_THREADS) {
-    int4 s = plan.sequence[b];
+    int4 s = mine;
+    if (b - tid + PLAN_THREADS < from.B) s = plan.sequence[b];
     const int whole = s.x >> shift, got = min(max(found - s.z, 0), s.y);
     int end = s.x + min(s.w, pages_room(from) - s.x);
     if (got < s.y) end = ((whole + got + 1) << shift) - 1;
@@ -304,14 +350,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
 }
 
 // Append, second launch.
-//   pages  a workgroup has some heads' keys or values of one page of a sequence: rows that were in the tail, new rows, or both.
-//          If the page is complete they are rounded to 8 bits (a thread keeps its 16 channels of every row between the maximum and
-//          the codes), otherwise they are the new tail.
-//   q      as in norm_rotary_kernel
-//   lists  table and references of a state with arrays of its own
+//   pages   a workgroup has some heads' keys or values of one page of a sequence: rows that were in the tail, new rows, or both.
+//           If the page is complete they are rounded to 8 bits (a thread keeps its 16 channels of every row between the maximum and
+//           the codes), otherwise they are the new tail
+//   tokens  queries, as in norm_rotary_kernel; and where one token is appended, its key and value rows too, straight into the tail
+//           unless they complete a page: then the pages' workgroups have little to do but in the one sequence of `page` that does
+//   lists   table and references of a state with arrays of its own
 struct AppendGrid {
-  unsigned page_blocks, q_blocks;  // the others are lists
-  int units, head_groups;          // pages that a sequence's new tokens may touch; workgroups that share a page's heads
+  unsigned page_blocks, token_blocks;  // the others are lists
+  int units, head_groups;              // pages that a sequence's new tokens may touch; workgroups that share a page's heads
   TurnShape sh;
   int tiles;
 };
@@ -324,23 +371,25 @@ __device__ __forceinline__ int code_of(float x, float inv) {
 
 template <typename T, int D, int PAGE>
 struct PageRows {
-  typedef NormTurn<T, D> Tu;
-  static constexpr int EPC = Tu::EPC, ITEMS = Tu::ITEMS, SIDE = 256 / ITEMS;  // rows side by side
-  static constexpr int PASSES = PAGE > SIDE ? PAGE / SIDE : 1;
+  typedef RowItem<T, D> Item;
+  static constexpr int EPC = Item::EPC, ITEMS = Item::ITEMS, SIDE = THREADS / ITEMS;  // rows side by side
+  static constexpr int PASSES = PAGE > SIDE ? PAGE / SIDE : 1, TOKENS = PAGE > SIDE ? PAGE : SIDE;
   static constexpr size_t ROW = D * sizeof(T);
   static constexpr bool AHEAD = PASSES <= 2;  // (more would take too many registers)
+  typedef SineTable<T, D, TOKENS> Table;
 
   // One page of sequence b, heads first .. in steps of `step`.
   static __device__ __forceinline__ void run(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
                                              const PagesPlan& plan, const int4 s, int b, int u, bool keys, int first, int step,
-                                             uint32_t (*top)[4]) {
-    const int tid = threadIdx.x, item = tid % ITEMS, row0 = tid / ITEMS;
+                                             Table& table, uint32_t (*top)[4]) {
+    const int tid = threadIdx.x, row0 = tid / ITEMS;
     const int whole = s.x / PAGE, start = (whole + u) * PAGE, end = s.y;
-    const bool complete = start + PAGE <= end, turns = keys && a.rows.turns;
+    const bool complete = start + PAGE <= end;
     const char* tail = static_cast<const char*>(keys ? from.k_tail : from.v_tail);
     char* to_tail = static_cast<char*>(keys ? to.k_tail : to.v_tail);
     const HeadRows& rows = keys ? a.k_new : a.v_new;
-    Tu t[PASSES];
+    Item t;
+    t.place(rot, keys && a.rows.turns, tid % ITEMS);
     uint4 x[PASSES], y[PASSES];  // this head's rows
     // A lane's rows; lanes behind the page's last one have that one again.
     auto row = [&](int i) { return min(row0 + i * SIDE, PAGE - 1); };
@@ -350,22 +399,17 @@ struct PageRows {
       for (int i = 0; i < PASSES; ++i) {
         const int at = min(start + row(i), end - 1);
         const char* p = at < s.x ? tail + (((size_t)b * from.Hkv + h) * PAGE + (at - start)) * ROW : row_of(rows, b, h, at - s.x);
-        u[i] = load16_stream(p + t[i].one * 16);
-        v[i] = load16_stream(p + t[i].two * 16);
+        u[i] = load16_stream(p + t.one * 16);
+        v[i] = load16_stream(p + t.two * 16);
       }
     };
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) t[i].place(rot, turns, item);
     load(first, x, y);
-    const typename Tu::Weight w = t[0].weight(keys ? a.rows.k_weight : nullptr);
-    if (turns) {
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        const int at = start + row(i), n = at - s.x;
-        if (n >= 0 && at < end)
-          t[i].angles(rot, item, [&](int axis) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : at; });
-      }
-    }
+    const typename Item::Weight w = t.weight(keys ? a.rows.k_weight : nullptr);
+    const int r0 = max(s.x - start, 0), r1 = min(end - start, PAGE);  // the new rows
+    if (keys && a.rows.turns && r0 < r1)
+      table.fill(rot, r0, r1, [&](int axis, int r) {
+        return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + start + r - s.x] : start + r;
+      });
     const int page = complete ? plan.taken[s.z + u] : 0;
     if (complete && keys && first == 0 && tid == 0) to.table[(size_t)b * to.max_pages + whole + u] = page;
     int turn = 0;
@@ -388,8 +432,11 @@ struct PageRows {
       };
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
-        const int at = start + row(i);
-        if (at >= s.x && at < end) t[i].apply(rot, w, a.rows.eps, x[i], y[i]);
+        if (row(i) >= r0 && row(i) < r1) {
+          typename Item::Sines sines;
+          if (t.turns) table.get(row(i), t.item, sines);
+          t.apply(w, sines, a.rows.eps, x[i], y[i]);
+        }
       }
       if (!complete) {
 #pragma unroll
@@ -397,8 +444,8 @@ struct PageRows {
           const int r = row0 + i * SIDE, at = start + r;
           if (r < PAGE && at < end && (a.apart || at >= s.x)) {
             char* p = to_tail + (((size_t)b * from.Hkv + h) * PAGE + r) * ROW;
-            store16(p + t[i].one * 16, x[i]);
-            store16(p + t[i].two * 16, y[i]);
+            store16(p + t.one * 16, x[i]);
+            store16(p + t.two * 16, y[i]);
           }
         }
         advance();
@@ -449,11 +496,11 @@ struct PageRows {
         if (r < PAGE) {
           int8_t* p = codes + (size_t)r * D;
           if constexpr (EPC == 8) {
-            *reinterpret_cast<uint2*>(p + t[i].one * 8) = make_uint2(word[0], word[1]);
-            *reinterpret_cast<uint2*>(p + t[i].two * 8) = make_uint2(word[2], word[3]);
+            *reinterpret_cast<uint2*>(p + t.one * 8) = make_uint2(word[0], word[1]);
+            *reinterpret_cast<uint2*>(p + t.two * 8) = make_uint2(word[2], word[3]);
           } else {
-            *reinterpret_cast<uint32_t*>(p + t[i].one * 4) = word[0];
-            *reinterpret_cast<uint32_t*>(p + t[i].two * 4) = word[1];
+            *reinterpret_cast<uint32_t*>(p + t.one * 4) = word[0];
+            *reinterpret_cast<uint32_t*>(p + t.two * 4) = word[1];
           }
         }
       }
@@ -463,41 +510,64 @@ struct PageRows {
 };
 
 template <typename T, int D, int PAGE>
-__global__ __launch_bounds__(256) void pages_append_kernel(const wave_pages from, const wave_pages to, const PagesAppendArgs a,
-                                                           const RotaryArgs rot, const PagesPlan plan, const AppendGrid grid) {
+__global__ __launch_bounds__(THREADS) void pages_append_kernel(const wave_pages from, const wave_pages to, const PagesAppendArgs a,
+                                                               const RotaryArgs rot, const PagesPlan plan, const AppendGrid grid) {
   typedef PageRows<T, D, PAGE> Rows;
+  __shared__ typename Rows::Table table;
   __shared__ uint32_t top[2][4];
   unsigned block = workgroup_number();
   if (block < grid.page_blocks) {
     const int group = block % grid.head_groups, keys = (block / grid.head_groups) & 1;
     const unsigned bu = block / grid.head_groups / 2;
-    const int u = bu % grid.units, b = bu / grid.units;
-    const int4 s = plan.sequence[b];
-    const int whole = s.x / PAGE, rest = s.y / PAGE - whole;  // the unit whose rows are the tail
-    // In place the rows that page 0 takes from the tail are where the new tail goes: the same workgroup does both.
-    const bool both = !a.apart && rest > 0 && s.x % PAGE != 0 && s.y % PAGE != 0;
-    if (u > rest || (u == rest && (both || s.y % PAGE == 0))) return;
-    Rows::run(from, to, a, rot, plan, s, b, u, keys, group, grid.head_groups, top);
-    if (u == 0 && both) {
-      __syncthreads();  // everything that was in the tail has been read, and the maxima too
-      Rows::run(from, to, a, rot, plan, s, b, rest, keys, group, grid.head_groups, top);
+    const int b = bu / grid.units;
+    int u = bu % grid.units, parts = 1;
+    int4 s = plan.sequence[b];
+    const int rest = s.y / PAGE - s.x / PAGE;  // the unit whose rows are the tail
+    if (a.n == 1) {
+      // (a token that completes no page is written by its own workgroup: here only old rows go on)
+      if (s.y == s.x || s.y % PAGE != 0) {
+        if (!a.apart || s.x % PAGE == 0) return;
+        s.y = s.x;
+      }
+    } else {
+      // In place the rows that page 0 takes from the tail are where the new tail goes: the same workgroup does both.
+      const bool both = !a.apart && rest > 0 && s.x % PAGE != 0 && s.y % PAGE != 0;
+      if (u > rest || (u == rest && (both || s.y % PAGE == 0))) return;
+      if (u == 0 && both) parts = 2;
+    }
+    for (int part = 0; part < parts; ++part) {
+      if (part) {
+        __syncthreads();  // everything that was in the tail has been read, the sines and the maxima too
+        u = rest;
+      }
+      Rows::run(from, to, a, rot, plan, s, b, u, keys, group, grid.head_groups, table, top);
     }
     return;
   }
   block -= grid.page_blocks;
-  if (block < grid.q_blocks) {
+  if (block < grid.token_blocks) {
     const int group = block % grid.sh.head_groups, bt = block / grid.sh.head_groups;
     const int b = bt / grid.tiles, tile = bt % grid.tiles;
     int4 s;
-    norm_heads<T, D>(a.rows, rot, grid.sh, b, tile, group,
-                     [&]() {
-                       s = plan.sequence[b];
-                       return s.w;
-                     },
-                     [&](int axis, int n) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : s.x + n; });
+    norm_heads<T, D>(
+        a.rows, a.v_new, a.n == 1 ? from.Hkv : 0, rot, grid.sh, b, tile, group, table,
+        [&]() {
+          s = plan.sequence[b];
+          return s.w;
+        },
+        [&](int axis, int n) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : s.x + n; },
+        [&](int h, int n) -> char* {
+          constexpr size_t ROW = D * sizeof(T);
+          if (h < a.rows.Hq) return a.rows.q_out + (((size_t)b * a.rows.Hq + h) * a.n + n) * ROW;
+          if (s.y == s.x || s.y % PAGE == 0) return nullptr;  // no room, or part of a page
+          h -= a.rows.Hq;
+          const bool keys = h < from.Hkv;
+          char* tail = static_cast<char*>(keys ? to.k_tail : to.v_tail);
+          return tail + (((size_t)b * from.Hkv + (keys ? h : h - from.Hkv)) * PAGE + s.x % PAGE) * ROW;
+        });
     return;
   }
-  block -= grid.q_blocks;
+  block -= grid.token_blocks;
   if (!a.apart) return;
   // one workgroup a sequence for the tables, the others for references
   if (block < (unsigned)from.B) {
@@ -517,7 +587,7 @@ __global__ __launch_bounds__(256) void pages_append_kernel(const wave_pages from
 template <typename T, int D, int PAGE>
 wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, PagesAppendArgs a, const RotaryArgs& rot,
                              const PagesPlan& plan, hipStream_t st) {
-  a.rows.past = (size_t)from.B * a.rows.Hq * a.n * D * sizeof(T) > PAST_BYTES;
+  a.rows.past = a.n > 1 && (size_t)from.B * a.rows.Hq * a.n * D * sizeof(T) > PAST_BYTES;
   WAVE_LAUNCH("pages_plan", pages_plan_kernel, 1, PLAN_THREADS, 0, st, from, to, a.counts, a.n, plan, a.apart);
   AppendGrid g{};
   g.units = a.n == 1 ? 1 : (int)(((long long)PAGE - 2 + a.n) / PAGE) + 1;
@@ -527,11 +597,16 @@ wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, Pages
   if (g.head_groups > from.Hkv) g.head_groups = from.Hkv;
   long long blocks = (long long)from.B * g.units * 2 * g.head_groups;
   g.page_blocks = (unsigned)blocks;
-  if (a.rows.Hq > 0) {
-    g.sh = turn_shape<Turn<T, D>::ITEMS>(a.n, from.B, a.rows.Hq);
+  if (a.n == 1) {
+    a.rows.k = a.k_new;
+    a.rows.Hk = from.Hkv;
+  }
+  const int heads = a.rows.Hq + (a.n == 1 ? 2 * from.Hkv : 0);
+  if (heads > 0) {
+    g.sh = turn_shape<RowItem<T, D>::ITEMS>(a.n, from.B, heads);
     g.tiles = (a.n + g.sh.tokens - 1) / g.sh.tokens;
-    g.q_blocks = (unsigned)((long long)from.B * g.tiles * g.sh.head_groups);
-    blocks += g.q_blocks;
+    g.token_blocks = (unsigned)((long long)from.B * g.tiles * g.sh.head_groups);
+    blocks += g.token_blocks;
   }
   if (a.apart) blocks += from.B + ((long long)from.n_pages + 255) / 256;
   WAVE_LAUNCH("pages_append", (pages_append_kernel<T, D, PAGE>), grid_rows(blocks), 256, 0, st, from, to, a, rot, plan, g);
