@@ -257,16 +257,47 @@ PagesPlan pages_plan(const wave_pages& p, void* ws) {
 constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64, PLAN_PER = 16, PLAN_ROUND = PLAN_PER * PLAN_THREADS;
 constexpr int PLAN_MANY = (1 << 30) - 1;  // sums stop here: more pages than there can be
 __device__ __forceinline__ int sum_to_many(int a, int b) { return min(a + b, PLAN_MANY); }
+// What the threads before this one have, and all of them together, starting from `sum`; `sum` is then the whole.  Two barriers.
+__device__ __forceinline__ int plan_scan(int x, int& sum, int (&part)[PLAN_WAVES]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int incl = wave_scan(x, 0, sum_to_many), below = __shfl_up(incl, 1);
+  if (lane == 63) part[wave] = incl;
+  __syncthreads();
+  int before = sum;
+#pragma unroll
+  for (int w = 0; w < PLAN_WAVES; ++w) {
+    if (w == wave) before = sum;
+    sum = sum_to_many(sum, part[w]);
+  }
+  __syncthreads();
+  return sum_to_many(before, lane ? below : 0);
+}
 
 __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pages from, const wave_pages to, const int32_t* counts, int n,
                                                                  const PagesPlan plan, bool apart) {
-  __shared__ int part[PLAN_WAVES], place[PLAN_PER * PLAN_WAVES + 1];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, shift = page_shift(from.page);
-  // the first round's references are on their way while the lengths are looked at
-  int ref[PLAN_PER];
+  typedef __attribute__((ext_vector_type(4), aligned(4))) int int4_of_ints;
+  __shared__ int part[PLAN_WAVES];
+  const int tid = threadIdx.x, shift = page_shift(from.page);
+  // A thread has sixteen pages side by side.
+  int4_of_ints ref[PLAN_PER / 4];
   auto load = [&](int r0) {
+    const int first = r0 + tid * PLAN_PER;
+    if (first + PLAN_PER <= from.n_pages) {
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) ref[i] = from.references[min(r0 + i * PLAN_THREADS + tid, from.n_pages - 1)];
+      for (int i = 0; i < PLAN_PER / 4; ++i) ref[i] = *reinterpret_cast<const int4_of_ints*>(from.references + first + i * 4);
+    } else {  // the last ones: pages that there are not count as taken
+#pragma unroll
+      for (int i = 0; i < PLAN_PER; ++i) {
+        const int r = from.references[min(first + i, from.n_pages - 1)];
+        ref[i / 4][i % 4] = first + i < from.n_pages ? r : 1;
+      }
+    }
+  };
+  auto free_pages = [&]() {
+    uint32_t free = 0;
+#pragma unroll
+    for (int i = 0; i < PLAN_PER; ++i) free |= (uint32_t)(ref[i / 4][i % 4] <= 0) << i;
+    return free;
   };
   load(0);
   int wanted = 0;  // pages wanted by the sequences so far
@@ -280,61 +311,23 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
       const int fit = min(count, pages_room(from) - length);
       need = ((length + fit) >> shift) - (length >> shift);
     }
-    const int incl = wave_scan(need, 0, sum_to_many);
-    if (lane == 63) part[wave] = incl;
-    __syncthreads();
-    int before = wanted;
-#pragma unroll
-    for (int w = 0; w < PLAN_WAVES; ++w) {
-      if (w == wave) before = wanted;
-      wanted = sum_to_many(wanted, part[w]);
-    }
     // (where the sums stop, there is no page anyway)
-    const int below = __shfl_up(incl, 1);
-    mine = make_int4(length, need, sum_to_many(before, lane ? below : 0), count);
+    mine = make_int4(length, need, plan_scan(need, wanted, part), count);
     if (b0 + PLAN_THREADS < from.B) plan.sequence[b] = mine;  // (the last round's stay where they are)
-    __syncthreads();
   }
   int found = 0;
   if (tid == 0) plan.last[0] = -1;
   for (int r0 = 0; r0 < from.n_pages && found < wanted; r0 += PLAN_ROUND) {
-    uint64_t free[PLAN_PER];
-#pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
-      free[i] = __ballot(ref[i] <= 0 && r0 + i * PLAN_THREADS + tid < from.n_pages);
-      if (lane == 0) place[i * PLAN_WAVES + wave] = __popcll(free[i]);
-    }
-    __syncthreads();
+    uint32_t free = free_pages();
     if (r0 + PLAN_ROUND < from.n_pages) load(r0 + PLAN_ROUND);
-    if (wave == 0) {  // the sums before each of the 256 counts
-      int c[4], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c[i] = place[lane * 4 + i];
-        sum += c[i];
-      }
-      const int incl = wave_incl_scan(sum);
-      int at = incl - sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        place[lane * 4 + i] = at;
-        at += c[i];
-      }
-      if (lane == 63) place[PLAN_PER * PLAN_WAVES] = incl;
+    const int first = r0 + tid * PLAN_PER;
+    int rank = plan_scan(__popc(free), found, part);
+    for (; free && rank < wanted; free &= free - 1, ++rank) {
+      const int page = first + __ffs(free) - 1;
+      plan.taken[rank] = page;
+      if (!apart) to.references[page] = 1;
+      if (rank == wanted - 1) plan.last[0] = page;
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
-      const int rank = found + place[i * PLAN_WAVES + wave] + __popcll(free[i] & ((1ull << lane) - 1));
-      if ((free[i] >> lane & 1) && rank < wanted) {
-        const int page = r0 + i * PLAN_THREADS + tid;
-        plan.taken[rank] = page;
-        if (!apart) to.references[page] = 1;
-        if (rank == wanted - 1) plan.last[0] = page;
-      }
-    }
-    found += place[PLAN_PER * PLAN_WAVES];
-    __syncthreads();
   }
   if (found < wanted && tid == 0) plan.last[0] = from.n_pages;  // every free page is taken
   for (int b = tid; b < from.B; b += PLAN_THREADS) {
