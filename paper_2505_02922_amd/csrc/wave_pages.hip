@@ -638,7 +638,7 @@ __global__ __launch_bounds__(256) void pages_read_kernel(const wave_pages p, con
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int length = pages_length(p, b), whole = length >> shift << shift;
   const long long first = a.first ? a.first[b] : 0;
-  const long long at = (first >> 5 << 5) + (long long)tile * READ_TILE + wave * READ_CHUNK;  // the wave's first row
+  const long long at = (first & ~31ll) + (long long)tile * READ_TILE + wave * READ_CHUNK;  // the wave's first row
   const long long low = first > 0 ? first : 0, high = min(first + a.n, (long long)length);
   if (at + READ_CHUNK <= low || at >= high) return;
   const int c0 = (int)at, sub = lane / LANES, part = lane % LANES;
@@ -697,12 +697,58 @@ __global__ __launch_bounds__(256) void pages_references_kernel(const int32_t* fr
   if (i < n) to[i] = from[i];
 }
 
-// Into arrays of its own.  The first workgroups change references: one for each sequence of `to`, which leaves table and length
-// too, and one for each of `from`; a sequence that stays where it is changes nothing.  The others copy the tails, a head's keys
-// or values each, and take longer.
-__global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, int row_bytes) {
+// Into arrays of its own.
+//   counts  COUNT_PAGES pages' references: from's, and what `to` and `from` hold of them, counted in LDS by going through all
+//           tables.  Where these have more than COUNT_ENTRIES entries, references are copied by a launch before this one, and each
+//           sequence's workgroup adds to them (eight sequences: 2.8 us, in two launches 3.8 and the host's second call; 256 of 63
+//           entries, 32256 in all: the counting takes 40 us, two launches 27; 31 with the tails' keys copied in the first of them)
+//   tables  a sequence of `to`: its table, its length.  A sequence that stays where it is changes no reference
+//   leave   a sequence of `from`, where it takes its references away itself
+//   tails   a head's keys or values of a sequence
+constexpr int COUNT_PAGES = 4096, COUNT_SEQUENCES = 512, COUNT_ENTRIES = 4096;
+struct CopyGrid {
+  unsigned counts, leave;  // workgroups
+  int row_bytes;
+};
+
+__device__ __forceinline__ void count_references(const wave_pages& from, const wave_pages& to, const int32_t* parent, int p0) {
+  __shared__ int count[COUNT_PAGES], source[COUNT_SEQUENCES], held[COUNT_SEQUENCES];
+  const int pages = min(COUNT_PAGES, from.n_pages - p0), all = to.B + from.B, shift = page_shift(from.page);
+  for (int i = threadIdx.x; i < pages; i += 256) count[i] = from.references[p0 + i];
+  for (int i = threadIdx.x; i < all; i += 256) {
+    const int b = i < to.B ? i : i - to.B, p = b < to.B ? parent_of(from, parent, b) : -1, s = i < to.B ? p : b;
+    source[i] = max(s, 0);
+    held[i] = s < 0 || p == b ? 0 : pages_length(from, s) >> shift;
+  }
+  __syncthreads();
+  constexpr int BATCH = 8;
+  const int entries = all * from.max_pages;
+  for (int i0 = threadIdx.x; i0 < entries; i0 += 256 * BATCH) {
+    int page[BATCH], at[BATCH], column[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = min(i0 + k * 256, entries - 1);
+      at[k] = i / from.max_pages;
+      column[k] = i - at[k] * from.max_pages;
+      page[k] = page_entry(from, source[at[k]], column[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (i0 + k * 256 < entries && column[k] < held[at[k]] && page[k] >= p0 && page[k] < p0 + pages)
+        atomicAdd(&count[page[k] - p0], at[k] < to.B ? 1 : -1);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < pages; i += 256) to.references[p0 + i] = count[i];
+}
+
+__global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, const CopyGrid grid) {
   unsigned block = workgroup_number();
   const int shift = page_shift(from.page);
+  if (block < grid.counts) {
+    count_references(from, to, parent, block * COUNT_PAGES);
+    return;
+  }
+  block -= grid.counts;
   if (block < (unsigned)to.B) {
     const int b = block, s = parent_of(from, parent, b);
     const int length = s < 0 ? 0 : pages_length(from, s), whole = length >> shift;
@@ -710,28 +756,29 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, 
     for (int i = threadIdx.x; i < whole; i += 256) {
       const int entry = from.table[(size_t)s * from.max_pages + i];
       to.table[(size_t)b * to.max_pages + i] = entry;
-      if (s != b) atomicAdd(&to.references[min(max(entry, 0), from.n_pages - 1)], 1);
+      if (grid.counts == 0 && s != b) atomicAdd(&to.references[min(max(entry, 0), from.n_pages - 1)], 1);
     }
     return;
   }
   block -= to.B;
-  if (block < (unsigned)from.B) {
+  if (block < grid.leave) {
     const int b = block;
     if (b < to.B && parent[b] == b) return;
     const int whole = pages_length(from, b) >> shift;
     for (int i = threadIdx.x; i < whole; i += 256) atomicSub(&to.references[page_entry(from, b, i)], 1);
     return;
   }
-  block -= from.B;
+  block -= grid.leave;
   const bool keys = (block & 1) == 0;
   const unsigned unit = block / 2;
   const int b = unit / from.Hkv, h = unit % from.Hkv;
   if (b >= to.B) return;
   const int s = parent_of(from, parent, b);
   if (s < 0) return;
-  const int chunks = (pages_length(from, s) & (from.page - 1)) * (row_bytes / 16);
-  const char* x = static_cast<const char*>(keys ? from.k_tail : from.v_tail) + ((size_t)s * from.Hkv + h) * from.page * row_bytes;
-  char* y = static_cast<char*>(keys ? to.k_tail : to.v_tail) + (size_t)unit * to.page * row_bytes;
+  const int chunks = (pages_length(from, s) & (from.page - 1)) * (grid.row_bytes / 16);
+  const size_t page_bytes = (size_t)from.page * grid.row_bytes;
+  const char* x = static_cast<const char*>(keys ? from.k_tail : from.v_tail) + ((size_t)s * from.Hkv + h) * page_bytes;
+  char* y = static_cast<char*>(keys ? to.k_tail : to.v_tail) + unit * page_bytes;
   constexpr int BATCH = 4;
   for (int i = threadIdx.x; i < chunks; i += 256 * BATCH) {
     uint4 u[BATCH];
@@ -786,10 +833,18 @@ wave_status launch_pages_reorder(const wave_pages& from, const wave_pages& to, c
   if (to.lengths == from.lengths) {
     WAVE_LAUNCH("pages_leave", pages_leave_kernel, grid_rows(from.B), 256, 0, st, from, parent);
   } else {
-    WAVE_LAUNCH("pages_references", pages_references_kernel, grid_rows(((long long)from.n_pages + 255) / 256), 256, 0, st,
-                from.references, to.references, from.n_pages);
-    WAVE_LAUNCH("pages_copy", pages_copy_kernel, grid_rows((long long)to.B + from.B + (long long)to.B * to.Hkv * 2), 256, 0, st, from, to,
-                parent, from.d * (from.dtype == WAVE_BF16 ? 2 : 4));
+    CopyGrid g{};
+    g.row_bytes = from.d * (from.dtype == WAVE_BF16 ? 2 : 4);
+    const long long all = (long long)to.B + from.B;
+    if (all <= COUNT_SEQUENCES && all * from.max_pages <= COUNT_ENTRIES) {
+      g.counts = (unsigned)(((long long)from.n_pages + COUNT_PAGES - 1) / COUNT_PAGES);
+    } else {
+      g.leave = from.B;
+      WAVE_LAUNCH("pages_references", pages_references_kernel, grid_rows(((long long)from.n_pages + 255) / 256), 256, 0, st,
+                  from.references, to.references, from.n_pages);
+    }
+    WAVE_LAUNCH("pages_copy", pages_copy_kernel, grid_rows(g.counts + to.B + (long long)g.leave + (long long)to.B * to.Hkv * 2), 256, 0, st,
+                from, to, parent, g);
   }
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }

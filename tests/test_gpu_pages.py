@@ -659,6 +659,38 @@ def test_reorder_copies_forks_and_frees():
         assert plain.references == [held.count(p) for p in range(n_pages)]
 
 
+@pytest.mark.parametrize("B,to_B,most,n_pages", [(3, 5, 2, 4096), (40, 33, 56, 9000), (40, 33, 57, 9000), (200, 312, 8, 20000), (200, 313, 7, 20000),
+                                                 (1, 4000, 3, 5), (40, 33, 450, 9000)])
+def test_references_of_many_tables(B, to_B, most, n_pages):
+    """Tables of as many entries as one launch counts and of more, pages that many sequences share; against sums in numpy."""
+    rng = np.random.default_rng(B)
+    page = 32
+    pages, to = wb.alloc_pages(torch.float32, B, 1, 64, page, n_pages, most), None
+    table = rng.integers(0, n_pages, (B, most))
+    table[rng.random((B, most)) < 0.3] = 1
+    lengths = rng.integers(0, most * page + page, B)
+    parent = rng.integers(-2, B + 1, to_B)
+    stay = rng.random(to_B) < 0.2
+    parent[stay] = np.arange(to_B)[stay]
+    references = rng.integers(0, 50, n_pages)
+    pages.table.copy_(torch.from_numpy(table)), pages.lengths.copy_(torch.from_numpy(lengths)), pages.references.copy_(torch.from_numpy(references))
+    pages.k_tail.normal_(), pages.v_tail.normal_()
+    to = wb.alloc_pages(torch.float32, to_B, 1, 64, page, n_pages, most, pool=pages)
+    to.references.fill_(-9)
+    wb.wave_pages_reorder(pages, torch.from_numpy(parent).to(torch.int32).cuda(), to)
+    inside = (parent >= 0) & (parent < B)
+    source = np.where(inside, parent, 0)
+    new = np.where(inside, lengths[source], 0)
+    want = references.copy()
+    for rows, n, sign in ((table[source], new, 1), (table, lengths, -1)):
+        np.add.at(want, rows[np.arange(most)[None] < (n // page)[:, None]], sign)
+    assert np.array_equal(to.references.cpu().numpy(), want) and np.array_equal(to.lengths.cpu().numpy(), new)
+    got, tails = to.table.cpu().numpy(), to.k_tail.cpu()
+    for b in range(0, to_B, 1 + to_B // 50):
+        assert np.array_equal(got[b, :new[b] // page], table[source[b], :new[b] // page])
+        assert torch.equal(tails[b, :, :new[b] % page], pages.k_tail[int(source[b]), :, :new[b] % page].cpu())
+
+
 def test_reorder_identity_and_a_callers_own_reference():
     B, Hkv, d, page = 3, 1, 64, 32
     x = torch.randn(B, Hkv, 70, d, generator=_gen(12)).cuda()
