@@ -22,6 +22,12 @@ __device__ __forceinline__ float item_sum(float x) {
   return x;
 }
 
+// 1 / sqrt(x): the instruction's, which is off by a last place, and one step of Newton's iteration, unless that is infinite or zero.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float r = rsqrtf(x), better = fmaf(0.5f * r, fmaf(-x * r, r, 1.f), r);
+  return better == better ? better : r;
+}
+
 constexpr int THREADS = 256;
 
 template <typename T, int D>
@@ -64,10 +70,13 @@ struct RowItem {
     unpack<T>(a, x);
     unpack<T>(b, y);
     if (w.any) {
-      float sum = 0.f;
+      float sum_x = 0.f, sum_y = 0.f;
 #pragma unroll
-      for (int e = 0; e < EPC; ++e) sum = fmaf(y[e], y[e], fmaf(x[e], x[e], sum));
-      const float f = rsqrtf(fmaf(item_sum<ITEMS>(sum), 1.f / D, eps));
+      for (int e = 0; e < EPC; ++e) {
+        sum_x = fmaf(x[e], x[e], sum_x);
+        sum_y = fmaf(y[e], y[e], sum_y);
+      }
+      const float f = inverse_root(fmaf(item_sum<ITEMS>(sum_x + sum_y), 1.f / D, eps));
       float u[EPC], v[EPC];
       unpack<T>(w.a, u);
       unpack<T>(w.b, v);
@@ -92,6 +101,23 @@ struct RowItem {
   }
 };
 
+// Cosine (x) and sine (y) of `turns` circles, off by little more than half a last place: the angle is cut to an eighth of a
+// circle in fp64, where whole and quarter circles come off without error, and its series (x^9 and x^10 in the last terms, the next ones
+// are below 2^-28 of the sums) take it as two floats.  (A function of one float is off by pi u for the rounding of its argument, and
+// by its own last places: four times as many rows would then be rounded to bf16 the other way.)
+__device__ __forceinline__ float2 cosine_and_sine(double turns) {
+  const double part = turns - rint(turns), quarters = rint(part * 4.0), angle = fma(quarters, -0.25, part) * 6.283185307179586477;
+  const float x = (float)angle, rest = (float)(angle - (double)x), z = x * x, z_rest = fmaf(x, x, -z);
+  const float sine_terms = z * fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f);
+  const float sine = x + fmaf(x, sine_terms, rest);
+  const float near = fmaf(z, -0.5f, 1.f), lost = fmaf(z, -0.5f, 1.f - near);  // 1 - z / 2 and what its rounding left
+  const float cosine_terms = fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f);
+  const float cosine = near + fmaf(z * z, cosine_terms, fmaf(x, -rest, fmaf(z_rest, -0.5f, lost)));
+  const int q = (int)quarters;
+  const float c = q & 1 ? sine : cosine, s = q & 1 ? cosine : sine;
+  return make_float2((q + 1) & 2 ? -c : c, q & 2 ? -s : s);
+}
+
 // Cosines and sines of ROWS rows in LDS, a row's [two pairs of an item][item], so that the items of a row read neighbouring 16
 // bytes.
 template <typename T, int D, int ROWS>
@@ -115,11 +141,7 @@ struct SineTable {
     if (any) {
 #pragma unroll 1
       for (int r = r0 + threadIdx.x / PAIRS; r < r1; r += SIDE) {
-        // angle in fp64; a circle is `1` in turns, so the nearest whole number of circles comes off without error
-        const double to = (double)position[axis][r], part = fma(to, per, -rint(to * per));
-        float2 cs;
-        sincospif((float)(part + part), &cs.y, &cs.x);
-        reinterpret_cast<float2*>(&pairs[r][(e >> 1) * ITEMS + item])[e & 1] = cs;
+        reinterpret_cast<float2*>(&pairs[r][(e >> 1) * ITEMS + item])[e & 1] = cosine_and_sine((double)position[axis][r] * per);
       }
     }
     __syncthreads();
