@@ -57,7 +57,8 @@ struct Codes {
       for (int s = 0; s < CHUNKS; ++s) k.x[t][s] = load16(lds + (t * 16 + c) * ROW + ((s * 4 + g) ^ place(c)) * 16);
     return k;
   }
-  // rows: the step's first row of values; nobody else reads them
+  // rows: the step's first row of values.  Nobody else reads them, so they pass by the caches; but where a row is half a line (d = 64),
+  // two loads want it (16 sequences of 1000 .. 16000 rows: 30.8 us, past the caches 32.9)
   static __device__ __forceinline__ V load_v(const char* rows, int g, int c) {
     V v;
 #pragma unroll
@@ -69,7 +70,10 @@ struct Codes {
         v.x[j][1] = u.y;
       } else {
 #pragma unroll
-        for (int u = 0; u < WORDS; ++u) v.x[j][u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(at + u * 64 + c * 4));
+        for (int u = 0; u < WORDS; ++u) {
+          const uint32_t* word = reinterpret_cast<const uint32_t*>(at + u * 64 + c * 4);
+          v.x[j][u] = D == 64 ? *word : __builtin_nontemporal_load(word);
+        }
       }
     }
     return v;
@@ -294,8 +298,14 @@ wave_status pages_attend_td(const PagesAttendArgs& p, const PagesAttendGeom& g, 
 PagesAttendGeom pages_attend_geometry(const wave_pages& p, int Hq) {
   PagesAttendGeom g{};
   const long long room = (long long)p.max_pages * p.page + p.page - 1;
-  const long long steps = (room + SHORT_WAVES * 32 - 1) / (SHORT_WAVES * 32);
-  g.one_launch = steps <= 1 || (steps <= 2 && ((long long)p.B * p.Hkv <= 256 || p.B > 512));
+  // One launch where a wave has few steps to do and there are about as many units as CUs, so that its workgroups of eight waves fill
+  // them: up to two steps for up to 512 units, four from 128, eight from 256 on.  (In pieces and in one launch, bf16, d = 128, us: one
+  // sequence of 500 rows on eight KV heads 10.8 and 8.0; 32 of 160 .. 500 14.7 and 10.0, of 300 .. 1000 18.6 and 14.0, of 700 .. 2000 27.0
+  // and 22.3; 64 of 700 .. 2000 42.0 and 39.3.  8 of 1000 11.4 and 11.6, 16 of 2000 16.6 and 18.3, 256 of 500 54 and 61.)  With many
+  // sequences every piece's workgroup would read all their lengths.
+  const long long steps = (room + SHORT_WAVES * 32 - 1) / (SHORT_WAVES * 32), units = (long long)p.B * p.Hkv;
+  g.one_launch = steps <= 1 || (steps <= 2 && (units <= 512 || p.B > 512)) ||
+                 (units <= 512 && ((steps <= 4 && units >= 128) || (steps <= 8 && units >= 256)));
   // Two pieces a CU, and one where they are short.  Three for many sequences that can still be cut alike, since each then has few:
   // 64 sequences of 700 .. 4351 rows on four KV heads that begin with the same 640 38.4 us, with three 34.4; 32 of 2000 .. 8000 on eight
   // 64.2 and 62.7.  (64 on eight, in proportion, 66.3 and 69.9; 8 of 3001 .. 65536 95 and 97.6; four or six a CU, in turns,

@@ -556,6 +556,20 @@ def test_attention_long_and_many(dtype, B, Hq, Hkv, d, page, lengths):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,Hkv,d,page,room", [
+    (1, 1, 64, 32, 7), (1, 1, 64, 32, 8), (64, 8, 64, 64, 7), (65, 8, 64, 64, 7), (513, 1, 64, 128, 3), (16, 8, 128, 32, 31), (16, 8, 64, 32, 32), (15, 8, 64, 128, 7),
+    (32, 8, 64, 32, 63), (32, 8, 64, 64, 32), (31, 8, 64, 64, 31), (64, 8, 128, 128, 15), (43, 12, 64, 32, 63)])
+def test_attention_in_one_launch_and_in_pieces(dtype, B, Hkv, d, page, room):
+    """Batches on both sides of what one launch takes."""
+    g = np.random.default_rng(room)
+    lengths = g.integers(0, room * page + page, B).tolist()
+    lengths[:3] = [room * page + page - 1, 0, page][:B]
+    pages = _filled(dtype, B, Hkv, d, page, lengths, 3, room)
+    q = _query(dtype, B, 2 * Hkv, d, 4, 1.5)
+    _check_attention(q, pages, lengths, *wb.wave_pages_attention_decode(q, pages))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("room", [2, 60])
 def test_attention_extreme_scores(dtype, room):
     """Scores of hundreds, growing row by row and falling; pages of scale 0 (all scores alike)."""
