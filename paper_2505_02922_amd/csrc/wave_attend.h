@@ -270,13 +270,17 @@ struct State {
     if (__any(top > m + kSlack)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float grown = fmaxf(m, top);
-      const float f = m == neg_inf() ? 0.f : exp2f(m - grown);
-      m = grown;
-      l *= f;
-#pragma unroll
-      for (int a = 0; a < S::ACC; ++a) o[a] *= f;
+      raise(top);
     }
+  }
+  // to `top`, the same in all lanes of a column
+  __device__ __forceinline__ void raise(float top) {
+    const float grown = fmaxf(m, top);
+    const float f = m == neg_inf() ? 0.f : exp2f(m - grown);
+    m = grown;
+    l *= f;
+#pragma unroll
+    for (int a = 0; a < S::ACC; ++a) o[a] *= f;
   }
   // p: the weights exp(s / sqrt(d)) over the reference.  The scale is applied inside the difference, which is then rounded
   // once.
