@@ -272,7 +272,7 @@ __device__ __forceinline__ void copy_chunks(const char* x, char* y, int chunks) 
   }
 }
 
-// Append, first launch: one workgroup finds how many tokens of each sequence fit and which pages they take.  A sequence's
+// Append, first launch (but see OwnToken): one workgroup finds how many tokens of each sequence fit and which pages they take.  A sequence's
 // share depends on what those before it take, and the free pages are found by going through references in ascending order,
 // so the pages are the same in every run.  It is a chain of loads and scans behind barriers: 4.1 us for 64 sequences and a pool of
 // 2600 pages (5.1 with sixteen loads and ballots a thread instead of four wide loads and one scan).
@@ -309,33 +309,37 @@ __device__ __forceinline__ int plan_scan(int x, int& sum, int (&part)[PLAN_WAVES
   return sum_to_many(before, lane ? below : 0);
 }
 
-__global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pages from, const wave_pages to, const int32_t* counts, int n,
-                                                                 const PagesPlan plan, bool apart) {
+// The references of PER pages side by side; pages that there are not count as taken.
+template <int PER>
+struct PageReferences {
   typedef __attribute__((ext_vector_type(4), aligned(4))) int int4_of_ints;
-  __shared__ int part[PLAN_WAVES];
-  const int tid = threadIdx.x, shift = page_shift(from.page);
-  // A thread has sixteen pages side by side.
-  int4_of_ints ref[PLAN_PER / 4];
-  auto load = [&](int r0) {
-    const int first = r0 + tid * PLAN_PER;
-    if (first + PLAN_PER <= from.n_pages) {
+  int4_of_ints ref[PER / 4];
+  __device__ __forceinline__ void load(const wave_pages& p, int first) {
+    if (first + PER <= p.n_pages) {
 #pragma unroll
-      for (int i = 0; i < PLAN_PER / 4; ++i) ref[i] = *reinterpret_cast<const int4_of_ints*>(from.references + first + i * 4);
-    } else {  // the last ones: pages that there are not count as taken
+      for (int i = 0; i < PER / 4; ++i) ref[i] = *reinterpret_cast<const int4_of_ints*>(p.references + first + i * 4);
+    } else {
 #pragma unroll
-      for (int i = 0; i < PLAN_PER; ++i) {
-        const int r = from.references[min(first + i, from.n_pages - 1)];
-        ref[i / 4][i % 4] = first + i < from.n_pages ? r : 1;
+      for (int i = 0; i < PER; ++i) {
+        const int r = p.references[min(first + i, p.n_pages - 1)];
+        ref[i / 4][i % 4] = first + i < p.n_pages ? r : 1;
       }
     }
-  };
-  auto free_pages = [&]() {
-    uint32_t free = 0;
+  }
+  __device__ __forceinline__ uint32_t free() const {  // a bit each
+    uint32_t f = 0;
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) free |= (uint32_t)(ref[i / 4][i % 4] <= 0) << i;
-    return free;
-  };
-  load(0);
+    for (int i = 0; i < PER; ++i) f |= (uint32_t)(ref[i / 4][i % 4] <= 0) << i;
+    return f;
+  }
+};
+
+__global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pages from, const wave_pages to, const int32_t* counts, int n,
+                                                                 const PagesPlan plan, bool apart) {
+  __shared__ int part[PLAN_WAVES];
+  const int tid = threadIdx.x, shift = page_shift(from.page);
+  PageReferences<PLAN_PER> refs;
+  refs.load(from, tid * PLAN_PER);
   int wanted = 0;  // pages wanted by the sequences so far
   int4 mine = make_int4(0, 0, 0, 0);
   for (int b0 = 0; b0 < from.B; b0 += PLAN_THREADS) {
@@ -354,9 +358,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
   int found = 0;
   if (tid == 0) plan.last[0] = -1;
   for (int r0 = 0; r0 < from.n_pages && found < wanted; r0 += PLAN_ROUND) {
-    uint32_t free = free_pages();
-    if (r0 + PLAN_ROUND < from.n_pages) load(r0 + PLAN_ROUND);
+    uint32_t free = refs.free();
     const int first = r0 + tid * PLAN_PER;
+    if (r0 + PLAN_ROUND < from.n_pages) refs.load(from, first + PLAN_ROUND);
     int rank = plan_scan(__popc(free), found, part);
     for (; free && rank < wanted; free &= free - 1, ++rank) {
       const int page = first + __ffs(free) - 1;
@@ -386,9 +390,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
 //           unless they complete a page: then the pages' workgroups have little to do but in the one sequence of `page` that does
 //   lists   table and references of a state with arrays of its own
 // Four prompts of up to 8191 tokens, 32 and 8 heads, d = 128: 118 us, 553 MB, 4.7 TB/s (132 before the next head's rows were asked for
-// while this one's are rounded, and outputs passed by the caches).  One token of 64 sequences of 28 and 4 heads: 7.5 us into a state
-// beside, whose tails are 16 MB read and written; the tokens alone 4.8.
+// while this one's are rounded, and outputs passed by the caches).  One token of 64 sequences of 28 and 4 heads in place 4.8 us.
 struct AppendGrid {
+  unsigned reference_blocks;           // without a plan
   unsigned page_blocks, token_blocks;  // the others are lists
   int units, head_groups;              // pages that a sequence's new tokens may touch; workgroups that share a page's heads
   TurnShape sh;
@@ -410,10 +414,12 @@ struct PageRows {
   static constexpr bool AHEAD = PASSES <= 2;  // (more would take too many registers)
   typedef SineTable<T, D, TOKENS> Table;
 
-  // One page of sequence b, heads first .. in steps of `step`.
-  static __device__ __forceinline__ void run(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
-                                             const PagesPlan& plan, const int4 s, int b, int u, bool keys, int first, int step,
-                                             Table& table, uint32_t (*top)[4]) {
+  // Part u of sequence b's new state, heads first .. in steps of `step`; find(): the page that it goes to if it is complete; where
+  // that is not SURE, negative if there is none, and then nothing is done.
+  template <bool SURE, typename F>
+  static __device__ __forceinline__ bool run(const wave_pages& from, const wave_pages& to, const PagesAppendArgs& a, const RotaryArgs& rot,
+                                             const int4 s, int b, int u, bool keys, int first, int step, Table& table,
+                                             uint32_t (*top)[4], F&& find) {
     const int tid = threadIdx.x, row0 = tid / ITEMS;
     const int whole = s.x / PAGE, start = (whole + u) * PAGE, end = s.y;
     const bool complete = start + PAGE <= end;
@@ -442,7 +448,8 @@ struct PageRows {
       table.fill(rot, r0, r1, [&](int axis, int r) {
         return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + start + r - s.x] : start + r;
       });
-    const int page = complete ? plan.taken[s.z + u] : 0;
+    const int page = complete ? find() : 0;
+    if (!SURE && page < 0) return false;
     if (complete && keys && first == 0 && tid == 0) to.table[(size_t)b * to.max_pages + whole + u] = page;
     int turn = 0;
     for (int h = first; h < from.Hkv; h += step, turn ^= 1) {
@@ -538,32 +545,188 @@ struct PageRows {
       }
       advance();
     }
+    return true;
   }
 };
 
-template <typename T, int D, int PAGE>
+// One token into a state of its own arrays: `from` stays as it is, so a workgroup can find by itself what the plan says.  Only one whose
+// token completes a page has to look further than its sequence's length: at the other lengths, for how many before it do, and at
+// references; the rows are on their way meanwhile.  In one launch (with a plan's, us; calls in a row, so the host's part too): 64
+// sequences of 28 and 4 heads 10.7 (14.2), kernels 8.4 (4.0 + 6.2); 256 of them with 15.8K pages 16.1 (18.2), 16.1 (4.6 + 12.5); where
+// all complete a page the kernels are even.  Beyond these numbers of sequences and pages the plan, which reads them once.
+// The functions below take all threads together.  Their loads stand side by side without conditions: behind one each would be waited
+// for alone (12.5 -> 18.9 for 256 sequences).
+constexpr int OWN_SEQUENCES = 4 * THREADS, OWN_PAGES = 64 * THREADS, OWN_REFERENCES = 4;
+__device__ __forceinline__ int workgroup_sum(int x, int (&part)[THREADS / 64]) {
+  x = wave_sum_i(x);
+  __syncthreads();  // (what the call before this one left has been read)
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return part[0] + part[1] + part[2] + part[3];
+}
+struct OwnToken {
+  int length;
+  bool given, fits, completes;
+  __device__ __forceinline__ OwnToken(const wave_pages& p, int held, int count) {
+    length = min(max(held, 0), pages_room(p));
+    given = count > 0;
+    fits = given && length < pages_room(p);
+    completes = fits && ((length + 1) & (p.page - 1)) == 0;
+  }
+  __device__ __forceinline__ OwnToken(const wave_pages& p, const int32_t* counts, int b)
+      : OwnToken(p, p.lengths[b], counts ? counts[b] : 1) {}
+};
+// how many sequences below `end` complete a page
+__device__ __forceinline__ int own_wanted(const wave_pages& p, const int32_t* counts, int end, int (&part)[THREADS / 64]) {
+  constexpr int PER = OWN_SEQUENCES / THREADS;
+  int held[PER], count[PER], n = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) held[i] = p.lengths[min((int)threadIdx.x + i * THREADS, p.B - 1)];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) count[i] = 1;
+  if (counts) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) count[i] = counts[min((int)threadIdx.x + i * THREADS, p.B - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool completes = OwnToken(p, held[i], count[i]).completes;
+    n += (int)threadIdx.x + i * THREADS < end ? completes : 0;
+  }
+  return workgroup_sum(n, part);
+}
+// Four pages' references and which of them are free (a bit each, none behind the pool), without a branch: the last ones are read from
+// the pool's end on.
+struct OwnReferences {
+  PageReferences<4>::int4_of_ints ref;
+  int moved;
+  __device__ __forceinline__ void load(const wave_pages& p, int first) {
+    const int at = min(first, p.n_pages - 4);
+    ref = *reinterpret_cast<const PageReferences<4>::int4_of_ints*>(p.references + at);
+    moved = min(first - at, 31);
+  }
+  __device__ __forceinline__ uint32_t free() const {
+    uint32_t f = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f |= (uint32_t)(ref[i] <= 0) << i;
+    return f >> moved;
+  }
+};
+struct OwnCounts {
+  int sums[THREADS / 64], free[64], found;
+};
+// the page that sequence b, which completes one, takes (-1: none is free for it)
+__device__ __forceinline__ int own_page(const wave_pages& p, const int32_t* counts, int b, OwnCounts& shared) {
+  // Pieces of 256 pages, a piece each wave and round: how many are free in each, which one has the page, and then where it is there.
+  constexpr int PER = OWN_REFERENCES, PIECE = 64 * PER, WAVES = THREADS / 64, ROUNDS = OWN_PAGES / PIECE / WAVES;
+  static_assert(ROUNDS * WAVES == 64, "a lane each");
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  OwnReferences refs[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) refs[r].load(p, (r * WAVES + wave) * PIECE + lane * PER);
+  const int rank = own_wanted(p, counts, b, shared.sums);
+  uint64_t free = 0;  // this lane's, PER bits a round
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    int n = 0;
+    const uint32_t mine = refs[r].free();
+    free |= (uint64_t)mine << (PER * r);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) n += __popcll(__ballot(mine >> i & 1));
+    if (lane == 0) shared.free[r * WAVES + wave] = n;
+  }
+  __syncthreads();
+  const int upto = wave_incl_scan(shared.free[lane]);
+  const uint64_t behind = __ballot(upto > rank);
+  if (!behind) return -1;
+  const int piece = __ffsll((unsigned long long)behind) - 1;
+  if (piece % WAVES == wave) {
+    uint32_t mine = (uint32_t)(free >> (PER * (piece / WAVES))) & ((1u << PER) - 1);
+    const int here = __popc(mine);
+    int at = (piece ? __builtin_amdgcn_readlane(upto, piece - 1) : 0) + wave_incl_scan(here) - here;
+    if (rank >= at && rank < at + here) {
+      for (; at < rank; ++at) mine &= mine - 1;
+      shared.found = piece * PIECE + lane * PER + __ffs(mine) - 1;
+    }
+  }
+  __syncthreads();
+  return shared.found;
+}
+// references of the pages that workgroup `block` has: those of the first `wanted` free ones become 1
+__device__ __forceinline__ void own_references(const wave_pages& from, const wave_pages& to, const int32_t* counts, int block,
+                                               OwnCounts& shared) {
+  int(&part)[THREADS / 64] = shared.sums;
+  constexpr int PER = OWN_REFERENCES;
+  const int r0 = block * THREADS * PER, first = r0 + threadIdx.x * PER;
+  PageReferences<PER> refs;
+  refs.load(from, first);
+  const uint32_t free = refs.free();
+  int before = 0;  // free pages in front of the workgroup's
+  OwnReferences others[OWN_PAGES / THREADS / PER];
+#pragma unroll
+  for (int i = 0; i < OWN_PAGES / THREADS / PER; ++i) others[i].load(from, (min(i, block) * THREADS + threadIdx.x) * PER);
+#pragma unroll
+  for (int i = 0; i < OWN_PAGES / THREADS / PER; ++i)
+    before += i < block ? __popc(others[i].free()) : 0;
+  const int wanted = own_wanted(from, counts, from.B, part);
+  int rank = wanted;  // free pages in front of the thread's
+  if (wanted > 0) {
+    const int here = __popc(free), incl = wave_incl_scan(here), wave = threadIdx.x >> 6;
+    rank = workgroup_sum(before, part) + incl - here;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) part[wave] = incl;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) rank += part[w];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (first + i < from.n_pages) {
+      const bool is_free = free >> i & 1;
+      to.references[first + i] = is_free && rank < wanted ? 1 : refs.ref[0][i];
+      rank += is_free;
+    }
+}
+
+// FINDS: without a plan
+template <typename T, int D, int PAGE, bool FINDS>
 __global__ __launch_bounds__(THREADS) void pages_append_kernel(const wave_pages from, const wave_pages to, const PagesAppendArgs a,
                                                                const RotaryArgs rot, const PagesPlan plan, const AppendGrid grid) {
   typedef PageRows<T, D, PAGE> Rows;
   __shared__ typename Rows::Table table;
   __shared__ uint32_t top[2][4];
+  __shared__ OwnCounts own;
   unsigned block = workgroup_number();
+  if constexpr (FINDS) {  // (first, as theirs is the longest chain)
+    if (block < grid.reference_blocks) {
+      own_references(from, to, a.counts, block, own);
+      return;
+    }
+    block -= grid.reference_blocks;
+  }
   if (block < grid.page_blocks) {
     const int group = block % grid.head_groups, keys = (block / grid.head_groups) & 1;
     const unsigned bu = block / grid.head_groups / 2;
     const int b = bu / grid.units;
     int u = bu % grid.units, parts = 1;
-    const int4 s = plan.sequence[b];
+    int4 s;
+    if constexpr (FINDS) {
+      const OwnToken t(from, a.counts, b);
+      s = make_int4(t.length, t.length + t.fits, 0, t.given);
+    } else {
+      s = plan.sequence[b];
+    }
     const int rest = s.y / PAGE - s.x / PAGE;  // the unit whose rows are the tail
-    if (a.n == 1) {
+    auto copy_tail = [&]() {
+      for (int h = group; h < from.Hkv; h += grid.head_groups) {
+        const size_t at = ((size_t)b * from.Hkv + h) * PAGE * D * sizeof(T);
+        copy_chunks(static_cast<const char*>(keys ? from.k_tail : from.v_tail) + at, static_cast<char*>(keys ? to.k_tail : to.v_tail) + at,
+                    s.x % PAGE * (int)(D * sizeof(T) / 16));
+      }
+    };
+    if (FINDS || a.n == 1) {
       // (a token that completes no page is written by its own workgroup: here only old rows go on)
       if (s.y == s.x || s.y % PAGE != 0) {
-        if (!a.apart) return;
-        for (int h = group; h < from.Hkv; h += grid.head_groups) {
-          const size_t at = ((size_t)b * from.Hkv + h) * PAGE * D * sizeof(T);
-          copy_chunks(static_cast<const char*>(keys ? from.k_tail : from.v_tail) + at, static_cast<char*>(keys ? to.k_tail : to.v_tail) + at,
-                      s.x % PAGE * (int)(D * sizeof(T) / 16));
-        }
+        if (FINDS || a.apart) copy_tail();
         return;
       }
     } else {
@@ -572,12 +735,20 @@ __global__ __launch_bounds__(THREADS) void pages_append_kernel(const wave_pages 
       if (u > rest || (u == rest && (both || s.y % PAGE == 0))) return;
       if (u == 0 && both) parts = 2;
     }
-    for (int part = 0; part < parts; ++part) {
-      if (part) {
-        __syncthreads();  // everything that was in the tail has been read, the sines and the maxima too
-        u = rest;
+    if constexpr (FINDS) {
+      const bool found = Rows::template run<false>(from, to, a, rot, s, b, 0, keys, group, grid.head_groups, table, top,
+                                   [&]() { return own_page(from, a.counts, b, own); });
+      if (!found) copy_tail();
+      if (keys && group == 0 && threadIdx.x == 0) to.lengths[b] = found ? s.y : s.x;
+    } else {
+      for (int i = 0; i < parts; ++i) {
+        if (i) {
+          __syncthreads();  // everything that was in the tail has been read, the sines and the maxima too
+          u = rest;
+        }
+        const int page = u < rest ? plan.taken[s.z + u] : 0;
+        Rows::template run<true>(from, to, a, rot, s, b, u, keys, group, grid.head_groups, table, top, [page]() { return page; });
       }
-      Rows::run(from, to, a, rot, plan, s, b, u, keys, group, grid.head_groups, table, top);
     }
     return;
   }
@@ -587,9 +758,14 @@ __global__ __launch_bounds__(THREADS) void pages_append_kernel(const wave_pages 
     const int b = bt / grid.tiles, tile = bt % grid.tiles;
     int4 s;
     norm_heads<T, D>(
-        a.rows, a.v_new, a.n == 1 ? from.Hkv : 0, rot, grid.sh, b, tile, group, table,
+        a.rows, a.v_new, FINDS || a.n == 1 ? from.Hkv : 0, rot, grid.sh, b, tile, group, table,
         [&]() {
-          s = plan.sequence[b];
+          if constexpr (FINDS) {  // (a token that completes a page is the pages' workgroups' in any case)
+            const OwnToken t(from, a.counts, b);
+            s = make_int4(t.length, t.length + t.fits, 0, t.given);
+          } else {
+            s = plan.sequence[b];
+          }
           return s.w;
         },
         [&](int axis, int n) { return a.rows.coords ? a.rows.coords[((size_t)axis * from.B + b) * a.n + n] : s.x + n; },
@@ -608,11 +784,19 @@ __global__ __launch_bounds__(THREADS) void pages_append_kernel(const wave_pages 
   if (!a.apart) return;
   // one workgroup a sequence for the tables, the others for references
   if (block < (unsigned)from.B) {
-    const int whole = plan.sequence[block].x / PAGE;
+    int whole;
+    if constexpr (FINDS) {
+      const OwnToken t(from, a.counts, block);
+      whole = t.length / PAGE;
+      if (!t.completes && threadIdx.x == 0) to.lengths[block] = t.length + t.fits;
+    } else {
+      whole = plan.sequence[block].x / PAGE;
+    }
     const size_t at = (size_t)block * from.max_pages;
     for (int i = threadIdx.x; i < whole; i += 256) to.table[at + i] = from.table[at + i];
     return;
   }
+  if constexpr (FINDS) return;
   const int last = plan.last[0];
   const long long i = (long long)(block - from.B) * 256 + threadIdx.x;
   if (i < from.n_pages) {
@@ -625,8 +809,9 @@ template <typename T, int D, int PAGE>
 wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, PagesAppendArgs a, const RotaryArgs& rot,
                              const PagesPlan& plan, hipStream_t st) {
   a.rows.past = a.n > 1 && (size_t)from.B * a.rows.Hq * a.n * D * sizeof(T) > PAST_BYTES;
-  WAVE_LAUNCH("pages_plan", pages_plan_kernel, 1, PLAN_THREADS, 0, st, from, to, a.counts, a.n, plan, a.apart);
   AppendGrid g{};
+  const bool finds = a.n == 1 && a.apart && from.B <= OWN_SEQUENCES && from.n_pages >= 4 && from.n_pages <= OWN_PAGES;
+  if (!finds) WAVE_LAUNCH("pages_plan", pages_plan_kernel, 1, PLAN_THREADS, 0, st, from, to, a.counts, a.n, plan, a.apart);
   g.units = a.n == 1 ? 1 : (int)(((long long)PAGE - 2 + a.n) / PAGE) + 1;
   // A page's heads are split while the launch leaves most CUs without work; together they share the sines.
   g.head_groups = 1;
@@ -645,8 +830,12 @@ wave_status pages_append_tdp(const wave_pages& from, const wave_pages& to, Pages
     g.token_blocks = (unsigned)((long long)from.B * g.tiles * g.sh.head_groups);
     blocks += g.token_blocks;
   }
-  if (a.apart) blocks += from.B + ((long long)from.n_pages + 255) / 256;
-  WAVE_LAUNCH("pages_append", (pages_append_kernel<T, D, PAGE>), grid_rows(blocks), 256, 0, st, from, to, a, rot, plan, g);
+  g.reference_blocks = finds ? (from.n_pages + THREADS * OWN_REFERENCES - 1) / (THREADS * OWN_REFERENCES) : 0;
+  if (a.apart) blocks += from.B + (finds ? (long long)g.reference_blocks : ((long long)from.n_pages + 255) / 256);
+  if (finds)
+    WAVE_LAUNCH("pages_append", (pages_append_kernel<T, D, PAGE, true>), grid_rows(blocks), 256, 0, st, from, to, a, rot, plan, g);
+  else
+    WAVE_LAUNCH("pages_append", (pages_append_kernel<T, D, PAGE, false>), grid_rows(blocks), 256, 0, st, from, to, a, rot, plan, g);
   return hipGetLastError() == hipSuccess ? WAVE_OK : WAVE_ERR_HIP;
 }
 template <typename T, int D>

@@ -10,10 +10,11 @@ namespace {
 // A step: 32 rows of one page against 16 query columns.  Codes are whole numbers up to 127, which bf16 holds, so the products
 // are those of the plain cache's bf16 step with the codes widened on the way; the page's scales are the same for the whole
 // step, one inside the exponent, the other on the weights.  An fp32 query is three bf16 numbers that hold all its bits.
-// Eight sequences of 3001 .. 65536 rows, 32 and 8 heads, d = 128: 89.6 us, 562 MB (what is fetched, to 1 %), 6.3 TB/s, more than a plain
-// read's 5.57.  A step is about 350 vector instructions, 128 of them the widening (one a code and one for two) and 44 the weights' three
-// numbers; they keep the vector units busy for 52 % of that time, 59 % where 64 sequences of up to 4351 rows begin alike and a third of the
-// rows come from the caches (29 us, 165 MB of which 116 are fetched), 61 % at d = 64, where the steps are half as long (5.1 TB/s).
+// Eight sequences of 3001 .. 65536 rows, 32 and 8 heads, d = 128: 88.8 us, 562 MB (what is fetched, to 1 %), 6.3 TB/s, more than a plain
+// read's 5.57.  A step is about 325 vector instructions, 128 of them the widening (one a code and one for two); they keep the vector
+// units busy for 49 % of the time that a CU has work, 53 % at d = 64, 66 % where 64 sequences of up to 4351 rows begin alike and a
+// third of the rows come from the caches (28.7 us, 165 MB of which 116 are fetched).  Neither they nor the products bound that: with the
+// codes taken for bf16 as they are, and a product less a channel, the call took 31.4 us instead of 33.3.
 // ----------------------------------------------------------------------------
 template <typename T, int D>
 struct Codes {

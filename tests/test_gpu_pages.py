@@ -399,6 +399,49 @@ def test_free_pages_of_pools_of_every_size(n_pages, B):
             assert np.array_equal(k[b, 0, p:p + page].cpu().numpy(), codes.astype(np.float32) * scale)
 
 
+@pytest.mark.parametrize("n_pages,B,Hkv,page,d", [(3, 2, 1, 32, 64), (4, 3, 2, 64, 128), (1027, 1024, 1, 32, 64), (2600, 130, 3, 64, 128), (16384, 400, 1, 32, 64),
+                                                   (16385, 400, 1, 32, 64), (16000, 1025, 1, 32, 64), (5000, 70, 2, 128, 128)])
+@pytest.mark.parametrize("taken,whole", [(0.5, 0.1), (0.97, 0.5), (0.999, 0.9)])
+def test_a_token_into_a_state_beside_takes_the_same_pages_as_in_place(n_pages, B, Hkv, page, d, taken, whole):
+    """On both sides of the sizes from which a plan is made; with counts, pages that run out, and references below 0."""
+    g = _gen(n_pages + B)
+    most = 2
+    room = most * page + page - 1
+    a, b = (wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, n_pages, most) for _ in range(2))
+    to = wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, n_pages, most, pool=b)
+    to.references.fill_(9), to.table.fill_(-7), to.lengths.fill_(-1)
+    references = (torch.rand(n_pages, generator=g) < taken).to(torch.int32) * 2
+    references[torch.rand(n_pages, generator=g) < 0.01] = -3
+    lengths = torch.randint(0, room + 1, (B,), generator=g, dtype=torch.int32)
+    completes = torch.rand(B, generator=g) < whole
+    lengths[completes] = lengths[completes] // page * page + page - 1     # (those without room in the table among them)
+    counts = torch.randint(-1, 3, (B,), generator=g, dtype=torch.int32)
+    table = torch.randint(0, n_pages, (B, most), generator=g, dtype=torch.int32)
+    tail = torch.randn(2, B, Hkv, page, d, generator=g).bfloat16()
+    for s in (a, b):
+        s.references.copy_(references), s.lengths.copy_(lengths), s.table.copy_(table), s.k_tail.copy_(tail[0]), s.v_tail.copy_(tail[1])
+    q, k, v = (torch.randn(B, h, 1, d, generator=g).bfloat16().cuda() for h in (2 * Hkv, Hkv, Hkv))
+    r, w = wb.wave_rotary_plan(d, 1e4), (1 + 0.2 * torch.randn(d, generator=g)).bfloat16().cuda()
+    for c in (None, counts.cuda()):
+        outs = [torch.full_like(q, 3.0) for _ in range(2)]
+        kept = _state(b)
+        wb.wave_pages_append(a, k, v, q=q, q_weight=w, k_weight=w, rotary=r, counts=c, q_out=outs[0])
+        wb.wave_pages_append(b, k, v, q=q, q_weight=w, k_weight=w, rotary=r, counts=c, q_out=outs[1], to=to)
+        for name in OWN:
+            assert _same_bits(kept[name], b.t[name]), name
+        assert _same_bits(outs[0], outs[1]) and torch.equal(a.lengths, to.lengths) and torch.equal(a.references, to.references)
+        n = a.lengths.cpu()
+        for i in range(most):
+            held = n // page > i
+            assert torch.equal(a.table.cpu()[held, i], to.table.cpu()[held, i])
+        rows = (torch.arange(page)[None] < (n % page)[:, None])[:, None, :, None].expand(B, Hkv, page, d)
+        for name in ("k_tail", "v_tail"):
+            assert torch.equal(a.t[name].cpu()[rows], to.t[name].cpu()[rows]), name
+        for name in wb.PAGE_POOL:
+            assert _same_bits(a.t[name], to.t[name]), name
+        b, to = to, b
+
+
 def test_many_sequences_and_more_workgroups_than_a_launch_row():
     """Two million sequences; the rows of every one of them are its own."""
     B, d, page = (1 << 21) - 1, 64, 32
@@ -895,3 +938,78 @@ def test_offsets_beyond_32_bits():
     assert pages.table[0, :2].tolist() == [n_pages - 3, n_pages - 2] and bool(pages.k_codes[-3].any()) and not bool(pages.k_codes[:100].any())
     for a, b in zip(*got):
         assert _same_bits(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_read_of_one_side(dtype):
+    """Through the C ABI, which takes keys or values alone."""
+    pages = _filled(dtype, 2, 2, 128, 64, [200, 70], 18)
+    first = torch.tensor([3, 60], dtype=torch.int32, device="cuda")
+    both = wb.wave_pages_read(pages, 90, first=first, k_out=torch.full((2, 2, 90, 128), 5.0, dtype=TYPES[dtype], device="cuda"),
+                              v_out=torch.full((2, 2, 90, 128), 5.0, dtype=TYPES[dtype], device="cuda"))
+    stream = torch.cuda.current_stream().cuda_stream
+    for i, want in enumerate(both):
+        out = torch.full_like(want, 5.0)
+        at = [out.data_ptr() if j == i else None for j in range(2)]
+        assert wb.lib().wave_pages_read(pages.ref, first.data_ptr(), 90, *at, stream) == 0
+        assert _same_bits(out, want)
+
+
+def test_append_of_broadcast_rows():
+    """One key and value row for all heads, sequences and tokens, and queries that share one row a head: strides of 0."""
+    B, Hq, Hkv, d, n = 3, 8, 4, 64, 45
+    g = _gen(19)
+    k, v = (torch.randn(1, 1, 1, d, generator=g).bfloat16().cuda().expand(B, Hkv, n, d) for _ in range(2))
+    q = torch.randn(1, Hq, 1, d, generator=g).bfloat16().cuda().expand(B, Hq, n, d)
+    w, r = (1 + 0.2 * torch.randn(d, generator=g)).bfloat16().cuda(), wb.wave_rotary_plan(d, 1e4)
+    got = []
+    for dense in (False, True):
+        x = [t.contiguous() if dense else t for t in (k, v, q)]
+        pages = wb.alloc_pages(torch.bfloat16, B, Hkv, d, 32, 8, 2)
+        out = wb.wave_pages_append(pages, x[0], x[1], q=x[2], q_weight=w, k_weight=w, rotary=r)
+        got.append((out,) + wb.wave_pages_read(pages, n))
+    for a, b in zip(*got):
+        assert _same_bits(a, b)
+
+
+def test_captured_steps_in_place_replay():
+    """Appends in place and attention, captured once and replayed past the ends of pages, with eager work between the replays."""
+    B, Hq, Hkv, d, page = 4, 8, 2, 64, 32
+    g = _gen(20)
+    r, w = wb.wave_rotary_plan(d, 1e4), (1 + 0.2 * torch.randn(d, generator=g)).bfloat16().cuda()
+    tokens = [[torch.randn(B, h, 1, d, generator=g).bfloat16().cuda() for h in (Hq, Hkv, Hkv)] for _ in range(6)]
+
+    def make():
+        s = _filled("bf16", B, Hkv, d, page, [29, 60, 0, 31], 21, 20)
+        ws = wb.workspace(max(wb.wave_pages_append_workspace(s), wb.wave_pages_attention_workspace(s, Hq)))
+        x = [t.clone() for t in tokens[0]] + [torch.empty_like(tokens[0][0]), torch.empty(B, Hq, d, device="cuda"), torch.empty(B, Hq, device="cuda")]
+        return s, ws, x
+
+    def step(s, ws, x):
+        q, k, v, q_out, out, lse = x
+        wb.wave_pages_append(s, k, v, q=q, q_weight=w, k_weight=w, rotary=r, q_out=q_out, ws=ws)
+        wb.wave_pages_attention_decode(q_out.view(B, Hq, d), s, out=out, lse=lse, ws=ws)
+
+    eager, captured = make(), make()
+    step(*make())
+    torch.cuda.synchronize()
+    saved = _state(captured[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*captured)
+    for n in saved:
+        captured[0].t[n].copy_(saved[n])
+    for i, new in enumerate(tokens):
+        for s, _, x in (eager, captured):
+            for t, u in zip(x, new):
+                t.copy_(u)
+        step(*eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager[2][3:], captured[2][3:]):
+            assert _same_bits(a, b), i
+        assert torch.equal(eager[0].lengths, captured[0].lengths) and torch.equal(eager[0].references, captured[0].references), i
+        for a, b in zip(wb.wave_pages_read(eager[0], 70), wb.wave_pages_read(captured[0], 70)):
+            assert _same_bits(a, b), i
+    assert captured[0].lengths.tolist() == [n + len(tokens) for n in (29, 60, 0, 31)]
