@@ -509,6 +509,8 @@ wave_status wave_cache_evict(const wave_cache *from, const wave_cache *to, int n
  * references counts the sequences that hold a page; one with 0 (or less) is free, so an empty
  * cache is lengths and references of 0.  A caller who keeps a page (a prompt that comes back) adds 1 of its own.
  * A sequence is not cut short by setting its length back: the rows of a complete page are no longer in the tail.
+ * Appends to, and reorderings of, states of one pool take and give back the same pages: the caller orders them, and goes
+ * on with the state that the last one left.  What only reads a state may run beside an append that leaves it as it is.
  * The library reads lengths and table on the device: a length outside 0 ..
  * max_pages * page + page - 1 and an entry outside 0 .. n_pages - 1 count as the nearest inside.
  * Every call returns WAVE_ERR_SHAPE for a page other than 32, 64 or 128, B * Hkv of 2^21 and more,
