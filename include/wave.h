@@ -500,7 +500,7 @@ wave_status wave_cache_evict(const wave_cache *from, const wave_cache *to, int n
  * not depend on how its tokens came in, the newest rows are exact, and sequences that begin
  * alike share pages.
  *   scale = max |x| / 127 over the page's rows of a head, as they are in dtype;
- *   code  = x * (127 / max |x|) to the nearest whole number, ties to even (fp32)
+ *   code  = x * ((1 / max |x|) * 127) to the nearest whole number, ties to even (fp32, each step rounded)
  * and a row reads as code * scale.  A head's part of a page whose largest value is below 2^-100 reads as zeros
  * (scale 0); one that holds an infinity or no number reads as no numbers throughout.
  *

@@ -40,7 +40,7 @@ def page_codes(rows: np.ndarray) -> Tuple[np.ndarray, np.float32]:
     top = np.abs(rows).max()
     if top < LEAST:
         return np.zeros(rows.shape, np.int8), np.float32(0.0)
-    inv = np.float32(127.0) / top
+    inv = np.float32(1.0) / top * np.float32(127.0)
     return np.clip(np.rint(rows * inv), -127, 127).astype(np.int8), top / np.float32(127.0)
 
 

@@ -513,9 +513,10 @@ struct PageRows {
       if ((tid & 63) == 0) top[turn][tid >> 6] = most;
       __syncthreads();
       most = max(max(top[turn][0], top[turn][1]), max(top[turn][2], top[turn][3]));
-      // (below 2^-100, where 127 / max may be infinite, the page counts as zeros)
+      // (below 2^-100, where 127 / max may be infinite, the page counts as zeros.  The quotient as a reciprocal and a product, as most
+      // implementations of one array of quotients have it, rounds twice: that moves a code that is within 2e-5 of a border.)
       const bool number = most < 0x7f800000u, some = most >= 0x0d800000u;
-      const float inv = number && some ? 127.f / __uint_as_float(most) : 0.f;
+      const float inv = number && some ? 1.f / __uint_as_float(most) * 127.f : 0.f;
       const float scale = !number ? __uint_as_float(0x7fc00000u) : some ? __uint_as_float(most) / 127.f : 0.f;
       const size_t unit = (size_t)page * from.Hkv + h;
       if (tid == 0) (keys ? to.k_scales : to.v_scales)[unit] = scale;
