@@ -933,54 +933,65 @@ __global__ __launch_bounds__(256) void pages_references_kernel(const int32_t* fr
 }
 
 // Into arrays of its own.
-//   counts  COUNT_PAGES pages' references: from's, and what `to` and `from` hold of them, counted in LDS by going through all
-//           tables.  Where these have more than COUNT_ENTRIES entries, references are copied by a launch before this one, and each
-//           sequence's workgroup adds to them (eight sequences: 2.8 us, in two launches 3.8 and the host's second call; 256 of 63
-//           entries, 32256 in all: the counting takes 40 us, two launches 27; 31 with the tails' keys copied in the first of them)
+//   counts  COUNT_PAGES pages' references: from's, and what changes, counted in LDS by going through the tables of those sequences
+//           whose pages gain or lose.  Where these have more than COUNT_ENTRIES entries (or there are so many pages that they would be
+//           read too often), references are copied by a launch before this one, and each sequence's workgroup adds to them.  (Us, in one
+//           launch and in two: 8 sequences 5.7 and 8.9, 64 of 64 entries 7.0 and 8.5, 1000 of 4 7.3 and 8.9, two of 2000 6.7 and 8.9; 128
+//           of 64, whose tails take as long, 11.1 and 9.1; 256 of 63 18.0 and 14.1.)
 //   tables  a sequence of `to`: its table, its length.  A sequence that stays where it is changes no reference
 //   leave   a sequence of `from`, where it takes its references away itself
 //   tails   a head's keys or values of a sequence
-constexpr int COUNT_PAGES = 4096, COUNT_SEQUENCES = 512, COUNT_ENTRIES = 4096;
+constexpr int COUNT_PAGES = 1024, COUNT_SEQUENCES = 1024, COUNT_ENTRIES = 4096, COUNT_READS = 1 << 22;
 struct CopyGrid {
   unsigned counts, leave;  // workgroups
-  int row_bytes;
+  int row_bytes, lane_shift;
 };
 
-__device__ __forceinline__ void count_references(const wave_pages& from, const wave_pages& to, const int32_t* parent, int p0) {
-  __shared__ int count[COUNT_PAGES], source[COUNT_SEQUENCES], held[COUNT_SEQUENCES];
-  const int pages = min(COUNT_PAGES, from.n_pages - p0), all = to.B + from.B, shift = page_shift(from.page);
-  for (int i = threadIdx.x; i < pages; i += 256) count[i] = from.references[p0 + i];
-  for (int i = threadIdx.x; i < all; i += 256) {
-    const int b = i < to.B ? i : i - to.B, p = b < to.B ? parent_of(from, parent, b) : -1, s = i < to.B ? p : b;
-    source[i] = max(s, 0);
-    held[i] = s < 0 || p == b ? 0 : pages_length(from, s) >> shift;
+__device__ __forceinline__ void count_references(const wave_pages& from, const wave_pages& to, const int32_t* parent, int p0, int lane_shift) {
+  // what a sequence of `from` adds to its pages' references: the sequences of `to` that come from it elsewhere, less itself if it leaves
+  __shared__ int count[COUNT_PAGES], weight[COUNT_SEQUENCES], held[COUNT_SEQUENCES];
+  const int pages = min(COUNT_PAGES, from.n_pages - p0), shift = page_shift(from.page);
+  for (int i = threadIdx.x; i < pages; i += THREADS) count[i] = from.references[p0 + i];
+  for (int s = threadIdx.x; s < from.B; s += THREADS) {
+    weight[s] = s < to.B && parent[s] == s ? 0 : -1;
+    held[s] = pages_length(from, s) >> shift;
   }
   __syncthreads();
+  for (int b = threadIdx.x; b < to.B; b += THREADS) {
+    const int s = parent_of(from, parent, b);
+    if (s >= 0 && s != b) atomicAdd(&weight[s], 1);
+  }
+  __syncthreads();
+  // 2^lane_shift lanes a row of the table
   constexpr int BATCH = 8;
-  const int entries = all * from.max_pages;
-  for (int i0 = threadIdx.x; i0 < entries; i0 += 256 * BATCH) {
-    int page[BATCH], at[BATCH], column[BATCH];
+  const int lane = threadIdx.x & ((1 << lane_shift) - 1), rows = THREADS >> lane_shift;
+  for (int s0 = threadIdx.x >> lane_shift; s0 < from.B; s0 += rows * BATCH) {
+    int w[BATCH], end[BATCH], most = 0;
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
-      const int i = min(i0 + k * 256, entries - 1);
-      at[k] = i / from.max_pages;
-      column[k] = i - at[k] * from.max_pages;
-      page[k] = page_entry(from, source[at[k]], column[k]);
+      const int s = s0 + k * rows;
+      w[k] = s < from.B ? weight[s] : 0;
+      end[k] = w[k] ? held[s] : 0;
+      most = max(most, end[k]);
     }
+    for (int column = lane; column < most; column += 1 << lane_shift) {
+      int page[BATCH];
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k)
-      if (i0 + k * 256 < entries && column[k] < held[at[k]] && page[k] >= p0 && page[k] < p0 + pages)
-        atomicAdd(&count[page[k] - p0], at[k] < to.B ? 1 : -1);
+      for (int k = 0; k < BATCH; ++k) page[k] = page_entry(from, min(s0 + k * rows, from.B - 1), column);
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k)
+        if (column < end[k] && page[k] >= p0 && page[k] < p0 + pages) atomicAdd(&count[page[k] - p0], w[k]);
+    }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < pages; i += 256) to.references[p0 + i] = count[i];
+  for (int i = threadIdx.x; i < pages; i += THREADS) to.references[p0 + i] = count[i];
 }
 
 __global__ __launch_bounds__(256) void pages_copy_kernel(const wave_pages from, const wave_pages to, const int32_t* parent, const CopyGrid grid) {
   unsigned block = workgroup_number();
   const int shift = page_shift(from.page);
   if (block < grid.counts) {
-    count_references(from, to, parent, block * COUNT_PAGES);
+    count_references(from, to, parent, block * COUNT_PAGES, grid.lane_shift);
     return;
   }
   block -= grid.counts;
@@ -1062,9 +1073,10 @@ wave_status launch_pages_reorder(const wave_pages& from, const wave_pages& to, c
   } else {
     CopyGrid g{};
     g.row_bytes = from.d * (from.dtype == WAVE_BF16 ? 2 : 4);
-    const long long all = (long long)to.B + from.B;
-    if (all <= COUNT_SEQUENCES && all * from.max_pages <= COUNT_ENTRIES) {
-      g.counts = (unsigned)(((long long)from.n_pages + COUNT_PAGES - 1) / COUNT_PAGES);
+    const long long entries = (long long)from.B * from.max_pages, blocks = ((long long)from.n_pages + COUNT_PAGES - 1) / COUNT_PAGES;
+    if (from.B <= COUNT_SEQUENCES && to.B <= 4 * COUNT_SEQUENCES && entries <= COUNT_ENTRIES && entries * blocks <= COUNT_READS) {
+      g.counts = (unsigned)blocks;
+      while (g.lane_shift < 8 && 1 << g.lane_shift < from.max_pages) ++g.lane_shift;
     } else {
       g.leave = from.B;
       WAVE_LAUNCH("pages_references", pages_references_kernel, grid_rows(((long long)from.n_pages + 255) / 256), 256, 0, st,

@@ -717,7 +717,8 @@ def test_reorder_copies_forks_and_frees():
 
 
 @pytest.mark.parametrize("B,to_B,most,n_pages", [(3, 5, 2, 4096), (40, 33, 56, 9000), (40, 33, 57, 9000), (200, 312, 8, 20000), (200, 313, 7, 20000),
-                                                 (1, 4000, 3, 5), (40, 33, 450, 9000)])
+                                                 (1, 4000, 3, 5), (40, 33, 450, 9000), (64, 70, 64, 70000), (64, 64, 65, 9000), (1024, 900, 4, 5000), (1025, 1025, 3, 5000),
+                                                 (1000, 4096, 4, 1023), (10, 4097, 4, 1025), (2, 7, 2048, 4100), (2, 7, 2049, 4100), (16, 16, 256, 1100000)])
 def test_references_of_many_tables(B, to_B, most, n_pages):
     """Tables of as many entries as one launch counts and of more, pages that many sequences share; against sums in numpy."""
     rng = np.random.default_rng(B)
