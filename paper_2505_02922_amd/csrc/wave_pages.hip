@@ -208,10 +208,11 @@ __device__ __forceinline__ void norm_heads(const NormArgs& a, const HeadRows& va
         if (h < a.Hq) w = wq;
         if (h < heads) t.apply(w, sines, a.eps, u[i], v[i]);
         char* to = out(h, n);
+        if (!to) continue;
         if (a.past) {
           store16_stream(to + t.one * 16, u[i]);
           store16_stream(to + t.two * 16, v[i]);
-        } else if (to) {
+        } else {
           store16(to + t.one * 16, u[i]);
           store16(to + t.two * 16, v[i]);
         }

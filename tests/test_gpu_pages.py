@@ -1014,3 +1014,62 @@ def test_captured_steps_in_place_replay():
         for a, b in zip(wb.wave_pages_read(eager[0], 70), wb.wave_pages_read(captured[0], 70)):
             assert _same_bits(a, b), i
     assert captured[0].lengths.tolist() == [n + len(tokens) for n in (29, 60, 0, 31)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv", [(24, 8), (32, 0), (0, 32)])
+def test_norms_of_outputs_that_pass_by_the_caches(dtype, Hq, Hkv):
+    """Just above 32 MB of outputs, queries and keys or one of them alone: the rows of smaller calls, bit for bit."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(22)
+    d, n = 128, 4100 if dtype == "bf16" else 2053
+    size = 32 * n * d * (2 if dtype == "bf16" else 4)
+    assert 32 << 20 < size < 33 << 20
+    x = torch.randn(1, n, 34, d, generator=g, device="cuda").to(TYPES[dtype]).transpose(1, 2)
+    q, k = x[:, :Hq] if Hq else None, x[:, 32 - Hkv:32] if Hkv else None
+    w, r = (1 + 0.2 * torch.randn(d, generator=g, device="cuda")).to(TYPES[dtype]), wb.wave_rotary_plan(96, 1e4, [20, 28])
+    coords = torch.randint(0, 1 << 20, (2, 1, n), generator=g, device="cuda", dtype=torch.int32)
+    whole = wb.wave_norm_rotary_apply(q, k, w if Hq else None, w if Hkv else None, coords=coords, rotary=r)
+    for a in range(0, n, 1000):
+        part = wb.wave_norm_rotary_apply(*(None if t is None else t[:, :, a:a + 1000] for t in (q, k)), w if Hq else None, w if Hkv else None,
+                                         coords=coords[:, :, a:a + 1000], rotary=r)
+        for t, u in zip(whole, part):
+            assert (t is None) == (u is None) and (t is None or _same_bits(t[:, :, a:a + 1000], u)), a
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_append_with_queries_that_pass_by_the_caches(dtype):
+    """Ragged, with just above 32 MB of queries, in place and into a state beside: the rows of appends in pieces, bit for bit; those behind a
+    sequence's count, and what lies in front of and behind the output, as they were."""
+    B, Hq, Hkv, d, page, n = 2, 16, 2, 128, 64, 4100 if dtype == "bf16" else 2053
+    g = torch.Generator(device="cuda")
+    g.manual_seed(23)
+    q, k, v = (torch.randn(B, n, Hq + 2 * Hkv, d, generator=g, device="cuda").to(TYPES[dtype]).transpose(1, 2).split([Hq, Hkv, Hkv], 1))
+    size = B * Hq * n * d
+    assert 32 << 20 < size * q.element_size() < 33 << 20
+    w, r = (1 + 0.2 * torch.randn(d, generator=g, device="cuda")).to(TYPES[dtype]), wb.wave_rotary_plan(128, 1e4)
+    counts = torch.tensor([n - 1, n // 3], dtype=torch.int32, device="cuda")
+    new = lambda pool=None: wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, 140, 70, pool=pool)
+    states, outs, cuts = [], [], (0, 5, 900, 1800, n)
+    for apart in (False, True, None):
+        pages = new()
+        to = new(pages) if apart else pages
+        held = torch.full((size + 2 * d,), 7.0, dtype=TYPES[dtype], device="cuda")
+        out = held[d:-d].view(B, Hq, n, d)
+        if apart is None:
+            for a, b in zip(cuts, cuts[1:]):
+                part = torch.full((B, Hq, b - a, d), 7.0, dtype=TYPES[dtype], device="cuda")
+                wb.wave_pages_append(pages, k[:, :, a:b], v[:, :, a:b], q=q[:, :, a:b], q_weight=w, k_weight=w, rotary=r, counts=(counts - a).clamp(0, b - a),
+                                     q_out=part)
+                out[:, :, a:b] = part
+        else:
+            wb.wave_pages_append(pages, k, v, q=q, q_weight=w, k_weight=w, rotary=r, counts=counts, q_out=out, to=to)
+        states.append(to), outs.append(held)
+    assert bool((outs[0][:d] == 7.0).all()) and bool((outs[0][-d:] == 7.0).all())
+    out = outs[0][d:-d].view(B, Hq, n, d)
+    for b, count in enumerate(counts.tolist()):
+        assert bool((out[b, :, count:] == 7.0).all()) and not bool((out[b, :, :count] == 7.0).all(-1).any())
+    for s, o in zip(states[1:], outs[1:]):
+        assert _same_bits(o, outs[0]) and torch.equal(s.lengths, counts)
+        for x, y in zip(wb.wave_pages_read(s, n), wb.wave_pages_read(states[0], n)):
+            assert _same_bits(x, y)
