@@ -552,7 +552,8 @@ typedef struct {
  * Tokens that do not fit, in the table's row or because no page is free for them, are left out (their rows of q_out are
  * written): a sequence then ends one row before the page that it did not get, and lengths
  * says how many there are.  What the call writes must not overlap what it reads or writes otherwise.
- * WAVE_ERR_SHAPE: n_new above 2^30, B * n_new of 2^31 and more, B * Hq of 2^24 and more. */
+ * WAVE_ERR_SHAPE: n_new above 2^30, B * n_new of 2^31 and more, B * Hq of 2^24 and more; queries that are turned without
+ * coords where a token's number could pass 2^31 - 1: max_pages * page + page - 1 + n_new above 2^31. */
 size_t wave_pages_append_workspace(const wave_pages *from);
 wave_status wave_pages_append(const wave_pages *from, const wave_pages *to, const wave_rows *k_new,
                               const wave_rows *v_new, const wave_rows *q, int Hq, int n_new,

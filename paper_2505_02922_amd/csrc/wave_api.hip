@@ -881,6 +881,8 @@ wave_status wave_pages_append(const wave_pages* from, const wave_pages* to, cons
   const wave_pages& p = *from;
   if (!k_new || !v_new || n_new < 1 || (q && Hq < 1) || (coords && !rotary)) return WAVE_ERR_ARG;
   if (n_new > (1 << 30) || (long long)p.B * n_new >= (1ll << 31) || (q && (long long)p.B * Hq >= kMaxGrid)) return WAVE_ERR_SHAPE;
+  // (without coordinates the queries of tokens that find no room have numbers behind the table's)
+  if (q && rotary && !coords && (long long)p.max_pages * p.page + p.page - 1 + n_new > (1ll << 31)) return WAVE_ERR_SHAPE;
   PagesAppendArgs a{};
   NormArgs& r = a.rows;
   st = check_norm(norm, &r);

@@ -160,6 +160,25 @@ def test_append_refuses():
     assert call(qo=kn) == ARG and call(qo=q + 256) == ARG and call(ws=c.table & ~255) == ARG
 
 
+def test_append_refuses_tokens_whose_numbers_pass_31_bits():
+    """Without coordinates a token's position is its number: the last row that the table has room for, and n_new - 1 behind it (the
+    queries of tokens that find no room are turned too)."""
+    L = wb.lib()
+    c, rot = _pages(B=1, Hkv=1, d=64, page=128, n_pages=1, max_pages=1 << 23), wb.wave_rotary_plan(64, 1e4)
+    kn, q, qo, xy, ws = (i << 44 for i in range(1, 6))
+    once = wb.wave_rows(kn, 0, 0, 0)
+    most = (1 << 31) - (c.max_pages * c.page + c.page - 1)
+
+    def call(n, rot=rot, xy=None, q=wb.wave_rows(q, 0, 0, 0), qo=qo):
+        return L.wave_pages_append(c, c, once, once, q, 1, n, None, wb.wave_head_norm(kn + (1 << 40), None, 0.0), rot, xy, qo, ws, 1 << 20, None)
+
+    assert most < 1 << 30
+    for n in (most + 1, 1 << 30):
+        assert call(n) == SHAPE
+    if not torch.cuda.is_available():      # made-up addresses: the launch has to fail
+        assert call(most) == HIP and call(1 << 30, xy=xy) == HIP and call(1 << 30, rot=None) == HIP and call(1 << 30, q=None, qo=None) == HIP
+
+
 def test_read_refuses():
     L = wb.lib()
     c = _pages()
