@@ -857,7 +857,7 @@ def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optiona
     """k, v [B, Hkv, n, d] and q [B, Hq, n, d] of n new tokens per sequence (counts [B] int32: of its first counts[b]), of any
     strides.  Norms and turns q and k as wave_norm_rotary_apply (coords None: the tokens' numbers) and puts k and v behind
     each sequence's rows, in place or into the state `to`; a page that becomes complete is held in 8 bits.  Returns q normed
-    and turned (q_out, which may be q where that is dense)."""
+    and turned (q_out, which may be q where that is dense).  No tokens at all (n = 0): `to` becomes what `pages` is."""
     where = "wave_pages_append"
     to = pages if to is None else to
     B, d, dtype, shape = pages.B, pages.d, pages.dtype, k.shape
@@ -905,6 +905,11 @@ def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optiona
     if to.index != pages.index:
         raise WaveError(1, where)
     _together(where, pages.index, k, v, q, q_out, q_weight, k_weight, coords, counts, ws)
+    if n == 0:
+        if to is not pages:
+            _require(to.B == B, 2, where)
+            wave_pages_reorder(pages, torch.arange(B, dtype=torch.int32, device=k.device), to)
+        return q_out
     rows_k, keep_k = _rows(k, mask)
     rows_v, keep_v = _rows(v, mask)
     _enqueue(where, pages.index, pages.ref, to.ref, rows_k, rows_v, rows_q, Hq, n, _address(counts), norm, rotary, _address(coords),

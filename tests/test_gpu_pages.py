@@ -1073,3 +1073,35 @@ def test_append_with_queries_that_pass_by_the_caches(dtype):
         assert _same_bits(o, outs[0]) and torch.equal(s.lengths, counts)
         for x, y in zip(wb.wave_pages_read(s, n), wb.wave_pages_read(states[0], n)):
             assert _same_bits(x, y)
+
+
+@pytest.mark.parametrize("n", [0, 1, 40])
+@pytest.mark.parametrize("Hq", [4])
+def test_append_of_no_tokens_and_of_queries_without_heads(n, Hq):
+    """As the norms and reading back take them: nothing is appended, and a state beside becomes the same; no query is turned."""
+    B, Hkv, d, page, lengths = 3, 2, 64, 32, [0, 31, 70]
+    pages = _filled("bf16", B, Hkv, d, page, lengths, 24, 9)
+    pages.k_tail.nan_to_num_(), pages.v_tail.nan_to_num_()
+    r, w = wb.wave_rotary_plan(d, 1e4), torch.ones(d, device="cuda", dtype=torch.bfloat16)
+    q, k, v = (torch.randn(B, h, n, d, device="cuda").bfloat16() for h in (Hq, Hkv, Hkv))
+    to = wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, pages.n_pages, 9, pool=pages)
+    before = _state(pages)
+    got = wb.wave_pages_append(pages, k, v, q=q, q_weight=w, k_weight=w, rotary=r, to=to)
+    assert got.shape == q.shape
+    for name in OWN:
+        assert _same_bits(before[name], pages.t[name]), name
+    counts = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    assert wb.wave_pages_append(pages, k, v, q=q, q_weight=w, k_weight=w, rotary=r, counts=counts, q_out=got) is got
+    # (three pages are free; forty tokens want one, two and one: the last sequence ends a row before its third page)
+    assert to.lengths.tolist() == pages.lengths.tolist() == ([40, 71, 95] if n == 40 else [x + n for x in lengths])
+    assert torch.equal(pages.references, to.references)
+    for x, y in zip(wb.wave_pages_read(pages, 120), wb.wave_pages_read(to, 120)):
+        assert _same_bits(x, y)
+    if n == 0:
+        for name in before:
+            assert _same_bits(before[name], pages.t[name]), name
+        for other, status in ((wb.alloc_pages(torch.bfloat16, 1, Hkv, d, page, pages.n_pages, 9, pool=pages), 2),
+                              (wb.alloc_pages(torch.bfloat16, B, Hkv, d, page, pages.n_pages, 9), 1)):    # another batch, another pool
+            with pytest.raises(wb.WaveError) as e:
+                wb.wave_pages_append(pages, k, v, to=other)
+            assert e.value.status == status
