@@ -879,7 +879,8 @@ def wave_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optiona
             q_out = new(q, memory_format=torch.contiguous_format)
         else:
             _as_is(where, q_out, dtype, heads)
-        rows_q, keep_q = _rows(q, mask)
+        if Hq:
+            rows_q, keep_q = _rows(q, mask)
     else:
         q_out = None
     if coords is not None:

@@ -1076,7 +1076,7 @@ def test_append_with_queries_that_pass_by_the_caches(dtype):
 
 
 @pytest.mark.parametrize("n", [0, 1, 40])
-@pytest.mark.parametrize("Hq", [4])
+@pytest.mark.parametrize("Hq", [0, 4])
 def test_append_of_no_tokens_and_of_queries_without_heads(n, Hq):
     """As the norms and reading back take them: nothing is appended, and a state beside becomes the same; no query is turned."""
     B, Hkv, d, page, lengths = 3, 2, 64, 32, [0, 31, 70]
