@@ -1105,3 +1105,33 @@ def test_append_of_no_tokens_and_of_queries_without_heads(n, Hq):
             with pytest.raises(wb.WaveError) as e:
                 wb.wave_pages_append(pages, k, v, to=other)
             assert e.value.status == status
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,page", [(64, 32), (128, 64), (128, 128)])
+def test_what_eight_bits_cost_attention_has_a_bound(dtype, d, page):
+    """Attention over complete pages against fp64 attention over the raw rows that were appended.  A page's channel is off by at most e = s (1/2 +
+    127 * 4 u), s the page's scale (half a code; 1 / max, its products with 127 and the value, s), so a row's score by |q|_1 e / sqrt(d) <= D.
+    Each weight p is then p e^x / (sum of p e^x) with |x| <= D, off by at most (e^(2 D) - 1) p: the output by that of the sum of p |v|, and by
+    the values' own e; the normaliser's logarithm by D.  1e-4 is ten times what the kernel's sums may be off by."""
+    B, Hq, Hkv, lengths = 3, 8, 2, [4 * page, 5 * page + 7, page - 1]
+    g = _gen(25)
+    n = max(lengths)
+    k, v = (torch.randn(B, Hkv, n, d, generator=g).to(TYPES[dtype]).cuda() for _ in range(2))
+    q = _query(dtype, B, Hq, d, 25)
+    pages = wb.alloc_pages(TYPES[dtype], B, Hkv, d, page, 16, 6)
+    wb.wave_pages_append(pages, k, v, counts=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    out, lse = wb.wave_pages_attention_decode(q, pages)
+    for b, length in enumerate(lengths):
+        whole = length // page * page
+        for h in range(Hkv):
+            K, V, Q = k[b, h, :length].double(), v[b, h, :length].double(), q[b, h * 4:h * 4 + 4].double()
+            off = [torch.zeros(length, dtype=torch.float64, device="cuda") for _ in range(2)]
+            for x, e in ((K, off[0]), (V, off[1])):
+                e[:whole] = (x[:whole].view(-1, page * d).abs().amax(1) / 127 * (0.5 + 127 * 4 * U)).repeat_interleave(page)
+            z = Q @ K.T / math.sqrt(d)
+            D = Q.abs().sum(-1, keepdim=True) * off[0].max() / math.sqrt(d)
+            p, total = torch.softmax(z, -1), torch.logsumexp(z, -1)
+            bar = torch.expm1(2 * D) * (p @ V.abs()) + off[1].max() + 1e-4 * V.abs().max()
+            assert bool(((out[b, h * 4:h * 4 + 4].double() - p @ V).abs() <= bar).all()), (b, h)
+            assert bool(((lse[b, h * 4:h * 4 + 4].double() - total).abs() <= D[:, 0] + 1e-4).all()), (b, h)
