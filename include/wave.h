@@ -377,8 +377,9 @@ typedef struct {
  *   coords     DEVICE [n_axes,B,N] int32
  *   q_out, k_out  DEVICE [B,Hq,N,d] and [B,Hkv,N,d] dtype, dense, 16-byte aligned; each may be its own input
  *              where that is dense, and must not overlap anything else that the call reads or writes
- * Sums of squares, norms, sines and products are fp32 (angles as in wave_rotary_apply) and each
- * result is rounded once to dtype: a row whose squares add up to 2^128 and more has norm infinity.
+ * Sums of squares, norms, sines and products are fp32 and each result is rounded once to dtype: a row whose squares add
+ * up to 2^128 and more has norm infinity, squares below 2^-149 count as 0.  Angles are those of wave_rotary_apply, their sines and
+ * cosines nearer than there (to a last place, there to 2^-22), so a turned row may have other last bits than that call's.
  * Sizes as in wave_rotary_apply, with H = Hq + Hkv. */
 wave_status wave_norm_rotary_apply(const wave_rows *q, int Hq, const wave_rows *k, int Hkv,
                                    const wave_head_norm *norm, const wave_rotary *rotary,
@@ -513,6 +514,8 @@ wave_status wave_cache_evict(const wave_cache *from, const wave_cache *to, int n
  * on with the state that the last one left.  What only reads a state may run beside an append that leaves it as it is.
  * The library reads lengths and table on the device: a length outside 0 ..
  * max_pages * page + page - 1 and an entry outside 0 .. n_pages - 1 count as the nearest inside.
+ * max_pages and n_pages also choose between forms of a call, as lengths are the device's: short sequences have their fastest
+ * attention, reordering and appended token in a table and a pool that are not much larger than they need.
  * Every call returns WAVE_ERR_SHAPE for a page other than 32, 64 or 128, B * Hkv of 2^21 and more,
  * n_pages above 2^28, or max_pages * page above 2^30.
  * ------------------------------------------------------------------------- */
@@ -575,7 +578,9 @@ wave_status wave_pages_read(const wave_pages *pages, const int32_t *first, int n
  *   workspace     DEVICE, 256-byte aligned, >= wave_pages_attention_workspace(...)
  * A sequence without rows has out = 0 and lse = -infinity.  Scores are exact products of queries and codes, summed in fp32,
  * times the page's scale; the softmax and all sums are fp32, and a softmax weight meets the values' codes as three bf16
- * numbers that hold all its bits.  (references is not needed.)
+ * numbers that hold all its bits.  Sums are divided by the normaliser at their end, over weights of up to 2^8: they are no numbers where 2^8
+ * times a sequence's rows times its largest value passes 2^128, or d * 127 times the largest channel of a query does.
+ * (references is not needed.)
  * WAVE_ERR_SHAPE: Hq / Hkv not a whole number in 1 .. 8, or B * Hq of 2^24 and more. */
 size_t wave_pages_attention_workspace(const wave_pages *pages, int Hq);
 wave_status wave_pages_attention_decode(const void *q, int Hq, const wave_pages *pages, float *out, float *lse,

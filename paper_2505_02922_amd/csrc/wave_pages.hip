@@ -63,7 +63,7 @@ struct RowItem {
     y = fmaf(x, s, y * c);
     x = u;
   }
-  // All lanes of the row together.  x * (w / norm) in fp32, then the turn, then one rounding.
+  // All lanes of the row together.  (x * (1 / norm)) * w in fp32, then the turn, then one rounding.
   __device__ __forceinline__ void apply(const Weight& w, const Sines& t, float eps, uint4& a, uint4& b) const {
     if (!w.any && !turns) return;
     float x[EPC], y[EPC];
@@ -101,8 +101,8 @@ struct RowItem {
   }
 };
 
-// Cosine (x) and sine (y) of `turns` circles, off by little more than half a last place: the angle is cut to an eighth of a
-// circle in fp64, where whole and quarter circles come off without error, and its series (x^9 and x^10 in the last terms, the next ones
+// Cosine (x) and sine (y) of `turns` circles, off by less than 0.88 of a last place (0.873 the most of 2 * 10^8 angles around an eighth of
+// a circle, where both are furthest off; 0.84 of 3 * 10^7 anywhere): the angle is cut to an eighth of a circle in fp64, where whole and quarter circles come off without error, and its series (x^9 and x^10 in the last terms, the next ones
 // are below 2^-28 of the sums) take it as two floats.  (A function of one float is off by pi u for the rounding of its argument, and
 // by its own last places: four times as many rows would then be rounded to bf16 the other way.)
 __device__ __forceinline__ float2 cosine_and_sine(double turns) {
@@ -276,7 +276,8 @@ __device__ __forceinline__ void copy_chunks(const char* x, char* y, int chunks) 
 // Append, first launch (but see OwnToken): one workgroup finds how many tokens of each sequence fit and which pages they take.  A sequence's
 // share depends on what those before it take, and the free pages are found by going through references in ascending order,
 // so the pages are the same in every run.  It is a chain of loads and scans behind barriers: 4.1 us for 64 sequences and a pool of
-// 2600 pages (5.1 with sixteen loads and ballots a thread instead of four wide loads and one scan).
+// 2600 pages (5.1 with sixteen loads and ballots a thread instead of four wide loads and one scan), and about 1.5 us more for every 16384
+// pages in front of the last one wanted: with all but the last eight taken 3.9 us for 2600, 5.0 for 32768, 13.3 for 100000, 98 for a million.
 struct PagesPlan {
   int4* sequence;   // [B] rows before, rows after, its first one among the taken pages, tokens given
   int32_t* taken;   // [n_pages] the taken pages in ascending order
@@ -391,7 +392,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(const wave_pag
 //           unless they complete a page: then the pages' workgroups have little to do but in the one sequence of `page` that does
 //   lists   table and references of a state with arrays of its own
 // Four prompts of up to 8191 tokens, 32 and 8 heads, d = 128: 118 us, 553 MB, 4.7 TB/s (132 before the next head's rows were asked for
-// while this one's are rounded, and outputs passed by the caches).  One token of 64 sequences of 28 and 4 heads in place 4.8 us.
+// while this one's are rounded, and outputs passed by the caches).  One token of 64 sequences of 28 and 4 heads in place 4.8 us, 6.0 where one
+// of them completes a page.
 struct AppendGrid {
   unsigned reference_blocks;           // without a plan
   unsigned page_blocks, token_blocks;  // the others are lists
@@ -514,8 +516,10 @@ struct PageRows {
       if ((tid & 63) == 0) top[turn][tid >> 6] = most;
       __syncthreads();
       most = max(max(top[turn][0], top[turn][1]), max(top[turn][2], top[turn][3]));
-      // (below 2^-100, where 127 / max may be infinite, the page counts as zeros.  The quotient as a reciprocal and a product, as most
-      // implementations of one array of quotients have it, rounds twice: that moves a code that is within 2e-5 of a border.)
+      // (below 2^-100, where 127 / max may be infinite, the page counts as zeros.  The definition has the quotient as a reciprocal and a
+      // product, two roundings for 127 / max's one.  With the product that follows x * inv is off by up to 3 u of itself, 2.3e-5 at 127: a
+      // code may fall otherwise where its value lies as near to a border, 1.5e-5 with the one quotient.  From 2^126 on 1 / max is
+      // subnormal and off by up to 2^-22 of itself: 4.6e-5.)
       const bool number = most < 0x7f800000u, some = most >= 0x0d800000u;
       const float inv = number && some ? 1.f / __uint_as_float(most) * 127.f : 0.f;
       const float scale = !number ? __uint_as_float(0x7fc00000u) : some ? __uint_as_float(most) / 127.f : 0.f;
@@ -555,7 +559,8 @@ struct PageRows {
 // token completes a page has to look further than its sequence's length: at the other lengths, for how many before it do, and at
 // references; the rows are on their way meanwhile.  In one launch (with a plan's, us; calls in a row, so the host's part too): 64
 // sequences of 28 and 4 heads 10.7 (14.2), kernels 8.4 (4.0 + 6.2); 256 of them with 15.8K pages 16.1 (18.2), 16.1 (4.6 + 12.5); where
-// all complete a page the kernels are even.  Beyond these numbers of sequences and pages the plan, which reads them once.
+// all complete a page the kernels are even.  Beyond these numbers of sequences and pages the plan, which reads them once: the 64 sequences in
+// a pool of 65536 pages, with the rows read back, 19.5 for 16.5.
 // The functions below take all threads together.  Their loads stand side by side without conditions: behind one each would be waited
 // for alone (12.5 -> 18.9 for 256 sequences).
 constexpr int OWN_SEQUENCES = 4 * THREADS, OWN_PAGES = 64 * THREADS, OWN_REFERENCES = 4;
@@ -938,7 +943,8 @@ __global__ __launch_bounds__(256) void pages_references_kernel(const int32_t* fr
 //           whose pages gain or lose.  Where these have more than COUNT_ENTRIES entries (or there are so many pages that they would be
 //           read too often), references are copied by a launch before this one, and each sequence's workgroup adds to them.  (Us, in one
 //           launch and in two: 8 sequences 5.7 and 8.9, 64 of 64 entries 7.0 and 8.5, 1000 of 4 7.3 and 8.9, two of 2000 6.7 and 8.9; 128
-//           of 64, whose tails take as long, 11.1 and 9.1; 256 of 63 18.0 and 14.1.)
+//           of 64, whose tails take as long, 11.1 and 9.1; 256 of 63 18.0 and 14.1.)  The host knows the table's entries, not those in
+//           use: eight beams of six pages take 5.7 in a table of six entries a row, 8.4 in one of 1024
 //   tables  a sequence of `to`: its table, its length.  A sequence that stays where it is changes no reference
 //   leave   a sequence of `from`, where it takes its references away itself
 //   tails   a head's keys or values of a sequence

@@ -10,10 +10,11 @@ namespace {
 // A step: 32 rows of one page against 16 query columns.  Codes are whole numbers up to 127, which bf16 holds, so the products
 // are those of the plain cache's bf16 step with the codes widened on the way; the page's scales are the same for the whole
 // step, one inside the exponent, the other on the weights.  An fp32 query is three bf16 numbers that hold all its bits.
-// Eight sequences of 3001 .. 65536 rows, 32 and 8 heads, d = 128: 88.8 us, 562 MB (what is fetched, to 1 %), 6.3 TB/s, more than a plain
+// Eight sequences of 3001 .. 65536 rows, 32 and 8 heads, d = 128: 88.8 us, 562 MB (576 fetched), 6.3 TB/s, more than a plain
 // read's 5.57.  A step is about 325 vector instructions, 128 of them the widening (one a code and one for two); they keep the vector
-// units busy for 49 % of the time that a CU has work, 53 % at d = 64, 66 % where 64 sequences of up to 4351 rows begin alike and a
-// third of the rows come from the caches (28.7 us, 165 MB of which 116 are fetched).  Neither they nor the products bound that: with the
+// units busy for 49 % of the time that a CU has work, 58 % at d = 64, 51 % for 64 sequences of 700 .. 4351 rows on four KV heads (39.8 us with
+// the join, 169 MB; fp32, three products for one, 46 % of a longer time, 50.9), and 66 % where those begin alike and a third of the rows
+// come from the caches (28.1 us, 165 MB of which 118 are fetched, 4.2 TB/s).  Neither the widening nor the products bound that: with the
 // codes taken for bf16 as they are, and a product less a channel, the call took 31.4 us instead of 33.3.
 // ----------------------------------------------------------------------------
 template <typename T, int D>
@@ -367,7 +368,9 @@ PagesAttendGeom pages_attend_geometry(const wave_pages& p, int Hq) {
   // them: up to two steps for up to 512 units, four from 128, eight from 256 on.  (In pieces and in one launch, bf16, d = 128, us: one
   // sequence of 500 rows on eight KV heads 10.8 and 8.0; 32 of 160 .. 500 14.7 and 10.0, of 300 .. 1000 18.6 and 14.0, of 700 .. 2000 27.0
   // and 22.3; 64 of 700 .. 2000 42.0 and 39.3.  8 of 1000 11.4 and 11.6, 16 of 2000 16.6 and 18.3, 256 of 500 54 and 61.)  With many
-  // sequences every piece's workgroup would read all their lengths.
+  // sequences every piece's workgroup would read all their lengths.  The rule goes by the table's room, since the lengths are the
+  // device's: in a table of 1024 pages the same short sequences are cut into pieces (3 of up to 200 6.6 and 10.1, one of 500 8.0 and 10.3, 32
+  // of 160 .. 500 10.1 and 14.6, of 300 .. 1000 14.8 and 19.2).
   const long long steps = (room + SHORT_WAVES * 32 - 1) / (SHORT_WAVES * 32), units = (long long)p.B * p.Hkv;
   g.one_launch = steps <= 1 || (steps <= 2 && (units <= 512 || p.B > 512)) ||
                  (units <= 512 && ((steps <= 4 && units >= 128) || (steps <= 8 && units >= 256)));

@@ -1,4 +1,6 @@
-// Turning rows by their positions: what the kernels that do it share.
+// Turning rows by their positions: the plain cache's turn (Turn), and what the kernels that norm rows first share with it (packing,
+// the shape of a workgroup).  Those take their sines from LDS, where each is formed once and from two floats; Turn's are a function of one
+// float and off by up to 2^-22, so the same row may be rounded the other way there.
 #pragma once
 
 #include "wave_common.h"
